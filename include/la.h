@@ -292,6 +292,85 @@ la_status la_decode_steps(const la_shape* shape, const void* q, const void* k, c
                           const float* lambda_host, float* kv, void* o, void* stream);
 
 /*
+ * The gated delta rule: linear attention whose state gives up what it holds for a key before it takes the key's new value, with a
+ * decay per token.  Per batch and value head h, with q and k of key head h / (H / Hk) and a state S [d,e]:
+ *   S_t = exp(g_t) (S_{t-1} - beta_t k_t (k_t^T S_{t-1})) + beta_t k_t v_t^T,      o_t = scale S_t^T q_t.
+ *   q, k         [B,Hk,N,d] (LA_LAYOUT_BHND) or [B,N,Hk,d] (LA_LAYOUT_BNHD), in_dtype; keys are taken as they are (a layer makes them
+ *                of unit length first: with |k| <= 1 and 0 <= beta <= 2 a step does not enlarge the state);
+ *   v, d_o       [B,H,N,e] or [B,N,H,e], in_dtype;       o, dq, dk, dv  as q, k, v, out_dtype;
+ *   g, beta      DEVICE, [B,H,N] or [B,N,H] fp32: log decay (-inf forgets everything; meant to be <= 0) and writing strength, any
+ *                value, 0 included: a token with g = 0 and beta = 0 leaves the state as it is (padding behind a sequence);
+ *   dg, dbeta    the same layout, fp32;
+ *   states       [B,H,d,e] fp32, as those of la_fwd; kv_in / kv_out / grad_kv_out / grad_kv_in may be NULL.
+ * d == e in {64, 128}; 1 <= Hk <= H, H a multiple of Hk; B * H <= 65535; types as in la_shape.  Accumulation and states are fp32.  bf16
+ * inputs run on the tensor cores (path AUTO or TENSOR), where operands formed on chip are carried as two bf16 terms (x to 2^-17);
+ * fp32 inputs, and path SIMT, on the CUDA cores.
+ *
+ *   la_delta_fwd     all tokens, from kv_in (NULL: zeros).  workspace: la_delta_workspace_bytes(LA_OP_FWD, shape) bytes, 256-byte
+ *                    aligned; calls that share one must be stream-ordered.  Linear in N: a state and the operands that lead from one to
+ *                    the next for every chunk of 128 (CUDA cores: 64) tokens of a head.
+ *   la_delta_bwd     gradients of <o, d_o> + <kv_out, grad_kv_out>; those of shared heads are summed over the heads that share them.
+ *                    fwd_workspace: the workspace of a preceding la_delta_fwd of the same shape, inputs and kv_in, untouched since (it
+ *                    is only read), or NULL: its contents are then made again.  workspace: la_delta_workspace_bytes(LA_OP_BWD, shape)
+ *                    bytes, or less by those of LA_OP_FWD where fwd_workspace is given; it must not overlap fwd_workspace.
+ *   la_delta_steps   shape->N >= 1 tokens one after the other on a state that is read once, kept on chip and written once, IN PLACE:
+ *                    decoding.  Needs no workspace.  N calls with one token give the bits of one call with N.
+ * Sums run in a fixed order: the same call gives the same bits.
+ */
+typedef struct {
+  int B, H, Hk, N, d, e;
+  la_dtype in_dtype, out_dtype;
+  int path;    /* la_path */
+  int layout;  /* la_layout */
+  float scale; /* of q; finite */
+} la_delta_shape;
+
+size_t la_delta_workspace_bytes(int op, const la_delta_shape* shape);
+la_status la_delta_fwd(const la_delta_shape* shape, const void* q, const void* k, const void* v, const float* g, const float* beta,
+                       void* o, const float* kv_in, float* kv_out, void* workspace, size_t workspace_bytes, void* stream);
+la_status la_delta_bwd(const la_delta_shape* shape, const void* q, const void* k, const void* v, const float* g, const float* beta,
+                       const void* d_o, void* dq, void* dk, void* dv, float* dg, float* dbeta, const float* kv_in,
+                       const float* grad_kv_out, float* grad_kv_in, const void* fwd_workspace, void* workspace,
+                       size_t workspace_bytes, void* stream);
+la_status la_delta_steps(const la_delta_shape* shape, const void* q, const void* k, const void* v, const float* g, const float* beta,
+                         float* kv, void* o, void* stream);
+
+/*
+ * What stands between two blocks of a model, per token's row of D features, with rms(a) = sqrt(mean(a^2) + eps):
+ *   z = y / rms(y) (.) w_post (.) act(u)      norm and gate of the block's output y (post_norm = 0: without the norm)
+ *   h = x + s (.) z                            residual stream
+ *   n = h / rms(h) (.) w_pre                   what the next block reads
+ * eps = 0 is Eq. 8's SimpleRMSNorm: a row of zeros gives zeros.
+ *   x, h, dh, dx         [rows, D] res_dtype (n is made from h before it is rounded);
+ *   y, u, n, dn, dy, du  [rows, D] dtype;  u NULL: no gate;  gate: LA_GATE_*, act(u) = u, sigmoid(u) or u sigmoid(u);
+ *   w_post, s, w_pre     DEVICE [D] fp32, or NULL for ones;
+ *   la_block_norm_fwd    h or n may be NULL (not wanted), not both;
+ *   la_block_norm_bwd    gradients of <h, dh> + <n, dn>, everything made again from x, y and u; dh or dn may be NULL (zero), not both;
+ *                        dw_post, ds, dw_pre [D] fp32 may be NULL; du is required with u.  workspace:
+ *                        la_block_norm_workspace_bytes(shape), 256-byte aligned.
+ * dtype BF16 with res_dtype BF16 or F32, or both F32; 1 <= D <= 16384 (a multiple of 8 moves 16 bytes at a time), rows >= 1.  Sums
+ * are fp32 and run in a fixed order.
+ */
+#define LA_GATE_PLAIN 0
+#define LA_GATE_SIGMOID 1
+#define LA_GATE_SILU 2
+typedef struct {
+  long long rows;
+  int D;
+  la_dtype dtype, res_dtype;
+  int gate;      /* LA_GATE_* (ignored without u) */
+  int post_norm; /* 1: norm of y, 0: none */
+  float eps;     /* >= 0 */
+} la_block_norm_shape;
+
+size_t la_block_norm_workspace_bytes(const la_block_norm_shape* shape);
+la_status la_block_norm_fwd(const la_block_norm_shape* shape, const void* x, const void* y, const void* u, const float* w_post,
+                            const float* s, const float* w_pre, void* h, void* n, void* stream);
+la_status la_block_norm_bwd(const la_block_norm_shape* shape, const void* x, const void* y, const void* u, const float* w_post,
+                            const float* s, const float* w_pre, const void* dh, const void* dn, void* dx, void* dy, void* du,
+                            float* dw_post, float* ds, float* dw_pre, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * Forward pass without caller-provided scratch (the paper has no counterpart; this is a
  * deployment convenience).  Same result as la_fwd, but the per-segment state scratch comes
  * from a fixed LA_NOALLOC_SCRATCH_BYTES array that is part of the library's device image,

@@ -24,11 +24,14 @@ LA_SPLIT_SCORES, LA_SPLIT_STATE, LA_SPLIT_DECAYED = 1, 2, 4
 LA_PRECISION_DEFAULT = -1
 LA_OP_FWD, LA_OP_BWD, LA_OP_DECODE = 0, 1, 2
 LA_LAYOUT_BHND, LA_LAYOUT_BNHD = 0, 1
+LA_GATE_PLAIN, LA_GATE_SIGMOID, LA_GATE_SILU = 0, 1, 2
 
 EXPORTS = ("la_workspace_bytes", "la_segment_length", "la_fwd", "la_bwd", "la_decode_step",
            "la_status_string", "la_version", "la_launch_count", "la_profile_enable",
            "la_profile_collect", "la_host_arena_bytes", "la_fwd_bwd_host", "la_device_status", "la_fwd_noalloc", "la_bwd_reuse",
            "la_selftest_bounded_wait", "la_fwd_gated", "la_gate_bwd", "la_gate_fwd", "la_decode_steps", "la_varlen_workspace_bytes", "la_fwd_varlen",
+           "la_delta_workspace_bytes", "la_delta_fwd", "la_delta_bwd", "la_delta_steps", "la_block_norm_workspace_bytes", "la_block_norm_fwd",
+           "la_block_norm_bwd",
            "la_bwd_varlen", "la_lrpe_workspace_bytes", "la_lrpe_fwd", "la_lrpe_bwd", "la_chunk_state_workspace_bytes", "la_chunk_state", "la_chain_states")
 LA_NOALLOC_SCRATCH_BYTES = 32 << 20
 KERNEL_KINDS = ("prepass", "scan", "walk", "decode", "walk_pair", "gate", "lrpe")
@@ -39,6 +42,17 @@ class LaShape(ctypes.Structure):
                 ("e", ctypes.c_int), ("in_dtype", ctypes.c_int), ("out_dtype", ctypes.c_int),
                 ("seg_len", ctypes.c_int), ("path", ctypes.c_int), ("precision", ctypes.c_int),
                 ("layout", ctypes.c_int)]
+
+
+class LaDeltaShape(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int), ("H", ctypes.c_int), ("Hk", ctypes.c_int), ("N", ctypes.c_int), ("d", ctypes.c_int),
+                ("e", ctypes.c_int), ("in_dtype", ctypes.c_int), ("out_dtype", ctypes.c_int), ("path", ctypes.c_int),
+                ("layout", ctypes.c_int), ("scale", ctypes.c_float)]
+
+
+class LaBlockNormShape(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_longlong), ("D", ctypes.c_int), ("dtype", ctypes.c_int), ("res_dtype", ctypes.c_int),
+                ("gate", ctypes.c_int), ("post_norm", ctypes.c_int), ("eps", ctypes.c_float)]
 
 
 class LaError(RuntimeError):
@@ -109,6 +123,21 @@ def load():
         lib.la_chain_states.restype = I
         lib.la_decode_steps.argtypes = [sp, vp, vp, vp, fp, vp, vp, vp]
         lib.la_decode_steps.restype = I
+        dp, np_ = ctypes.POINTER(LaDeltaShape), ctypes.POINTER(LaBlockNormShape)
+        lib.la_delta_workspace_bytes.argtypes = [I, dp]
+        lib.la_delta_workspace_bytes.restype = sz
+        lib.la_delta_fwd.argtypes = [dp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        lib.la_delta_fwd.restype = I
+        lib.la_delta_bwd.argtypes = [dp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        lib.la_delta_bwd.restype = I
+        lib.la_delta_steps.argtypes = [dp, vp, vp, vp, vp, vp, vp, vp, vp]
+        lib.la_delta_steps.restype = I
+        lib.la_block_norm_workspace_bytes.argtypes = [np_]
+        lib.la_block_norm_workspace_bytes.restype = sz
+        lib.la_block_norm_fwd.argtypes = [np_, vp, vp, vp, vp, vp, vp, vp, vp, vp]
+        lib.la_block_norm_fwd.restype = I
+        lib.la_block_norm_bwd.argtypes = [np_, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        lib.la_block_norm_bwd.restype = I
         lib.la_host_arena_bytes.argtypes = [sp]
         lib.la_host_arena_bytes.restype = sz
         lib.la_fwd_bwd_host.argtypes = [sp, vp, vp, vp, vp, fp, vp, vp, vp, vp, vp, sz, vp]
@@ -132,7 +161,7 @@ def load():
             raise RuntimeError("extension module _la_call is missing; run `python -m paper_2307_14995_b200.build`") from e
         address = {name: ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in EXPORTS}
         address["la_bwd"] = address["la_bwd_reuse"]  # (the same with a NULL fwd_workspace)
-        _la_call.bind(LaShape, _handle)
+        _la_call.bind(LaShape, _handle, LaDeltaShape, LaBlockNormShape)
         # whoever sees _call finds the whole table behind it
         _address = address
         _call = _la_call.call
@@ -141,8 +170,8 @@ def load():
 
 
 def _enter(name: str, kinds: str, *args) -> None:
-    """Calls a C function; kinds has a letter for each argument (s: shape, t: tensor or None, i: integer,
-    h: host memory, r: stream)."""
+    """Calls a C function; kinds has a letter for each argument (s, d, n: shape of the core, the delta rule, the norms; t: tensor or None,
+    i: integer, h: host memory, r: stream)."""
     if _call is None:
         load()
     rc = _call(_address[name], kinds, *args)
@@ -369,6 +398,124 @@ def la_lrpe_bwd(shape: LaShape, q, k, v, do, theta, lam, dq, dk, dv, dtheta, pos
                 grad_kv_in=None, workspace=None, stream=None):
     _enter("la_lrpe_bwd", "sttttthittttttttir", shape, q, k, v, do, theta, _lam(lam), int(pos0), dq, dk, dv, dtheta, kv_in, grad_kv_out,
            grad_kv_in, workspace, _bytes(workspace), stream)
+
+
+# ---- the gated delta rule, and the norms between two blocks -------------------------------
+# Their gates, weights and shared heads make it easy to hand over a tensor of another type or size than the shape says, which would be
+# read out of bounds; so types, sizes and device are looked at here (1 us for a decode step).
+_TORCH = {LA_BF16: torch.bfloat16, LA_F32: torch.float32}
+
+
+def _matches(name, device, tensors, dtype, numel):
+    for what, t in tensors.items():
+        if t is None:
+            continue
+        if t.dtype is not dtype or t.numel() != numel:
+            raise ValueError("%s: %s has to be %s with %d elements, not %s with %d" % (name, what, dtype, numel, t.dtype, t.numel()))
+        if t.get_device() != device:
+            raise ValueError("%s: %s has to be on the current CUDA device" % (name, what))
+
+
+def _current_device() -> int:
+    return torch.cuda.current_device() if _CURRENT_DEVICE is None or not torch.cuda.is_initialized() else _CURRENT_DEVICE()
+
+
+def make_delta_shape(B, H, N, d, e, in_dtype, out_dtype, Hk=None, scale=1.0, path=LA_PATH_AUTO, layout=LA_LAYOUT_BHND) -> LaDeltaShape:
+    """H value heads; Hk (default H) heads of q and k, each shared by H / Hk value heads."""
+    return LaDeltaShape(B, H, H if Hk is None else Hk, N, d, e, _DT[in_dtype], _DT[out_dtype], path, layout, scale)
+
+
+def delta_workspace_bytes(op: int, shape: LaDeltaShape) -> int:
+    n = load().la_delta_workspace_bytes(op, ctypes.byref(shape))
+    if n == ctypes.c_size_t(-1).value:
+        raise LaError(2, "la_delta_workspace_bytes")
+    return int(n)
+
+
+def alloc_delta_workspace(op: int, shape: LaDeltaShape, device) -> torch.Tensor:
+    return torch.empty(delta_workspace_bytes(op, shape), dtype=torch.uint8, device=device)
+
+
+def _delta_checks(name, s, q, k, v, g, beta, outs, qk_outs, gates, states, workspaces, more_in=()):
+    if type(s) is not LaDeltaShape:
+        raise TypeError("a delta shape is expected, not %s" % type(s).__name__)
+    device, inp, out = _current_device(), _TORCH.get(s.in_dtype), _TORCH.get(s.out_dtype)
+    rows = s.B * s.N
+    _matches(name, device, {"q": q, "k": k}, inp, rows * s.Hk * s.d)
+    _matches(name, device, {"v": v, **dict(more_in)}, inp, rows * s.H * s.e)
+    _matches(name, device, {"g": g, "beta": beta, **gates}, torch.float32, rows * s.H)
+    _matches(name, device, outs, out, rows * s.H * s.e)
+    if qk_outs:
+        _matches(name, device, qk_outs, out, rows * s.Hk * s.d)
+    _matches(name, device, states, torch.float32, s.B * s.H * s.d * s.e)
+    for w in workspaces:
+        if w is not None and w.get_device() != device:
+            raise ValueError("%s: workspaces have to be on the current CUDA device" % name)
+
+
+def la_delta_fwd(shape: LaDeltaShape, q, k, v, g, beta, o, kv_in=None, kv_out=None, workspace=None, stream=None):
+    """Gated delta rule over all tokens: q, k have shape.Hk heads, v and o shape.H; g (log decay) and beta are fp32, one per token and
+    value head, in the layout of v without its features."""
+    _delta_checks("la_delta_fwd", shape, q, k, v, g, beta, {"o": o}, None, {}, {"kv_in": kv_in, "kv_out": kv_out}, (workspace,))
+    _enter("la_delta_fwd", "dtttttttttir", shape, q, k, v, g, beta, o, kv_in, kv_out, workspace, _bytes(workspace), stream)
+
+
+def la_delta_bwd(shape: LaDeltaShape, q, k, v, g, beta, do, dq, dk, dv, dg, dbeta, kv_in=None, grad_kv_out=None, grad_kv_in=None,
+                 workspace=None, stream=None, fwd_workspace=None):
+    """fwd_workspace: the workspace of the matching la_delta_fwd call, whose contents are otherwise made again."""
+    _delta_checks("la_delta_bwd", shape, q, k, v, g, beta, {"dv": dv}, {"dq": dq, "dk": dk}, {"dg": dg, "dbeta": dbeta},
+                  {"kv_in": kv_in, "grad_kv_out": grad_kv_out, "grad_kv_in": grad_kv_in}, (workspace, fwd_workspace), {"do": do})
+    if fwd_workspace is not None and _bytes(fwd_workspace) < delta_workspace_bytes(LA_OP_FWD, shape):
+        raise LaError(3, "la_delta_bwd (fwd_workspace)")
+    _enter("la_delta_bwd", "dttttttttttttttttir", shape, q, k, v, g, beta, do, dq, dk, dv, dg, dbeta, kv_in, grad_kv_out, grad_kv_in,
+           fwd_workspace, workspace, _bytes(workspace), stream)
+
+
+def la_delta_steps(shape: LaDeltaShape, q, k, v, g, beta, kv, o, stream=None):
+    """shape.N consecutive tokens on the state kv, updated in place: decoding."""
+    _delta_checks("la_delta_steps", shape, q, k, v, g, beta, {"o": o}, None, {}, {"kv": kv}, ())
+    _enter("la_delta_steps", "dtttttttr", shape, q, k, v, g, beta, kv, o, stream)
+
+
+def make_block_norm_shape(rows, D, dtype, res_dtype, eps=0.0, gate=LA_GATE_PLAIN, post_norm=True) -> LaBlockNormShape:
+    return LaBlockNormShape(rows, D, _DT[dtype], _DT[res_dtype], gate, int(bool(post_norm)), eps)
+
+
+def block_norm_workspace_bytes(shape: LaBlockNormShape) -> int:
+    n = load().la_block_norm_workspace_bytes(ctypes.byref(shape))
+    if n == ctypes.c_size_t(-1).value:
+        raise LaError(2, "la_block_norm_workspace_bytes")
+    return int(n)
+
+
+def alloc_block_norm_workspace(shape: LaBlockNormShape, device) -> torch.Tensor:
+    return torch.empty(block_norm_workspace_bytes(shape), dtype=torch.uint8, device=device)
+
+
+def _norm_checks(name, s, rows, res_rows, weights, workspace=None):
+    if type(s) is not LaBlockNormShape:
+        raise TypeError("a block norm shape is expected, not %s" % type(s).__name__)
+    device = _current_device()
+    _matches(name, device, rows, _TORCH.get(s.dtype), s.rows * s.D)
+    _matches(name, device, res_rows, _TORCH.get(s.res_dtype), s.rows * s.D)
+    _matches(name, device, weights, torch.float32, s.D)
+    if workspace is not None and workspace.get_device() != device:
+        raise ValueError("%s: the workspace has to be on the current CUDA device" % name)
+
+
+def la_block_norm_fwd(shape: LaBlockNormShape, x, y, u=None, w_post=None, s=None, w_pre=None, h=None, n=None, stream=None):
+    """h = x + s (.) norm(y) (.) w_post (.) act(u), n = norm(h) (.) w_pre: norm and gate of a block's output y, the residual stream x
+    and h, the next block's input n."""
+    _norm_checks("la_block_norm_fwd", shape, {"y": y, "u": u, "n": n}, {"x": x, "h": h}, {"w_post": w_post, "s": s, "w_pre": w_pre})
+    _enter("la_block_norm_fwd", "nttttttttr", shape, x, y, u, w_post, s, w_pre, h, n, stream)
+
+
+def la_block_norm_bwd(shape: LaBlockNormShape, x, y, u, w_post, s, w_pre, dh, dn, dx, dy, du=None, dw_post=None, ds=None, dw_pre=None,
+                      workspace=None, stream=None):
+    _norm_checks("la_block_norm_bwd", shape, {"y": y, "u": u, "dn": dn, "dy": dy, "du": du}, {"x": x, "dh": dh, "dx": dx},
+                 {"w_post": w_post, "s": s, "w_pre": w_pre, "dw_post": dw_post, "ds": ds, "dw_pre": dw_pre}, workspace)
+    _enter("la_block_norm_bwd", "ntttttttttttttttir", shape, x, y, u, w_post, s, w_pre, dh, dn, dx, dy, du, dw_post, ds, dw_pre,
+           workspace, _bytes(workspace), stream)
 
 
 def host_arena_bytes(shape: LaShape) -> int:

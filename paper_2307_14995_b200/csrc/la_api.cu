@@ -10,6 +10,7 @@
 #include <cstdlib>
 
 #include "../../include/la.h"
+#include "la_check.cuh"
 #include "la_common.cuh"
 
 namespace la {
@@ -91,8 +92,6 @@ struct Plan {
   Packed pk;        // start == NULL: dense batch
   Folded fold;      // batches == 0: none
 };
-
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 la_status check_shape(const la_shape* s, bool need_n) {
   if (!s) return LA_ERR_INVALID_ARG;
@@ -243,19 +242,6 @@ la_status make_table(const la_shape* s, const float* lambda_host, DecayTable* ta
   for (int h = s->H; h < LA_MAX_H; ++h) tab->s2[h] = 0.0;
   return LA_OK;
 }
-
-la_status check_device() {
-  int dev = 0, major = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess) return LA_ERR_CUDA;
-  if (cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev) != cudaSuccess)
-    return LA_ERR_CUDA;
-  return major == 10 ? LA_OK : LA_ERR_ARCH;
-}
-
-#define LA_TRY_CUDA(expr)                       \
-  do {                                          \
-    if ((expr) != cudaSuccess) return LA_ERR_CUDA; \
-  } while (0)
 
 // Writes first tokens, lengths and order of a packed batch (stream-ordered).
 la_status packed_upload(const Packed& pk, cudaStream_t cs) {

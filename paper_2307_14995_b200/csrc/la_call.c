@@ -6,6 +6,8 @@
 //   t  tensor        its address, NULL for None; refused with ValueError unless it is a contiguous CUDA tensor
 //   i  integer       its value
 //   s  shape         the address of a structure of the type given to bind
+//   d  delta shape   the same of the type for the gated delta rule
+//   n  norm shape    the same of the type for the norms between two blocks
 //   h  host memory   the address of a ctypes array, or the address itself
 //   r  stream        what the function given to bind makes of it, asked when the arguments before it have been accepted
 // A decode step spends longer in argument conversion than its kernel runs: through ctypes and Python-level checks a call costs
@@ -17,14 +19,15 @@
 #define MAX_ARGS 24
 
 static PyObject *s_is_cuda, *s_is_contiguous, *s_data_ptr, *stream_of;
-static PyTypeObject *shape_type, *ctypes_array;
+static PyTypeObject *shape_type, *delta_type, *norm_type, *ctypes_array;
 
 // 1: *out holds the slot; 0: an exception is set.
 static int slot(char kind, PyObject* a, uint64_t* out) {
-  if (kind == 's' || (kind == 'h' && !PyLong_Check(a))) {
-    PyTypeObject* const type = kind == 's' ? shape_type : ctypes_array;
+  if (kind == 's' || kind == 'd' || kind == 'n' || (kind == 'h' && !PyLong_Check(a))) {
+    PyTypeObject* const type = kind == 's' ? shape_type : kind == 'd' ? delta_type : kind == 'n' ? norm_type : ctypes_array;
     if (!type || !PyObject_TypeCheck(a, type)) {
-      PyErr_Format(PyExc_TypeError, "%s is expected, not %.100s", kind == 's' ? "a shape" : "a ctypes array", Py_TYPE(a)->tp_name);
+      PyErr_Format(PyExc_TypeError, "%s is expected, not %.100s",
+                   kind == 's' ? "a shape" : kind == 'd' ? "a delta shape" : kind == 'n' ? "a block norm shape" : "a ctypes array", Py_TYPE(a)->tp_name);
       return 0;
     }
     Py_buffer view;
@@ -103,16 +106,20 @@ static PyObject* call(PyObject* self, PyObject* const* args, Py_ssize_t n) {
 
 static PyObject* bind(PyObject* self, PyObject* args) {
   (void)self;
-  PyObject *type, *f;
-  if (!PyArg_ParseTuple(args, "O!O", &PyType_Type, &type, &f)) return NULL;
+  PyObject *type, *f, *delta, *norm;
+  if (!PyArg_ParseTuple(args, "O!OO!O!", &PyType_Type, &type, &f, &PyType_Type, &delta, &PyType_Type, &norm)) return NULL;
   Py_INCREF(type);
   Py_XSETREF(shape_type, (PyTypeObject*)type);
+  Py_INCREF(delta);
+  Py_XSETREF(delta_type, (PyTypeObject*)delta);
+  Py_INCREF(norm);
+  Py_XSETREF(norm_type, (PyTypeObject*)norm);
   Py_INCREF(f);
   Py_XSETREF(stream_of, f);
   Py_RETURN_NONE;
 }
 
-static PyMethodDef methods[] = {{"bind", bind, METH_VARARGS, "bind(type of a shape, function that gives a stream's handle)"},
+static PyMethodDef methods[] = {{"bind", bind, METH_VARARGS, "bind(type of a shape, function that gives a stream's handle, types of a delta shape and of a norm shape)"},
                                 {"call", (PyCFunction)(void (*)(void))call, METH_FASTCALL, "call(address, kinds, arg, ...) -> status"},
                                 {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_la_call", NULL, -1, methods, NULL, NULL, NULL, NULL};

@@ -1,0 +1,1520 @@
+// Tensor-core kernels of the gated delta rule (included by la_tc.cu, inside its anonymous namespace, after the helpers and the walk, whose
+// arithmetic on pairs they share).  bf16 inputs, D = 128 or 64, chunks of 128 tokens.  Formulas: la_delta.cuh, in this order:
+//
+//   prepare   per chunk, from its own tokens: That by its transpose U = That^T (upper triangular, lanes are rows of U),
+//             X = scale ((Q K^T) (.) D) diag(beta) That,   J^T = K^T diag(beta e^(G_end - G)) That  [d, tokens],
+//             M = J^T diag(e^G) K,   N = J^T V.   Then the chunk as a whole is the affine map
+//                 S' = e^G_end S - M S + N,     and its outputs are   O = scale diag(e^G) Q S + X (V - diag(e^G) K S),
+//   chain     the map over all chunks, one after the other, a thread block per slice of value columns: one product a chunk,
+//   output    O, per chunk.
+//   Backward:   E = e^G_end E' - M^T E' + (scale Q^T diag(e^G) dO - K^T diag(e^G) Z),   Z = X^T dO: the same chain, in reverse,
+//   adjoint   Z and that sum, per chunk,
+//   values    Y = That (V - diag(e^G) K S) and dR = Z + U diag(beta e^(G_end - G)) K E', per chunk,
+//   gradients the rest, per chunk.
+//
+// Why: what is sequential is one product of [D, D] and [D, columns] per 128 tokens, with the operand already in the layout that the tensor
+// cores read (records below), and everything else has a thread block per chunk.  A walk that formed V' from What S, then S' from
+// V', would be two dependent products with two conversions between them.
+//
+// As in the walk, operands formed on chip from fp32 values are two bf16 terms hi + lo = x to 2^-17, and products of two such
+// operands leave out lo x lo.  Sums are fp32, in an order that depends on the shape alone.
+//
+// Operands in shared memory and in the workspace are images: rows of 128 bytes (64 elements) in the 128-byte swizzle, panel after panel of
+// 64 columns, all panels of hi and then those of lo; one image serves K-major and MN-major.  They move by untiled bulk copies.
+//
+// Every kernel waits for its predecessor before it does anything (its tensor memory included), and every wait inside is bounded: X_WAIT
+// makes the outcome the same for all threads of the block, which then drain what is in flight, free tensor memory and return.
+
+// Workspace records of one chunk of one head, in bytes.
+template <int D>
+struct XRec {
+  static constexpr size_t STATE = (size_t)D * D * 4;  // an image of a state or a state in fp32
+  static constexpr size_t ALL = 0;                     // e^G_end
+  static constexpr size_t U = 256, X = U + 65536, M = X + 65536, N = M + STATE, S = N + STATE, FWD = S + STATE;
+  static constexpr size_t TOK = (size_t)128 * D * 4;  // an image or fp32 values of all tokens
+  static constexpr size_t Z = 0, DR = Z + TOK, Y = DR + TOK, B = Y + TOK, E = B + STATE, BWD = E + STATE;
+};
+
+struct XMaps {
+  CUtensorMap q, k, v, d_o;
+};
+
+__device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_u32(dst)), "l"(src),
+               "r"(bytes), "r"(smem_u32(bar))
+               : "memory");
+}
+__device__ __forceinline__ void bulk_store(void* dst, const void* src, uint32_t bytes) {
+  asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(dst), "r"(smem_u32(src)), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void bulk_store_done() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
+
+// Byte offset of columns 8 c .. 8 c + 7 of row r in an image whose panels have `rows` rows.
+__device__ __forceinline__ uint32_t image_at(int r, int c, int rows) { return (uint32_t)((c >> 3) * rows * 128 + r * 128 + (((c & 7) ^ (r & 7)) << 4)); }
+
+// Eight values as packed hi and lo terms.
+__device__ __forceinline__ void split8(const float* x, uint4& h, uint4& l) {
+  split2(f2_pack(x[0], x[1]), h.x, l.x);
+  split2(f2_pack(x[2], x[3]), h.y, l.y);
+  split2(f2_pack(x[4], x[5]), h.z, l.z);
+  split2(f2_pack(x[6], x[7]), h.w, l.w);
+}
+__device__ __forceinline__ float bf_lo(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float bf_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
+__device__ __forceinline__ void join8(const uint4& h, const uint4& l, float* x) {
+  x[0] = bf_lo(h.x) + bf_lo(l.x); x[1] = bf_hi(h.x) + bf_hi(l.x);
+  x[2] = bf_lo(h.y) + bf_lo(l.y); x[3] = bf_hi(h.y) + bf_hi(l.y);
+  x[4] = bf_lo(h.z) + bf_lo(l.z); x[5] = bf_hi(h.z) + bf_hi(l.z);
+  x[6] = bf_lo(h.w) + bf_lo(l.w); x[7] = bf_hi(h.w) + bf_hi(l.w);
+}
+// 32 accumulator columns of this thread's lane
+__device__ __forceinline__ void load_acc(uint32_t taddr, float (&x)[32]) {
+  tmem_ld_x32(taddr, *reinterpret_cast<uint32_t(*)[32]>(&x));
+  tmem_ld_wait();
+}
+__device__ __forceinline__ float (&half32(float (&x)[64], int i))[32] { return *reinterpret_cast<float(*)[32]>(&x[32 * i]); }
+// 32 values as an A operand: 16 columns of hi terms, 16 of lo terms
+__device__ __forceinline__ void store_operand(uint32_t hi, uint32_t lo, const float (&x)[32]) {
+  uint32_t h[16], l[16];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) split2(f2_pack(x[2 * i], x[2 * i + 1]), h[i], l[i]);
+  tmem_st_x16(hi, h);
+  tmem_st_x16(lo, l);
+}
+
+// Decay sums of a chunk in units of log2, as two fp32 terms each: their differences keep the accuracy of the small ones among large.
+struct alignas(16) XGates {
+  float2 sum[128];
+  float beta[128];
+  double part[4];
+};
+__device__ __forceinline__ float decay2(const float2& a, const float2& b) { return ex2_approx((a.x - b.x) + (a.y - b.y)); }
+__device__ __forceinline__ float2 two_terms(double x) {
+  const float h = (float)x;
+  return make_float2(h, (float)(x - (double)h));
+}
+// Threads 0 .. 127 (whole warps) sum up; every thread of the block calls, a barrier has to follow.  end: the whole chunk's sum.
+__device__ __forceinline__ void load_gates2(XGates& s, const DeltaArgs& a, long long gate, int n, int tid, float2& end) {
+  double x = 0.0;
+  if (tid < 128) {
+    if (tid < n) x = clamped_log_decay(a.g[gate + tid * a.gT]) * 1.4426950408889634;
+    s.beta[tid] = tid < n ? a.beta[gate + tid * a.gT] : 0.f;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const double y = __shfl_up_sync(0xffffffffu, x, o);
+      if ((tid & 31) >= o) x += y;
+    }
+    if ((tid & 31) == 31) s.part[tid >> 5] = x;
+  }
+  __syncthreads();
+  if (tid < 128) {
+    for (int w = 0; w < (tid >> 5); ++w) x += s.part[w];
+    s.sum[tid] = two_terms(x);
+  }
+  end = two_terms(((s.part[0] + s.part[1]) + s.part[2]) + s.part[3]);
+}
+
+struct XPlace {
+  int b, h, hk, n;
+  long long row, gate;
+  size_t rec;
+};
+__device__ __forceinline__ XPlace x_place(const DeltaArgs& a, int bh, int c) {
+  XPlace p;
+  p.b = bh / a.H;
+  p.h = bh % a.H;
+  p.hk = p.h / (a.H / a.Hk);
+  p.n = min(128, a.N - c * 128);
+  p.row = p.b * a.sB + p.h * a.sH + (long long)c * 128 * a.sT;
+  p.gate = p.b * a.gB + p.h * a.gH + (long long)c * 128 * a.gT;
+  p.rec = (size_t)bh * a.nchunk + c;
+  return p;
+}
+
+#define X_WAIT(bar, par, code)                                              \
+  do {                                                                      \
+    const bool ok_ = wait_or_abort(&(bar), (par), &sm.abort);               \
+    if (!ok_ && !sm.abort) atomicCAS(&g_tc_status, 0u, (unsigned)(code));   \
+    if (!ok_) sm.abort = 1;                                                 \
+    if (!__syncthreads_and(ok_)) return false;                              \
+    tc_fence_after_sync();                                                  \
+  } while (0)
+
+// Operands written to shared memory (or tensor memory) are handed to the tensor cores: fences and a barrier.
+#define X_HAND_OVER()            \
+  do {                           \
+    fence_proxy_async_smem();    \
+    tmem_st_wait();              \
+    tc_fence_before_sync();      \
+    __syncthreads();             \
+    tc_fence_after_sync();       \
+  } while (0)
+
+// Announces `bytes` of loads on barrier i (one thread).
+template <typename SM>
+__device__ __forceinline__ uint64_t* expect(SM& sm, int i, uint32_t bytes) {
+  ++sm.armed[i];
+  mbar_arrive_expect_tx(&sm.bars[i], bytes);
+  return &sm.bars[i];
+}
+
+// Start and end that all kernels below share.  body() returns false when a wait gave up.
+template <int COLS, typename SM, typename F>
+__device__ __forceinline__ void x_run(SM& sm, int nbars, F body) {
+  const int tid = threadIdx.x, warp = tid >> 5;
+  grid_dep_wait();
+  if (tid == 0) {
+    for (int i = 0; i < nbars; ++i) {
+      mbar_init(&sm.bars[i], 1);
+      sm.armed[i] = 0;
+    }
+    sm.abort = 0;
+    fence_mbar_init();
+  }
+  if (warp == 1) {
+    tmem_alloc(&sm.tmem_slot, COLS);
+    tmem_relinquish();
+  }
+  tc_fence_before_sync();
+  __syncthreads();
+  tc_fence_after_sync();
+  grid_dep_launch();
+  const uint32_t tmem = sm.tmem_slot;
+  const bool ok = body(tmem);
+  if (!ok) {  // products and copies that are still under way end before the block does
+    if (warp == 0) {
+      umma_commit_if(&sm.bars[nbars - 1], elect_one());
+      drain_wait(&sm.bars[nbars - 1], 0);
+    }
+    if (tid == 32)
+      for (int i = 0; i < nbars - 1; ++i)
+        if (sm.armed[i]) drain_wait(&sm.bars[i], (sm.armed[i] - 1) & 1);
+  }
+  if (tid == 0) bulk_store_done();
+  tc_fence_before_sync();
+  __syncthreads();
+  if (warp == 1) tmem_dealloc(tmem, COLS);
+}
+
+constexpr uint32_t XHI = UMMA_DESC_HI_SBO1024;
+__device__ __forceinline__ uint32_t kmaj(const void* p) { return umma_desc_lo(smem_u32(p), 16); }
+__device__ __forceinline__ uint32_t mnmaj(const void* p, uint32_t panel = 16384) { return umma_desc_lo(smem_u32(p), panel); }
+
+// ---- prepare ---------------------------------------------------------------------------------------------------------------------------
+// One thread block of 256 threads per chunk; 97 KB of shared memory and 256 columns of tensor memory, so that two share an SM and one's
+// products run beside the other's conversions.  Thread (q, lane) of half `half` has row q * 32 + lane of every accumulator and of every
+// image, columns half * 64 .. + 63.
+//
+// The inverse U of the upper triangular I + (n diag(beta))^T, in fp32 as far as the CUDA cores make it: columns of the four diagonal
+// blocks of 32 by back substitution (a warp each), then U12 = -U11 A12 U22 for the two blocks of 64, then the same once more on the
+// tensor cores for the whole.  Powers of the triangle would need no order of rows, but grow far beyond the inverse where keys are alike.
+enum { XP_LOAD = 0, XP_V, XP_MMA, XP_DRAIN, XP_BARS };
+template <int D>
+struct alignas(1024) XPrepSmem {
+  unsigned char k[32768];  // (D = 64: the keys twice)
+  unsigned char x[65536];  // q; blocks of A and U in fp32; image of U; v; image of M
+  XGates gates;
+  float until[128];        // beta e^(G_end - G)
+  float since[128];        // e^G
+  uint64_t bars[XP_BARS];
+  int armed[XP_BARS];
+  uint32_t tmem_slot;
+  int abort;
+};
+
+// element (i, m) of a 64 x 64 fp32 block whose 16-byte groups are permuted by row, so that a thread per row stores without conflicts
+__device__ __forceinline__ int block_at(int i, int m) { return i * 64 + ((((m >> 2) ^ i) & 15) << 2) + (m & 3); }
+
+template <int D>
+__global__ void __launch_bounds__(256, 2)
+x_prepare_kernel(const __grid_constant__ XMaps maps, const __grid_constant__ DeltaArgs a) {
+  extern __shared__ unsigned char smem_raw[];
+  using Rec = XRec<D>;
+  XPrepSmem<D>& sm = *reinterpret_cast<XPrepSmem<D>*>(smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u));
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, q = warp & 3, half = warp >> 2, row = q * 32 + lane;
+  x_run<256>(sm, XP_BARS, [&](const uint32_t tmem) -> bool {
+    const XPlace p = x_place(a, blockIdx.y, blockIdx.x);
+    unsigned char* const rec = static_cast<unsigned char*>(a.ws) + p.rec * Rec::FWD;
+    const uint32_t R = tmem, P = tmem + 128, mine = (uint32_t)(q * 32) << 16;
+    constexpr int PANELS = D / 64;
+    if (tid == 0) {
+      uint64_t* const bar = expect(sm, XP_LOAD, (2 + PANELS) * 16384);
+      for (int x = 0; x < 2; ++x) tma_load_4d(sm.k + x * 16384, &maps.k, bar, D == 128 ? x * 64 : 0, blockIdx.x * 128, p.hk, p.b);
+      for (int x = 0; x < PANELS; ++x) tma_load_4d(sm.x + x * 16384, &maps.q, bar, x * 64, blockIdx.x * 128, p.hk, p.b);
+    }
+    float2 end;
+    load_gates2(sm.gates, a, p.gate, p.n, tid, end);
+    if (tid < 128) {
+      const float2 s = sm.gates.sum[tid];
+      sm.since[tid] = ex2_approx(s.x + s.y);
+      sm.until[tid] = sm.gates.beta[tid] * decay2(end, s);
+      if (tid == 0) *reinterpret_cast<float*>(rec + Rec::ALL) = ex2_approx(end.x + end.y);
+    }
+    constexpr uint32_t ID_KK = umma_idesc_bf16(128, 128, false, false);
+    constexpr uint32_t ID_KN64 = umma_idesc_bf16(128, 64, false, true);
+    constexpr uint32_t ID_KN = umma_idesc_bf16(128, 128, false, true);
+    constexpr uint32_t ID_NK = umma_idesc_bf16(128, 128, true, false);
+    constexpr int NK = D / 16;
+    __syncwarp();
+    const uint32_t go = warp == 0 ? elect_one() : 0;
+    int par = 0;
+    X_WAIT(sm.bars[XP_LOAD], 0, 50);
+    if (warp == 0) {
+      umma_group_ss<NK, true, true>(R, kmaj(sm.k), kmaj(sm.k), XHI, ID_KK, 0, go);
+      umma_group_ss<NK, true, true>(P, kmaj(sm.x), kmaj(sm.k), XHI, ID_KK, 0, go);
+      umma_commit_if(&sm.bars[XP_MMA], go);
+    }
+    X_WAIT(sm.bars[XP_MMA], par, 51);
+    par ^= 1;
+
+    // A = (n diag(beta))^T: row j, columns i > j
+    float* const fa = reinterpret_cast<float*>(sm.x);           // two blocks on the diagonal
+    float* const fu = reinterpret_cast<float*>(sm.x + 32768);   // the same of U
+    const float2 own = sm.gates.sum[row];
+    if (half >= (q >> 1)) {
+      const float bt = sm.gates.beta[row];
+      float x[64];
+      load_acc(R + mine + half * 64, half32(x, 0));
+      load_acc(R + mine + half * 64 + 32, half32(x, 1));
+#pragma unroll
+      for (int c = 0; c < 64; ++c) {
+        const int i = half * 64 + c;
+        x[c] = i > row ? x[c] * decay2(sm.gates.sum[i], own) * bt : 0.f;
+      }
+      if (half == (q >> 1)) {
+#pragma unroll
+        for (int c = 0; c < 64; c += 4)
+          *reinterpret_cast<float4*>(fa + half * 4096 + block_at(row & 63, c)) = make_float4(x[c], x[c + 1], x[c + 2], x[c + 3]);
+      } else {  // A12, in place of its scores
+        store_operand(R + mine + 64, R + mine + 96, half32(x, 0));
+        store_operand(R + mine + 80, R + mine + 112, half32(x, 1));
+      }
+    }
+    // P = scale ((Q K^T) (.) D) diag(beta): row i, columns m <= i, an A operand in place of its scores
+    {
+      float x[64];
+      load_acc(P + mine + half * 64, half32(x, 0));
+      load_acc(P + mine + half * 64 + 32, half32(x, 1));
+      if (half <= (q >> 1)) {
+#pragma unroll
+        for (int c = 0; c < 64; ++c) {
+          const int m = half * 64 + c;
+          x[c] = m <= row ? x[c] * (decay2(own, sm.gates.sum[m]) * (a.scale * sm.gates.beta[m])) : 0.f;
+        }
+      } else {
+#pragma unroll
+        for (int c = 0; c < 64; ++c) x[c] = 0.f;
+      }
+      tc_fence_before_sync();
+      __syncthreads();  // (the other half's columns are read; and A is written)
+      tc_fence_after_sync();
+      store_operand(P + mine + half * 32, P + mine + 64 + half * 32, half32(x, 0));
+      store_operand(P + mine + half * 32 + 16, P + mine + 64 + half * 32 + 16, half32(x, 1));
+    }
+    if (warp < 4) {  // blocks of 32: column `lane` of the inverse, from the diagonal upwards
+      const float* const blk = fa + (warp >> 1) * 4096;
+      const int o = (warp & 1) * 32;
+      float x[32];
+#pragma unroll
+      for (int i = 31; i >= 0; --i) {
+        float v[4] = {i == lane ? 1.f : 0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int m4 = (i + 1) / 4 * 4; m4 < 32; m4 += 4) {
+          const float4 w = *reinterpret_cast<const float4*>(blk + block_at(o + i, o + m4));
+          if (m4 + 0 > i) v[0] = fmaf(-w.x, x[m4 + 0], v[0]);
+          if (m4 + 1 > i) v[1] = fmaf(-w.y, x[m4 + 1], v[1]);
+          if (m4 + 2 > i) v[2] = fmaf(-w.z, x[m4 + 2], v[2]);
+          if (m4 + 3 > i) v[3] = fmaf(-w.w, x[m4 + 3], v[3]);
+        }
+        x[i] = (v[0] + v[1]) + (v[2] + v[3]);
+        fu[(warp >> 1) * 4096 + block_at(o + i, o + lane)] = x[i];
+      }
+    }
+    __syncthreads();
+    {  // blocks of 64: the upper right quarter is -U11 (A12 U22); the lower left one holds what is in brackets
+      const float* const fab = fa + (tid >> 7) * 4096;
+      float* const fub = fu + (tid >> 7) * 4096;
+      const int r = (tid & 127) >> 2, c0 = (tid & 3) * 8;
+#pragma unroll
+      for (int step = 0; step < 2; ++step) {
+        float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll 2
+        for (int m = 0; m < 32; m += 4) {
+          const float4 w = *reinterpret_cast<const float4*>(step == 0 ? fab + block_at(r, 32 + m) : fub + block_at(r, m));
+          const float ww[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            const int at = step == 0 ? 32 : 0;
+            const float4 b0 = *reinterpret_cast<const float4*>(fub + block_at(32 + m + x, at + c0));
+            const float4 b1 = *reinterpret_cast<const float4*>(fub + block_at(32 + m + x, at + c0 + 4));
+            v[0] = fmaf(ww[x], b0.x, v[0]); v[1] = fmaf(ww[x], b0.y, v[1]); v[2] = fmaf(ww[x], b0.z, v[2]); v[3] = fmaf(ww[x], b0.w, v[3]);
+            v[4] = fmaf(ww[x], b1.x, v[4]); v[5] = fmaf(ww[x], b1.y, v[5]); v[6] = fmaf(ww[x], b1.z, v[6]); v[7] = fmaf(ww[x], b1.w, v[7]);
+          }
+        }
+        const float sign = step == 0 ? 1.f : -1.f;
+        float* const to = fub + (step == 0 ? block_at(32 + r, c0) : block_at(r, 32 + c0));
+        float* const to4 = fub + (step == 0 ? block_at(32 + r, c0 + 4) : block_at(r, 32 + c0 + 4));
+        *reinterpret_cast<float4*>(to) = make_float4(sign * v[0], sign * v[1], sign * v[2], sign * v[3]);
+        *reinterpret_cast<float4*>(to4) = make_float4(sign * v[4], sign * v[5], sign * v[6], sign * v[7]);
+        __syncthreads();
+      }
+    }
+    // row `row & 63` of a diagonal block of U, as it is now
+    auto block_row = [&](int blk, float (&x)[64]) {
+      const int r = row & 63;
+#pragma unroll
+      for (int c = 0; c < 64; c += 4) {
+        const float4 w = *reinterpret_cast<const float4*>(fu + blk * 4096 + block_at(r, c));
+        const bool in = c >= 32 || r < 32;
+        x[c] = in ? w.x : 0.f;
+        x[c + 1] = in ? w.y : 0.f;
+        x[c + 2] = in ? w.z : 0.f;
+        x[c + 3] = in ? w.w : 0.f;
+      }
+    };
+    // 64 x 64 operand in A's place: rows are those of the product's K
+    auto put_square = [&](const float (&x)[64]) {
+#pragma unroll
+      for (int c = 0; c < 8; ++c) {
+        uint4 h, l;
+        split8(&x[8 * c], h, l);
+        const uint32_t at = image_at(row & 63, c, 64);
+        *reinterpret_cast<uint4*>(sm.x + at) = h;
+        *reinterpret_cast<uint4*>(sm.x + 8192 + at) = l;
+      }
+    };
+    auto square_product = [&](uint32_t hi, uint32_t lo) {  // to columns 0 .. 63 of R
+      if (warp == 0) {
+        umma_group_tsd4<false>(R, hi, mnmaj(sm.x), XHI, ID_KN64, 0, go);
+        umma_group_tsd4<false>(R, hi, mnmaj(sm.x + 8192), XHI, ID_KN64, 1, go);
+        umma_group_tsd4<false>(R, lo, mnmaj(sm.x), XHI, ID_KN64, 1, go);
+        umma_commit_if(&sm.bars[XP_MMA], go);
+      }
+    };
+    if (q >= 2 && half == 1) {
+      float x[64];
+      block_row(1, x);
+      put_square(x);
+    }
+    X_HAND_OVER();
+    square_product(R + 64, R + 96);  // A12 U22 (lanes 64 .. 127: whatever)
+    X_WAIT(sm.bars[XP_MMA], par, 52);
+    par ^= 1;
+    if (q < 2) {
+      float x[64];
+      if (half == 0) {
+        load_acc(R + mine, half32(x, 0));
+        load_acc(R + mine + 32, half32(x, 1));
+        put_square(x);
+      } else {
+        block_row(0, x);
+        store_operand(R + mine + 64, R + mine + 96, half32(x, 0));
+        store_operand(R + mine + 80, R + mine + 112, half32(x, 1));
+      }
+    }
+    X_HAND_OVER();
+    square_product(R + 64, R + 96);  // U11 (A12 U22)
+    X_WAIT(sm.bars[XP_MMA], par, 53);
+    par ^= 1;
+    {  // the image of U
+      float x[64];
+      if (q < 2 && half == 1) {
+        load_acc(R + mine, half32(x, 0));
+        load_acc(R + mine + 32, half32(x, 1));
+#pragma unroll
+        for (int c = 0; c < 64; ++c) x[c] = -x[c];
+      } else if (q >= 2 && half == 0) {
+#pragma unroll
+        for (int c = 0; c < 64; ++c) x[c] = 0.f;
+      } else {
+        block_row(half, x);
+      }
+      __syncthreads();  // (every block has been read)
+#pragma unroll
+      for (int c = 0; c < 8; ++c) {
+        uint4 h, l;
+        split8(&x[8 * c], h, l);
+        const uint32_t at = image_at(row, half * 8 + c, 128);
+        *reinterpret_cast<uint4*>(sm.x + at) = h;
+        *reinterpret_cast<uint4*>(sm.x + 32768 + at) = l;
+      }
+    }
+    X_HAND_OVER();
+    if (tid == 0) {
+      bulk_store(rec + Rec::U, sm.x, 65536);
+      tma_store_commit();
+    }
+    if (warp == 0) {  // X = P That: That [m][j] is U [j][m]
+      umma_group_tsd<true>(R, P, kmaj(sm.x), XHI, ID_KK, 0, go);
+      umma_group_tsd<true>(R, P, kmaj(sm.x + 32768), XHI, ID_KK, 1, go);
+      umma_group_tsd<true>(R, P + 64, kmaj(sm.x), XHI, ID_KK, 1, go);
+      umma_commit_if(&sm.bars[XP_MMA], go);
+      if (tid == 0) tma_store_wait_read();
+      __syncwarp();
+    }
+    X_WAIT(sm.bars[XP_MMA], par, 54);
+    par ^= 1;
+    // X leaves as an image; U's columns take beta e^(G_end - G)
+#pragma unroll
+    for (int pc = 0; pc < 2; ++pc) {
+      float x[32];
+      load_acc(R + mine + half * 64 + pc * 32, x);
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        uint4 h, l;
+        split8(&x[8 * c], h, l);
+        const uint32_t at = image_at(row, half * 8 + pc * 4 + c, 128);
+        *reinterpret_cast<uint4*>(rec + Rec::X + at) = h;
+        *reinterpret_cast<uint4*>(rec + Rec::X + 32768 + at) = l;
+      }
+    }
+#pragma unroll
+    for (int c = 0; c < 8; ++c) {
+      const uint32_t at = image_at(row, half * 8 + c, 128);
+      uint4 h = *reinterpret_cast<const uint4*>(sm.x + at), l = *reinterpret_cast<const uint4*>(sm.x + 32768 + at);
+      float x[8];
+      join8(h, l, x);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] *= sm.until[half * 64 + 8 * c + i];
+      split8(x, h, l);
+      *reinterpret_cast<uint4*>(sm.x + at) = h;
+      *reinterpret_cast<uint4*>(sm.x + 32768 + at) = l;
+    }
+    X_HAND_OVER();
+    if (warp == 0) {  // J^T [d, j] = K^T U'^T
+      umma_group_ss<8, false, true>(R, mnmaj(sm.k), kmaj(sm.x), XHI, ID_NK, 0, go);
+      umma_group_ss<8, false, true>(R, mnmaj(sm.k), kmaj(sm.x + 32768), XHI, ID_NK, 1, go);
+      umma_commit_if(&sm.bars[XP_MMA], go);
+    }
+    X_WAIT(sm.bars[XP_MMA], par, 55);
+    par ^= 1;
+    if (tid == 0) {  // (D = 64: [V | K])
+      uint64_t* const bar = expect(sm, XP_V, 32768);
+      tma_load_4d(sm.x, &maps.v, bar, 0, blockIdx.x * 128, p.h, p.b);
+      if (D == 128) tma_load_4d(sm.x + 16384, &maps.v, bar, 64, blockIdx.x * 128, p.h, p.b);
+      else tma_load_4d(sm.x + 16384, &maps.k, bar, 0, blockIdx.x * 128, p.hk, p.b);
+    }
+    // J^T as an A operand; D = 64: lanes 64 .. 127 have it once more, for M, times e^G
+#pragma unroll
+    for (int pc = 0; pc < 2; ++pc) {
+      float x[32];
+      load_acc(R + mine + half * 64 + pc * 32, x);
+      if (D == 64 && q >= 2) {
+#pragma unroll
+        for (int c = 0; c < 32; ++c) x[c] *= sm.since[half * 64 + pc * 32 + c];
+      }
+      store_operand(P + mine + half * 32 + pc * 16, P + mine + 64 + half * 32 + pc * 16, x);
+    }
+    X_HAND_OVER();
+    X_WAIT(sm.bars[XP_V], 0, 56);
+    if (warp == 0) {  // N = J^T V
+      umma_group_tsd<false>(R, P, mnmaj(sm.x), XHI, ID_KN, 0, go);
+      umma_group_tsd<false>(R, P + 64, mnmaj(sm.x), XHI, ID_KN, 1, go);
+      umma_commit_if(&sm.bars[XP_MMA], go);
+    }
+    X_WAIT(sm.bars[XP_MMA], par, 57);
+    par ^= 1;
+    const bool has_n = D == 128 || (q < 2 && half == 0), has_m = D == 128 || (q >= 2 && half == 1);
+    if (has_n) {  // column by column: a warp stores 128 consecutive bytes
+      float* const to = reinterpret_cast<float*>(rec + Rec::N) + row;
+#pragma unroll
+      for (int pc = 0; pc < 2; ++pc) {
+        float x[32];
+        load_acc(R + mine + half * 64 + pc * 32, x);
+#pragma unroll
+        for (int c = 0; c < 32; ++c) to[(half * 64 + pc * 32 + c) * D] = x[c];
+      }
+    }
+    if (D == 128) {  // J^T diag(e^G), and M
+#pragma unroll
+      for (int pc = 0; pc < 2; ++pc) {
+        uint32_t h[16], l[16];
+        float x[32];
+        tmem_ld_x16(P + mine + half * 32 + pc * 16, h);
+        tmem_ld_x16(P + mine + 64 + half * 32 + pc * 16, l);
+        tmem_ld_wait();
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          x[2 * i] = (bf_lo(h[i]) + bf_lo(l[i])) * sm.since[half * 64 + pc * 32 + 2 * i];
+          x[2 * i + 1] = (bf_hi(h[i]) + bf_hi(l[i])) * sm.since[half * 64 + pc * 32 + 2 * i + 1];
+        }
+        store_operand(P + mine + half * 32 + pc * 16, P + mine + 64 + half * 32 + pc * 16, x);
+      }
+      X_HAND_OVER();
+      if (warp == 0) {
+        umma_group_tsd<false>(R, P, mnmaj(sm.k), XHI, ID_KN, 0, go);
+        umma_group_tsd<false>(R, P + 64, mnmaj(sm.k), XHI, ID_KN, 1, go);
+        umma_commit_if(&sm.bars[XP_MMA], go);
+      }
+      X_WAIT(sm.bars[XP_MMA], par, 58);
+    }
+    if (has_m) {
+#pragma unroll
+      for (int pc = 0; pc < 2; ++pc) {
+        float x[32];
+        load_acc(R + mine + half * 64 + pc * 32, x);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          uint4 h, l;
+          split8(&x[8 * c], h, l);
+          const uint32_t at = image_at(row & (D - 1), (half * 8 + pc * 4 + c) & (D / 8 - 1), D);
+          *reinterpret_cast<uint4*>(sm.x + at) = h;
+          *reinterpret_cast<uint4*>(sm.x + D * D * 2 + at) = l;
+        }
+      }
+    }
+    X_HAND_OVER();
+    if (tid == 0) {
+      bulk_store(rec + Rec::M, sm.x, D * D * 4);
+      tma_store_commit();
+    }
+    return true;
+  });
+}
+
+// ---- chain -----------------------------------------------------------------------------------------------------------------------------
+// S' = e^G_end S - M S + N over the chunks (REV: E = e^G_end E' - M^T E' + B from the last to the first), NE value columns of one head
+// per thread block, the state in registers in fp32; the state that enters each chunk (REV: the gradient of the one that leaves it) goes
+// to the workspace as an image.  A step is one product, a conversion and two barriers; the images of M come three steps ahead.
+// Both terms of the state are columns of one B operand, [hi | lo], so that hi of M meets both in one pass: with NE = 32 an
+// instruction takes as long as its A operand comes from shared memory (4 KB, 32 clocks), whatever its columns.
+// D = 64: both terms of M are rows of one A operand; the rows of lo pass through shared memory to the threads of those of hi.
+constexpr int XC_STAGES = 3;
+enum { XC_LOAD0 = 0, XC_MMA = XC_STAGES, XC_DRAIN, XC_BARS };
+template <int D, int NE>
+struct alignas(1024) XChainSmem {
+  unsigned char m[XC_STAGES][D * D * 4];
+  unsigned char b[2 * NE * D * 2];
+  float other[D == 64 ? 64 : 1][NE + 1];
+  uint64_t bars[XC_BARS];
+  int armed[XC_BARS];
+  uint32_t tmem_slot;
+  int abort;
+};
+struct XChainArgs {
+  const unsigned char* fwd;  // records with M and e^G_end
+  const unsigned char* add;  // N or B of chunk 0 of head 0
+  unsigned char* image;      // where the images of the states go
+  size_t fwd_stride, add_stride, image_stride;
+  const float* in;           // [BH, D, D] or NULL
+  float* out;
+  int nchunk;
+};
+
+template <int D, int NE, bool REV>
+__global__ void __launch_bounds__(256)
+x_chain_kernel(const __grid_constant__ XChainArgs a) {
+  extern __shared__ unsigned char smem_raw[];
+  using Rec = XRec<D>;
+  using Sm = XChainSmem<D, NE>;
+  Sm& sm = *reinterpret_cast<Sm*>(smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u));
+  constexpr int V = NE / 2;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, q = warp & 3, half = warp >> 2, row = q * 32 + lane;
+  constexpr uint32_t COLS = 2 * NE < 32 ? 32 : 2 * NE;
+  x_run<COLS>(sm, XC_BARS, [&](const uint32_t tmem) -> bool {
+    const int bh = blockIdx.y, e0 = blockIdx.x * NE;
+    const uint32_t mine = (uint32_t)(q * 32) << 16;
+    const bool owner = D == 128 || q < 2;
+    const int first = REV ? a.nchunk - 1 : 0, step = REV ? -1 : 1;
+    auto index = [&](int i) { return (size_t)bh * a.nchunk + (size_t)(first + step * i); };
+    auto load_m = [&](int i) {
+      const int s = i % XC_STAGES;
+      bulk_load(sm.m[s], a.fwd + index(i) * a.fwd_stride + Rec::M, D * D * 4, expect(sm, XC_LOAD0 + s, D * D * 4));
+    };
+    if (tid == 0)
+      for (int i = 0; i < XC_STAGES && i < a.nchunk; ++i) load_m(i);
+    __syncwarp();
+    const uint32_t go = warp == 0 ? elect_one() : 0;
+    constexpr uint32_t ID2 = umma_idesc_bf16(128, 2 * NE, REV, true), ID1 = umma_idesc_bf16(128, NE, REV, true);
+    float s[V], add[V], all = 0.f;
+    if (owner) {
+      const size_t at = ((size_t)bh * D + row) * D + e0 + half * V;
+#pragma unroll
+      for (int i = 0; i < V; i += 4) {
+        const float4 w = a.in ? ld_f4(reinterpret_cast<const float4*>(a.in + at + i)) : make_float4(0.f, 0.f, 0.f, 0.f);
+        s[i] = w.x; s[i + 1] = w.y; s[i + 2] = w.z; s[i + 3] = w.w;
+      }
+    }
+    auto fetch = [&](int i, float (&to)[V], float& f) {  // of step i
+      const float* const from = reinterpret_cast<const float*>(a.add + index(i) * a.add_stride) + (size_t)(e0 + half * V) * D + row;
+#pragma unroll
+      for (int x = 0; x < V; ++x) to[x] = ld_f1(from + x * D);
+      f = ld_f1(reinterpret_cast<const float*>(a.fwd + index(i) * a.fwd_stride + Rec::ALL));
+    };
+    if (owner) fetch(0, add, all);
+    int par = 0;
+    for (int i = 0; i < a.nchunk; ++i) {
+      if (owner) {
+        unsigned char* const image = a.image + index(i) * a.image_stride;
+#pragma unroll
+        for (int c = 0; c < V / 8; ++c) {
+          uint4 h, l;
+          split8(&s[8 * c], h, l);
+          const int col = half * (V / 8) + c;  // 16-byte group of the slice
+          *reinterpret_cast<uint4*>(sm.b + image_at(row, col, D)) = h;
+          *reinterpret_cast<uint4*>(sm.b + image_at(row, NE / 8 + col, D)) = l;
+          const uint32_t at = image_at(row, e0 / 8 + col, D);
+          *reinterpret_cast<uint4*>(image + at) = h;
+          *reinterpret_cast<uint4*>(image + D * D * 2 + at) = l;
+        }
+      }
+      X_HAND_OVER();
+      if (warp == 0) {
+        const int st = i % XC_STAGES;
+        const bool ok = wait_or_abort(&sm.bars[XC_LOAD0 + st], (i / XC_STAGES) & 1, &sm.abort);
+        if (__all_sync(0xffffffffu, ok)) {
+          tc_fence_after_sync();
+          const unsigned char* const m = sm.m[st];
+          const uint32_t b = mnmaj(sm.b, D * 128);
+          if (D == 128) {
+            umma_group_ss<8, !REV, false>(tmem, REV ? mnmaj(m) : kmaj(m), b, XHI, ID2, 0, go);
+            umma_group_ss<8, !REV, false>(tmem, REV ? mnmaj(m + 32768) : kmaj(m + 32768), b, XHI, ID1, 1, go);
+          } else {
+            umma_group_ss<4, !REV, false>(tmem, REV ? mnmaj(m, 8192) : kmaj(m), b, XHI, ID2, 0, go);
+          }
+          umma_commit_if(&sm.bars[XC_MMA], go);
+        } else {
+          if (!ok && !sm.abort) atomicCAS(&g_tc_status, 0u, 60u);
+          sm.abort = 1;
+        }
+      }
+      float next[V], next_all = 0.f;
+      if (owner && i + 1 < a.nchunk) fetch(i + 1, next, next_all);
+      X_WAIT(sm.bars[XC_MMA], par, 61);
+      par ^= 1;
+      if (tid == 0 && i + XC_STAGES < a.nchunk) load_m(i + XC_STAGES);
+      __syncwarp();
+      uint32_t d0[V], d1[V];
+      if (V == 16) {
+        tmem_ld_x16(tmem + mine + half * V, *reinterpret_cast<uint32_t(*)[16]>(d0));
+        tmem_ld_x16(tmem + mine + NE + half * V, *reinterpret_cast<uint32_t(*)[16]>(d1));
+      } else {
+        tmem_ld_x32(tmem + mine + half * V, *reinterpret_cast<uint32_t(*)[32]>(d0));
+        tmem_ld_x32(tmem + mine + NE + half * V, *reinterpret_cast<uint32_t(*)[32]>(d1));
+      }
+      tmem_ld_wait();
+      if constexpr (D == 64) {
+        if (!owner)
+#pragma unroll
+          for (int x = 0; x < V; ++x) sm.other[row - 64][half * V + x] = __uint_as_float(d0[x]);
+        __syncthreads();
+      }
+      if (owner) {
+#pragma unroll
+        for (int x = 0; x < V; ++x) {
+          float m = __uint_as_float(d0[x]) + __uint_as_float(d1[x]);
+          if constexpr (D == 64) m += sm.other[row][half * V + x];
+          s[x] = fmaf(all, s[x], add[x]) - m;
+          add[x] = next[x];
+        }
+        all = next_all;
+      }
+    }
+    if (owner && a.out) {
+      const size_t at = ((size_t)bh * D + row) * D + e0 + half * V;
+#pragma unroll
+      for (int x = 0; x < V; x += 4) *reinterpret_cast<float4*>(a.out + at + x) = make_float4(s[x], s[x + 1], s[x + 2], s[x + 3]);
+    }
+    return true;
+  });
+}
+
+// ---- output ----------------------------------------------------------------------------------------------------------------------------
+// O = scale diag(e^G) Q S + X (V - diag(e^G) K S): 64 value columns of a chunk per thread block, two thread blocks to an SM.  Both terms of
+// the state, and then of the bracket, are one B operand of 128 columns [hi | lo]; the halves of the results are added up on the way
+// out of tensor memory.
+enum { XO_LOAD = 0, XO_X, XO_MMA, XO_DRAIN, XO_BARS };
+template <int D>
+struct alignas(1024) XOutSmem {
+  unsigned char qk[65536];  // q, k; then X
+  unsigned char s[32768];   // [hi | lo] of the state's columns, then of the bracket
+  XGates gates;
+  uint64_t bars[XO_BARS];
+  int armed[XO_BARS];
+  uint32_t tmem_slot;
+  int abort;
+};
+
+// 32 values of row (D features of T apart) as fp32, or zeros
+__device__ __forceinline__ void load_row32(const __nv_bfloat16* p, bool in, float (&x)[32]) {
+#pragma unroll
+  for (int c = 0; c < 4; ++c) {
+    uint4 w = make_uint4(0u, 0u, 0u, 0u);
+    if (in) w = *reinterpret_cast<const uint4*>(p + 8 * c);
+    x[8 * c] = bf_lo(w.x); x[8 * c + 1] = bf_hi(w.x); x[8 * c + 2] = bf_lo(w.y); x[8 * c + 3] = bf_hi(w.y);
+    x[8 * c + 4] = bf_lo(w.z); x[8 * c + 5] = bf_hi(w.z); x[8 * c + 6] = bf_lo(w.w); x[8 * c + 7] = bf_hi(w.w);
+  }
+}
+template <typename T>
+__device__ __forceinline__ void store_row32(T* p, const float (&x)[32]) {
+  if constexpr (sizeof(T) == 2) {
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      uint32_t w[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const __nv_bfloat162 v = __floats2bfloat162_rn(x[8 * c + 2 * i], x[8 * c + 2 * i + 1]);
+        w[i] = *reinterpret_cast<const uint32_t*>(&v);
+      }
+      *reinterpret_cast<uint4*>(p + 8 * c) = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+  } else {
+#pragma unroll
+    for (int c = 0; c < 8; ++c) *reinterpret_cast<float4*>(p + 4 * c) = make_float4(x[4 * c], x[4 * c + 1], x[4 * c + 2], x[4 * c + 3]);
+  }
+}
+// The sum of the two halves [hi | lo], 64 columns each, of a product: columns c0 .. c0 + 31
+__device__ __forceinline__ void load_both(uint32_t taddr, float (&x)[32]) {
+  float y[32];
+  load_acc(taddr, x);
+  load_acc(taddr + 64, y);
+#pragma unroll
+  for (int i = 0; i < 32; ++i) x[i] += y[i];
+}
+
+template <int D, typename TO>
+__global__ void __launch_bounds__(256, 2)
+x_output_kernel(const __grid_constant__ XMaps maps, const __grid_constant__ DeltaArgs a) {
+  extern __shared__ unsigned char smem_raw[];
+  using Rec = XRec<D>;
+  XOutSmem<D>& sm = *reinterpret_cast<XOutSmem<D>*>(smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u));
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, q = warp & 3, half = warp >> 2, row = q * 32 + lane;
+  x_run<256>(sm, XO_BARS, [&](const uint32_t tmem) -> bool {
+    constexpr int PANELS = D / 64, NK = D / 16;
+    const int c = blockIdx.x / PANELS, eh = blockIdx.x % PANELS;
+    const XPlace p = x_place(a, blockIdx.y, c);
+    const unsigned char* const rec = static_cast<const unsigned char*>(a.ws) + p.rec * Rec::FWD;
+    const uint32_t mine = (uint32_t)(q * 32) << 16;
+    if (tid == 0) {
+      uint64_t* const bar = expect(sm, XO_LOAD, 2 * PANELS * 16384 + 2 * D * 128);
+      for (int x = 0; x < PANELS; ++x) tma_load_4d(sm.qk + x * 16384, &maps.q, bar, x * 64, c * 128, p.hk, p.b);
+      for (int x = 0; x < PANELS; ++x) tma_load_4d(sm.qk + 32768 + x * 16384, &maps.k, bar, x * 64, c * 128, p.hk, p.b);
+      bulk_load(sm.s, rec + Rec::S + eh * D * 128, D * 128, bar);
+      bulk_load(sm.s + D * 128, rec + Rec::S + D * D * 2 + eh * D * 128, D * 128, bar);
+    }
+    float v[32];
+    load_row32(static_cast<const __nv_bfloat16*>(a.v) + p.row + row * a.sT + eh * 64 + half * 32, row < p.n, v);
+    float2 end;
+    load_gates2(sm.gates, a, p.gate, p.n, tid, end);
+    __syncthreads();
+    const float since = ex2_approx(sm.gates.sum[row].x + sm.gates.sum[row].y);
+    __syncwarp();
+    const uint32_t go = warp == 0 ? elect_one() : 0;
+    constexpr uint32_t ID2 = umma_idesc_bf16(128, 128, false, true), ID1 = umma_idesc_bf16(128, 64, false, true);
+    X_WAIT(sm.bars[XO_LOAD], 0, 70);
+    if (warp == 0) {
+      umma_group_ss<NK, true, false>(tmem, kmaj(sm.qk + 32768), mnmaj(sm.s, D * 128), XHI, ID2, 0, go);
+      umma_group_ss<NK, true, false>(tmem + 128, kmaj(sm.qk), mnmaj(sm.s, D * 128), XHI, ID2, 0, go);
+      umma_commit_if(&sm.bars[XO_MMA], go);
+    }
+    X_WAIT(sm.bars[XO_MMA], 0, 71);
+    if (tid == 0) bulk_load(sm.qk, rec + Rec::X, 65536, expect(sm, XO_X, 65536));
+    {
+      float x[32];
+      load_both(tmem + mine + half * 32, x);
+#pragma unroll
+      for (int i = 0; i < 32; ++i) x[i] = fmaf(-since, x[i], v[i]);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        uint4 h, l;
+        split8(&x[8 * i], h, l);
+        const uint32_t at = image_at(row, half * 4 + i, 128);
+        *reinterpret_cast<uint4*>(sm.s + at) = h;
+        *reinterpret_cast<uint4*>(sm.s + 16384 + at) = l;
+      }
+    }
+    X_HAND_OVER();
+    X_WAIT(sm.bars[XO_X], 0, 72);
+    if (warp == 0) {
+      umma_group_ss<8, true, false>(tmem, kmaj(sm.qk), mnmaj(sm.s), XHI, ID2, 0, go);
+      umma_group_ss<8, true, false>(tmem, kmaj(sm.qk + 32768), mnmaj(sm.s), XHI, ID1, 1, go);
+      umma_commit_if(&sm.bars[XO_MMA], go);
+    }
+    load_both(tmem + 128 + mine + half * 32, v);
+#pragma unroll
+    for (int i = 0; i < 32; ++i) v[i] *= a.scale * since;
+    X_WAIT(sm.bars[XO_MMA], 1, 73);
+    float x[32];
+    load_both(tmem + mine + half * 32, x);
+#pragma unroll
+    for (int i = 0; i < 32; ++i) x[i] += v[i];
+    if (row < p.n) store_row32(static_cast<TO*>(a.o) + p.row + row * a.sT + eh * 64 + half * 32, x);
+    return true;
+  });
+}
+
+// ---- adjoint ---------------------------------------------------------------------------------------------------------------------------
+// Z = X^T dO, and B = scale Q^T diag(e^G) dO - K^T diag(e^G) Z for the chain in reverse: 64 value columns of a chunk per thread block.
+// D = 64: [Q | K] are the rows of one A operand and [dO' | Z'] the columns of one B operand, of whose product two quarters are wanted.
+enum { XA_LOAD = 0, XA_QK, XA_MMA, XA_DRAIN, XA_BARS };
+template <int D>
+struct alignas(1024) XAdjSmem {
+  unsigned char x[65536];   // X; then q, k (D = 64: and the lo terms of the B operand)
+  unsigned char t[32768];   // dO in the second half; the B operand [hi | lo] (D = 64: its hi terms)
+  XGates gates;
+  uint64_t bars[XA_BARS];
+  int armed[XA_BARS];
+  uint32_t tmem_slot;
+  int abort;
+};
+
+template <int D>
+__global__ void __launch_bounds__(256, 2)
+x_adjoint_kernel(const __grid_constant__ XMaps maps, const __grid_constant__ DeltaArgs a) {
+  extern __shared__ unsigned char smem_raw[];
+  using Rec = XRec<D>;
+  XAdjSmem<D>& sm = *reinterpret_cast<XAdjSmem<D>*>(smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u));
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, q = warp & 3, half = warp >> 2, row = q * 32 + lane;
+  x_run<256>(sm, XA_BARS, [&](const uint32_t tmem) -> bool {
+    constexpr int PANELS = D / 64;
+    const int c = blockIdx.x / PANELS, eh = blockIdx.x % PANELS;
+    const XPlace p = x_place(a, blockIdx.y, c);
+    const unsigned char* const fwd = static_cast<const unsigned char*>(a.ws) + p.rec * Rec::FWD;
+    unsigned char* const bwd = static_cast<unsigned char*>(a.ws_bwd) + p.rec * Rec::BWD;
+    const uint32_t mine = (uint32_t)(q * 32) << 16, R = tmem + 128;
+    if (tid == 0) {
+      uint64_t* const bar = expect(sm, XA_LOAD, 65536 + 16384);
+      bulk_load(sm.x, fwd + Rec::X, 65536, bar);
+      tma_load_4d(sm.t + 16384, &maps.d_o, bar, eh * 64, c * 128, p.h, p.b);
+    }
+    float2 end;
+    load_gates2(sm.gates, a, p.gate, p.n, tid, end);
+    __syncthreads();
+    const float since = ex2_approx(sm.gates.sum[row].x + sm.gates.sum[row].y);
+    __syncwarp();
+    const uint32_t go = warp == 0 ? elect_one() : 0;
+    constexpr uint32_t ID1 = umma_idesc_bf16(128, 64, true, true), ID2 = umma_idesc_bf16(128, 128, true, true);
+    X_WAIT(sm.bars[XA_LOAD], 0, 80);
+    if (warp == 0) {
+      umma_group_ss<8, false, false>(tmem, mnmaj(sm.x), mnmaj(sm.t + 16384), XHI, ID1, 0, go);
+      umma_group_ss<8, false, false>(tmem, mnmaj(sm.x + 32768), mnmaj(sm.t + 16384), XHI, ID1, 1, go);
+      umma_commit_if(&sm.bars[XA_MMA], go);
+    }
+    uint4 raw[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) raw[i] = *reinterpret_cast<const uint4*>(sm.t + 16384 + image_at(row, half * 4 + i, 128));
+    X_WAIT(sm.bars[XA_MMA], 0, 81);
+    if (tid == 0) {
+      uint64_t* const bar = expect(sm, XA_QK, 2 * PANELS * 16384);
+      for (int x = 0; x < PANELS; ++x) tma_load_4d(sm.x + x * 16384, &maps.q, bar, x * 64, c * 128, p.hk, p.b);
+      for (int x = 0; x < PANELS; ++x) tma_load_4d(sm.x + (PANELS + x) * 16384, &maps.k, bar, x * 64, c * 128, p.hk, p.b);
+    }
+    float z[32];
+    load_acc(tmem + mine + half * 32, z);
+    {
+      float* const to = reinterpret_cast<float*>(bwd + Rec::Z) + (size_t)(eh * 64 + half * 32) * 128 + row;
+#pragma unroll
+      for (int i = 0; i < 32; ++i) to[i * 128] = z[i];
+    }
+    unsigned char* const lo_terms = D == 128 ? sm.t + 16384 : sm.x + 32768;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t w[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
+      float x[8];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) x[2 * k] = bf_lo(w[k]) * (a.scale * since), x[2 * k + 1] = bf_hi(w[k]) * (a.scale * since);
+      uint4 h, l;
+      split8(x, h, l);
+      const uint32_t at = image_at(row, half * 4 + i, 128);
+      *reinterpret_cast<uint4*>(sm.t + at) = h;
+      *reinterpret_cast<uint4*>(lo_terms + at) = l;
+    }
+    auto put_z = [&](unsigned char* hi, unsigned char* lo) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        uint4 h, l;
+        float x[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) x[k] = -since * z[8 * i + k];
+        split8(x, h, l);
+        const uint32_t at = image_at(row, half * 4 + i, 128);
+        *reinterpret_cast<uint4*>(hi + at) = h;
+        *reinterpret_cast<uint4*>(lo + at) = l;
+      }
+    };
+    if (D == 64) put_z(sm.t + 16384, sm.x + 49152);
+    X_HAND_OVER();
+    X_WAIT(sm.bars[XA_QK], 0, 82);
+    if (warp == 0) {
+      umma_group_ss<8, false, false>(R, mnmaj(sm.x), mnmaj(sm.t), XHI, ID2, 0, go);
+      if (D == 64) umma_group_ss<8, false, false>(R, mnmaj(sm.x), mnmaj(sm.x + 32768), XHI, ID2, 1, go);
+      umma_commit_if(&sm.bars[XA_MMA], go);
+    }
+    X_WAIT(sm.bars[XA_MMA], 1, 83);
+    float* const to = reinterpret_cast<float*>(bwd + Rec::B) + (eh * 64 + half * 32) * D + (row & (D - 1));
+    float x[32];
+    if constexpr (D == 128) {
+      put_z(sm.t, sm.t + 16384);
+      X_HAND_OVER();
+      if (warp == 0) {
+        umma_group_ss<8, false, false>(R, mnmaj(sm.x + 32768), mnmaj(sm.t), XHI, ID2, 1, go);
+        umma_commit_if(&sm.bars[XA_MMA], go);
+      }
+      X_WAIT(sm.bars[XA_MMA], 0, 84);
+      load_both(R + mine + half * 32, x);
+#pragma unroll
+      for (int i = 0; i < 32; ++i) to[i * D] = x[i];
+    } else {
+      float(*const other)[65] = reinterpret_cast<float(*)[65]>(sm.t);
+      load_acc(R + mine + (q >= 2 ? 64 : 0) + half * 32, x);
+      if (q >= 2)
+#pragma unroll
+        for (int i = 0; i < 32; ++i) other[half * 32 + i][row - 64] = x[i];
+      __syncthreads();
+      if (q < 2)
+#pragma unroll
+        for (int i = 0; i < 32; ++i) to[i * D] = x[i] + other[half * 32 + i][row];
+    }
+    return true;
+  });
+}
+
+// ---- values ----------------------------------------------------------------------------------------------------------------------------
+// Y = That (V - diag(e^G) K S) (even thread blocks) and dR = Z + U diag(beta e^(G_end - G)) K E' (odd ones), as images; dR is dV.
+enum { XV_LOAD = 0, XV_U, XV_MMA, XV_DRAIN, XV_BARS };
+template <int D>
+struct alignas(1024) XValSmem {
+  unsigned char u[65536];  // k; then U
+  unsigned char s[32768];  // [hi | lo] of the state's columns, of the bracket, of the result
+  XGates gates;
+  uint64_t bars[XV_BARS];
+  int armed[XV_BARS];
+  uint32_t tmem_slot;
+  int abort;
+};
+
+template <int D, typename TO>
+__global__ void __launch_bounds__(256, 2)
+x_values_kernel(const __grid_constant__ XMaps maps, const __grid_constant__ DeltaArgs a) {
+  extern __shared__ unsigned char smem_raw[];
+  using Rec = XRec<D>;
+  XValSmem<D>& sm = *reinterpret_cast<XValSmem<D>*>(smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u));
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, q = warp & 3, half = warp >> 2, row = q * 32 + lane;
+  x_run<128>(sm, XV_BARS, [&](const uint32_t tmem) -> bool {
+    constexpr int PANELS = D / 64, NK = D / 16;
+    const bool grad = blockIdx.x & 1;
+    const int c = (blockIdx.x >> 1) / PANELS, eh = (blockIdx.x >> 1) % PANELS;
+    const XPlace p = x_place(a, blockIdx.y, c);
+    const unsigned char* const fwd = static_cast<const unsigned char*>(a.ws) + p.rec * Rec::FWD;
+    unsigned char* const bwd = static_cast<unsigned char*>(a.ws_bwd) + p.rec * Rec::BWD;
+    const uint32_t mine = (uint32_t)(q * 32) << 16;
+    if (tid == 0) {
+      uint64_t* const bar = expect(sm, XV_LOAD, PANELS * 16384 + 2 * D * 128);
+      for (int x = 0; x < PANELS; ++x) tma_load_4d(sm.u + x * 16384, &maps.k, bar, x * 64, c * 128, p.hk, p.b);
+      const unsigned char* const state = grad ? bwd + Rec::E : fwd + Rec::S;
+      bulk_load(sm.s, state + eh * D * 128, D * 128, bar);
+      bulk_load(sm.s + D * 128, state + D * D * 2 + eh * D * 128, D * 128, bar);
+    }
+    float add[32];
+    if (grad) {
+      const float* const z = reinterpret_cast<const float*>(bwd + Rec::Z) + (size_t)(eh * 64 + half * 32) * 128 + row;
+#pragma unroll
+      for (int i = 0; i < 32; ++i) add[i] = ld_f1(z + i * 128);
+    } else {
+      load_row32(static_cast<const __nv_bfloat16*>(a.v) + p.row + row * a.sT + eh * 64 + half * 32, row < p.n, add);
+    }
+    float2 end;
+    load_gates2(sm.gates, a, p.gate, p.n, tid, end);
+    __syncthreads();
+    const float2 own = sm.gates.sum[row];
+    const float times = grad ? sm.gates.beta[row] * decay2(end, own) : -ex2_approx(own.x + own.y);
+    __syncwarp();
+    const uint32_t go = warp == 0 ? elect_one() : 0;
+    constexpr uint32_t ID2 = umma_idesc_bf16(128, 128, false, true), ID1 = umma_idesc_bf16(128, 64, false, true);
+    constexpr uint32_t ID2T = umma_idesc_bf16(128, 128, true, true), ID1T = umma_idesc_bf16(128, 64, true, true);
+    X_WAIT(sm.bars[XV_LOAD], 0, 90);
+    if (warp == 0) {
+      umma_group_ss<NK, true, false>(tmem, kmaj(sm.u), mnmaj(sm.s, D * 128), XHI, ID2, 0, go);
+      umma_commit_if(&sm.bars[XV_MMA], go);
+    }
+    X_WAIT(sm.bars[XV_MMA], 0, 91);
+    if (tid == 0) bulk_load(sm.u, fwd + Rec::U, 65536, expect(sm, XV_U, 65536));
+    float x[32];
+    auto put = [&]() {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        uint4 h, l;
+        split8(&x[8 * i], h, l);
+        const uint32_t at = image_at(row, half * 4 + i, 128);
+        *reinterpret_cast<uint4*>(sm.s + at) = h;
+        *reinterpret_cast<uint4*>(sm.s + 16384 + at) = l;
+      }
+    };
+    load_both(tmem + mine + half * 32, x);
+#pragma unroll
+    for (int i = 0; i < 32; ++i) x[i] = grad ? times * x[i] : fmaf(times, x[i], add[i]);
+    put();
+    X_HAND_OVER();
+    X_WAIT(sm.bars[XV_U], 0, 92);
+    if (warp == 0) {
+      if (grad) {
+        umma_group_ss<8, true, false>(tmem, kmaj(sm.u), mnmaj(sm.s), XHI, ID2, 0, go);
+        umma_group_ss<8, true, false>(tmem, kmaj(sm.u + 32768), mnmaj(sm.s), XHI, ID1, 1, go);
+      } else {
+        umma_group_ss<8, false, false>(tmem, mnmaj(sm.u), mnmaj(sm.s), XHI, ID2T, 0, go);
+        umma_group_ss<8, false, false>(tmem, mnmaj(sm.u + 32768), mnmaj(sm.s), XHI, ID1T, 1, go);
+      }
+      umma_commit_if(&sm.bars[XV_MMA], go);
+    }
+    X_WAIT(sm.bars[XV_MMA], 1, 93);
+    load_both(tmem + mine + half * 32, x);
+    if (grad) {
+#pragma unroll
+      for (int i = 0; i < 32; ++i) x[i] += add[i];
+      if (row < p.n) store_row32(static_cast<TO*>(a.dv) + p.row + row * a.sT + eh * 64 + half * 32, x);
+    }
+    put();
+    X_HAND_OVER();
+    if (tid == 0) {
+      unsigned char* const to = bwd + (grad ? Rec::DR : Rec::Y) + eh * 16384;
+      bulk_store(to, sm.s, 16384);
+      bulk_store(to + PANELS * 16384, sm.s + 16384, 16384);
+      tma_store_commit();
+    }
+    return true;
+  });
+}
+
+// ---- gradients ---------------------------------------------------------------------------------------------------------------------------
+// dQ, dK, dg and dbeta of a chunk of a key head: one thread block of 512 threads, which takes the value heads of the group one after
+// the other.  Thread (q, lane) of quarter w has row q * 32 + lane, columns w * 32 .. + 31 of every accumulator.
+//   1  Q K^T, K K^T, dO Y^T, then dR Y^T                    scores: F and -H stay in registers as two terms; Z's sums (dg, dbeta)
+//   2  dO S^T, dR S^T, then Y E'^T                          what the state has of dQ and dK, scaled by rows; a_i, b_j
+//   3  dQ += F K,   dK += F^T Q - H^T K - H K               F and -H as images, one of each for both orientations
+// Sums over columns of a chunk's [128, 128] matrix go by butterflies over the lanes (16 values, 16 shuffles); sums over s run by scans.
+enum { XG_QK = 0, XG_Y, XG_DR, XG_SH, XG_SL, XG_E, XG_MMA, XG_DRAIN, XG_BARS };
+template <int D>
+struct alignas(1024) XGradSmem {
+  static constexpr int TOK = 128 * D * 2;  // 128 rows of bf16
+  unsigned char a[4 * TOK > 65536 ? 65536 : 65536];  // q, k; dR; q, k
+  unsigned char o[32768];                               // dO
+  unsigned char y[65536];                               // Y; F
+  unsigned char s[65536];                               // sums; S; E'; -H
+  float2 sum[128];
+  uint64_t bars[XG_BARS];
+  int armed[XG_BARS];
+  uint32_t tmem_slot;
+  int abort;
+};
+struct XSums {  // (in the second half of s)
+  float col[4][128], pre[4][128], rows[4][128], total[4][4], suffix[128];
+  float a[4][128], b[4][128], a_sum[128], b_sum[128], part[16];
+};
+
+// Over the 32 lanes, sums of each of 16 values per lane: lane l returns that of value l / 2.
+__device__ __forceinline__ float lane_sums16(const float (&v)[16], int lane) {
+  float t[8], r[4], u[2];
+#pragma unroll
+  for (int x = 0; x < 8; ++x) {
+    const bool up = (lane & 16) != 0;
+    t[x] = (up ? v[8 + x] : v[x]) + __shfl_xor_sync(0xffffffffu, up ? v[x] : v[8 + x], 16);
+  }
+#pragma unroll
+  for (int x = 0; x < 4; ++x) {
+    const bool up = (lane & 8) != 0;
+    r[x] = (up ? t[4 + x] : t[x]) + __shfl_xor_sync(0xffffffffu, up ? t[x] : t[4 + x], 8);
+  }
+#pragma unroll
+  for (int x = 0; x < 2; ++x) {
+    const bool up = (lane & 4) != 0;
+    u[x] = (up ? r[2 + x] : r[x]) + __shfl_xor_sync(0xffffffffu, up ? r[x] : r[2 + x], 4);
+  }
+  const bool up = (lane & 2) != 0;
+  const float w = (up ? u[1] : u[0]) + __shfl_xor_sync(0xffffffffu, up ? u[0] : u[1], 2);
+  return w + __shfl_xor_sync(0xffffffffu, w, 1);
+}
+// Sum over the lanes from this one on, or up to and without it
+__device__ __forceinline__ float suffix_sum(float x, int lane) {
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const float y = __shfl_down_sync(0xffffffffu, x, o);
+    if (lane + o < 32) x += y;
+  }
+  return x;
+}
+__device__ __forceinline__ float prefix_sum_before(float x, int lane) {
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const float y = __shfl_up_sync(0xffffffffu, x, o);
+    if (lane >= o) x += y;
+  }
+  const float y = __shfl_up_sync(0xffffffffu, x, 1);
+  return lane == 0 ? 0.f : y;
+}
+__device__ __forceinline__ void load_row16(const __nv_bfloat16* p, bool in, float (&x)[16]) {
+#pragma unroll
+  for (int c = 0; c < 2; ++c) {
+    uint4 w = make_uint4(0u, 0u, 0u, 0u);
+    if (in) w = *reinterpret_cast<const uint4*>(p + 8 * c);
+    x[8 * c] = bf_lo(w.x); x[8 * c + 1] = bf_hi(w.x); x[8 * c + 2] = bf_lo(w.y); x[8 * c + 3] = bf_hi(w.y);
+    x[8 * c + 4] = bf_lo(w.z); x[8 * c + 5] = bf_hi(w.z); x[8 * c + 6] = bf_lo(w.w); x[8 * c + 7] = bf_hi(w.w);
+  }
+}
+__device__ __forceinline__ void load_acc16(uint32_t taddr, float (&x)[16]) { tmem_ld_x16(taddr, *reinterpret_cast<uint32_t(*)[16]>(&x)); }
+
+template <int D, typename TO>
+__global__ void __launch_bounds__(512, 1)
+x_gradient_kernel(const __grid_constant__ XMaps maps, const __grid_constant__ DeltaArgs a) {
+  extern __shared__ unsigned char smem_raw[];
+  using Rec = XRec<D>;
+  XGradSmem<D>& sm = *reinterpret_cast<XGradSmem<D>*>(smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u));
+  XSums& sums = *reinterpret_cast<XSums*>(sm.s + 32768);
+  static_assert(sizeof(XSums) <= 32768, "sums");
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, q = warp & 3, w4 = warp >> 2, row = q * 32 + lane, c0 = w4 * 32;
+  x_run<512>(sm, XG_BARS, [&](const uint32_t tmem) -> bool {
+    constexpr int PANELS = D / 64, NK = D / 16, TOK = 128 * D * 2;  // bytes of 128 rows of bf16, and half of their image
+    constexpr uint32_t ID_SC = umma_idesc_bf16(128, 128, false, false), ID_ST = umma_idesc_bf16(128, D, false, false);
+    constexpr uint32_t ID_N = umma_idesc_bf16(128, D, false, true), ID_T = umma_idesc_bf16(128, D, true, true);
+    const int c = blockIdx.x, b = blockIdx.y / a.Hk, hk = blockIdx.y % a.Hk, G = a.H / a.Hk;
+    const uint32_t mine = (uint32_t)(q * 32) << 16, T0 = tmem, T1 = tmem + 128, T2 = tmem + 256, T3 = tmem + 384;
+    const long long krow = b * a.sBk + hk * a.sHk + (long long)(c * 128 + row) * a.sTk + c0;
+    __syncwarp();
+    const uint32_t go = warp == 0 ? elect_one() : 0;
+    const bool feat = c0 < D;  // has columns of features
+    int mma = 0, second = 0;   // parities
+    unsigned char* const first = static_cast<unsigned char*>(a.ws_bwd) + ((size_t)(b * a.H + hk * G) * a.nchunk + c) * Rec::BWD;
+    auto load_qk = [&]() {
+      uint64_t* const bar = expect(sm, XG_QK, 2 * TOK);
+      for (int x = 0; x < PANELS; ++x) tma_load_4d(sm.a + x * 16384, &maps.q, bar, x * 64, c * 128, hk, b);
+      for (int x = 0; x < PANELS; ++x) tma_load_4d(sm.a + TOK + x * 16384, &maps.k, bar, x * 64, c * 128, hk, b);
+    };
+    for (int gh = 0; gh < G; ++gh, second ^= 1) {
+      const XPlace p = x_place(a, b * a.H + hk * G + gh, c);
+      const unsigned char* const fwd = static_cast<const unsigned char*>(a.ws) + p.rec * Rec::FWD;
+      const unsigned char* const bwd = static_cast<const unsigned char*>(a.ws_bwd) + p.rec * Rec::BWD;
+      if (tid == 0) {
+        load_qk();
+        uint64_t* const bar = expect(sm, XG_Y, 3 * TOK);
+        for (int x = 0; x < PANELS; ++x) tma_load_4d(sm.o + x * 16384, &maps.d_o, bar, x * 64, c * 128, p.h, p.b);
+        bulk_load(sm.y, bwd + Rec::Y, 2 * TOK, bar);
+      }
+      // gates: the sums stay in shared memory, the rest in registers
+      float2 end;
+      XGates& gates = *reinterpret_cast<XGates*>(sm.s);
+      load_gates2(gates, a, p.gate, p.n, tid, end);
+      __syncthreads();
+      const float2 own = gates.sum[row];
+      const float beta_row = gates.beta[row], since = ex2_approx(own.x + own.y), until = decay2(end, own), all = ex2_approx(end.x + end.y);
+      if (tid < 128) sm.sum[tid] = gates.sum[tid];
+      float beta_tid = tid < 128 ? gates.beta[tid] : 0.f;
+      X_WAIT(sm.bars[XG_QK], 0, 100);
+      X_WAIT(sm.bars[XG_Y], second, 101);
+      if (warp == 0) {
+        umma_group_ss<NK, true, true>(T0, kmaj(sm.a), kmaj(sm.a + TOK), XHI, ID_SC, 0, go);
+        umma_group_ss<NK, true, true>(T1, kmaj(sm.a + TOK), kmaj(sm.a + TOK), XHI, ID_SC, 0, go);
+        umma_group_ss<NK, true, true>(T2, kmaj(sm.o), kmaj(sm.y), XHI, ID_SC, 0, go);
+        umma_group_ss<NK, true, true>(T2, kmaj(sm.o), kmaj(sm.y + TOK), XHI, ID_SC, 1, go);
+        umma_commit_if(&sm.bars[XG_MMA], go);
+      }
+      X_WAIT(sm.bars[XG_MMA], mma, 102);
+      mma ^= 1;
+      if (tid == 0) {
+        bulk_load(sm.a, bwd + Rec::DR, 2 * TOK, expect(sm, XG_DR, 2 * TOK));
+      }
+      X_WAIT(sm.bars[XG_DR], second, 103);
+      if (warp == 0) {
+        umma_group_ss<NK, true, true>(T3, kmaj(sm.a), kmaj(sm.y), XHI, ID_SC, 0, go);
+        umma_group_ss<NK, true, true>(T3, kmaj(sm.a), kmaj(sm.y + TOK), XHI, ID_SC, 1, go);
+        umma_group_ss<NK, true, true>(T3, kmaj(sm.a + TOK), kmaj(sm.y), XHI, ID_SC, 1, go);
+        umma_commit_if(&sm.bars[XG_MMA], go);
+      }
+      // beta of this thread's columns is read from the gates before the state comes over them
+      float bcol = gates.beta[c0 + lane];
+      X_WAIT(sm.bars[XG_MMA], mma, 104);
+      mma ^= 1;
+      if (tid == 0) bulk_load(sm.s, fwd + Rec::S, D * D * 2, expect(sm, XG_SH, D * D * 2));
+
+      // ---- scores ----
+      uint32_t fh[16], fl[16], nh[16], nl[16];
+      float before = 0.f;  // Z's sum over this thread's columns so far
+#pragma unroll
+      for (int pc = 0; pc < 2; ++pc) {
+        float qk[16], kk[16], f[16], h[16];
+        load_acc16(T0 + mine + c0 + pc * 16, qk);
+        load_acc16(T1 + mine + c0 + pc * 16, kk);
+        load_acc16(T2 + mine + c0 + pc * 16, f);
+        load_acc16(T3 + mine + c0 + pc * 16, h);
+        tmem_ld_wait();
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int j = c0 + pc * 16 + i;
+          const float bj = __shfl_sync(0xffffffffu, bcol, pc * 16 + i);
+          const float dec = j <= row ? decay2(own, sm.sum[j]) : 0.f;
+          f[i] = j <= row ? a.scale * dec * f[i] : 0.f;
+          h[i] = j < row ? dec * h[i] : 0.f;
+          qk[i] = f[i] * qk[i] - h[i] * kk[i];   // Z without beta_j
+          kk[i] = row >= j ? before : 0.f;       // of the columns before j
+          before = fmaf(bj, qk[i], before);
+          f[i] *= bj;
+          h[i] *= -bj;
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          split2(f2_pack(f[2 * i], f[2 * i + 1]), fh[pc * 8 + i], fl[pc * 8 + i]);
+          split2(f2_pack(h[2 * i], h[2 * i + 1]), nh[pc * 8 + i], nl[pc * 8 + i]);
+        }
+        const float col = lane_sums16(qk, lane), pre = lane_sums16(kk, lane);
+        if ((lane & 1) == 0) {
+          sums.col[q][c0 + pc * 16 + (lane >> 1)] = col;
+          sums.pre[q][c0 + pc * 16 + (lane >> 1)] = pre;
+        }
+      }
+      sums.rows[w4][row] = before;
+      __syncthreads();
+      {
+        float off = 0.f;
+        for (int w = 0; w < w4; ++w) off += sums.rows[w][row];
+        const float x = suffix_sum(off, lane);
+        if (lane == 0) sums.total[w4][q] = x;
+        if (q == w4) sums.suffix[row] = x;
+      }
+      __syncthreads();
+      float dbeta = 0.f, dg = 0.f;
+      if (tid < 128) {  // token tid, in the quarter tid / 32
+        dg = sums.suffix[tid];
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          dbeta += sums.col[x][tid];
+          dg += sums.pre[x][tid];
+          if (x > (tid >> 5)) dg += sums.total[tid >> 5][x];
+        }
+      }
+      tc_fence_before_sync();
+      __syncthreads();
+      tc_fence_after_sync();
+      // ---- what the states have ----
+      if (tid == 0) bulk_load(sm.s + D * D * 2, fwd + Rec::S + D * D * 2, D * D * 2, expect(sm, XG_SL, D * D * 2));
+      X_WAIT(sm.bars[XG_SH], second, 105);
+      X_WAIT(sm.bars[XG_SL], second, 106);
+      if (warp == 0) {
+        umma_group_ss<NK, true, true>(T0, kmaj(sm.o), kmaj(sm.s), XHI, ID_ST, 0, go);
+        umma_group_ss<NK, true, true>(T0, kmaj(sm.o), kmaj(sm.s + D * D * 2), XHI, ID_ST, 1, go);
+        umma_group_ss<NK, true, true>(T1, kmaj(sm.a), kmaj(sm.s), XHI, ID_ST, 0, go);
+        umma_group_ss<NK, true, true>(T1, kmaj(sm.a), kmaj(sm.s + D * D * 2), XHI, ID_ST, 1, go);
+        umma_group_ss<NK, true, true>(T1, kmaj(sm.a + TOK), kmaj(sm.s), XHI, ID_ST, 1, go);
+        umma_commit_if(&sm.bars[XG_MMA], go);
+      }
+      // <S, E'> meanwhile, from the images
+      float whole = 0.f;
+      for (int i = tid; i < D * D / 8; i += 512) {
+        const uint4* const s = reinterpret_cast<const uint4*>(fwd + Rec::S) + i;
+        const uint4* const e = reinterpret_cast<const uint4*>(bwd + Rec::E) + i;
+        float x[8], y[8];
+        join8(s[0], s[D * D / 8], x);
+        join8(e[0], e[D * D / 8], y);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) whole = fmaf(x[k], y[k], whole);
+      }
+      whole *= all;
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) whole += __shfl_xor_sync(0xffffffffu, whole, o);
+      X_WAIT(sm.bars[XG_MMA], mma, 107);
+      mma ^= 1;
+      if (tid == 0) bulk_load(sm.s, bwd + Rec::E, D * D * 4, expect(sm, XG_E, D * D * 4));
+      float dot_a = 0.f, dot_b = 0.f;
+      if (feat)
+#pragma unroll
+        for (int pc = 0; pc < 2; ++pc) {
+          float x[16], w[16];
+          load_acc16(T0 + mine + c0 + pc * 16, x);
+          load_row16(static_cast<const __nv_bfloat16*>(a.q) + krow + pc * 16, row < p.n, w);
+          tmem_ld_wait();
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            x[i] *= a.scale * since;
+            dot_a = fmaf(x[i], w[i], dot_a);
+          }
+          tmem_st_x16(T0 + mine + c0 + pc * 16, *reinterpret_cast<uint32_t(*)[16]>(&x));
+          load_acc16(T1 + mine + c0 + pc * 16, x);
+          load_row16(static_cast<const __nv_bfloat16*>(a.k) + krow + pc * 16, row < p.n, w);
+          tmem_ld_wait();
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            x[i] *= -since;
+            dot_a = fmaf(x[i], w[i], dot_a);
+          }
+          tmem_st_x16(T1 + mine + c0 + pc * 16, *reinterpret_cast<uint32_t(*)[16]>(&x));
+        }
+      X_WAIT(sm.bars[XG_E], second, 108);
+      if (warp == 0) {
+        umma_group_ss<NK, true, true>(T2, kmaj(sm.y), kmaj(sm.s), XHI, ID_ST, 0, go);
+        umma_group_ss<NK, true, true>(T2, kmaj(sm.y), kmaj(sm.s + D * D * 2), XHI, ID_ST, 1, go);
+        umma_group_ss<NK, true, true>(T2, kmaj(sm.y + TOK), kmaj(sm.s), XHI, ID_ST, 1, go);
+        umma_commit_if(&sm.bars[XG_MMA], go);
+      }
+      X_WAIT(sm.bars[XG_MMA], mma, 109);
+      mma ^= 1;
+      if (tid == 0) load_qk();
+      if (feat)
+#pragma unroll
+        for (int pc = 0; pc < 2; ++pc) {
+          float x[16], w[16];
+          load_acc16(T2 + mine + c0 + pc * 16, x);
+          load_row16(static_cast<const __nv_bfloat16*>(a.k) + krow + pc * 16, row < p.n, w);
+          tmem_ld_wait();
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            x[i] *= until;
+            dot_b = fmaf(x[i], w[i], dot_b);
+          }
+          load_acc16(T1 + mine + c0 + pc * 16, w);
+          tmem_ld_wait();
+#pragma unroll
+          for (int i = 0; i < 16; ++i) w[i] = fmaf(beta_row, x[i], w[i]);
+          tmem_st_x16(T1 + mine + c0 + pc * 16, *reinterpret_cast<uint32_t(*)[16]>(&w));
+        }
+      // (Y and E' are read) F and -H as images
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t at = image_at(row, w4 * 4 + i, 128);
+        *reinterpret_cast<uint4*>(sm.y + at) = make_uint4(fh[4 * i], fh[4 * i + 1], fh[4 * i + 2], fh[4 * i + 3]);
+        *reinterpret_cast<uint4*>(sm.y + 32768 + at) = make_uint4(fl[4 * i], fl[4 * i + 1], fl[4 * i + 2], fl[4 * i + 3]);
+        *reinterpret_cast<uint4*>(sm.s + at) = make_uint4(nh[4 * i], nh[4 * i + 1], nh[4 * i + 2], nh[4 * i + 3]);
+        *reinterpret_cast<uint4*>(sm.s + 32768 + at) = make_uint4(nl[4 * i], nl[4 * i + 1], nl[4 * i + 2], nl[4 * i + 3]);
+      }
+      X_HAND_OVER();
+      X_WAIT(sm.bars[XG_QK], 1, 110);
+      if (warp == 0) {
+        const unsigned char *const qt = sm.a, *const kt = sm.a + TOK;
+#pragma unroll
+        for (int term = 0; term < 2; ++term) {
+          umma_group_ss<8, true, false>(T0, kmaj(sm.y + term * 32768), mnmaj(kt), XHI, ID_N, 1, go);
+          umma_group_ss<8, false, false>(T1, mnmaj(sm.y + term * 32768), mnmaj(qt), XHI, ID_T, 1, go);
+          umma_group_ss<8, false, false>(T1, mnmaj(sm.s + term * 32768), mnmaj(kt), XHI, ID_T, 1, go);
+          umma_group_ss<8, true, false>(T1, kmaj(sm.s + term * 32768), mnmaj(kt), XHI, ID_N, 1, go);
+        }
+        umma_commit_if(&sm.bars[XG_MMA], go);
+      }
+      // ---- dg, dbeta: in dO's place, which nothing reads any more ----
+      XSums& more = *reinterpret_cast<XSums*>(sm.o);
+      more.a[w4][row] = dot_a;
+      more.b[w4][row] = dot_b;
+      if (lane == 0) more.part[warp] = whole;
+      __syncthreads();
+      float ai = 0.f, bi = 0.f;
+      if (tid < 128) {
+        ai = (more.a[0][tid] + more.a[1][tid]) + (more.a[2][tid] + more.a[3][tid]);
+        bi = (more.b[0][tid] + more.b[1][tid]) + (more.b[2][tid] + more.b[3][tid]);
+        dbeta += bi;
+        bi *= beta_tid;
+        const float x = suffix_sum(ai, lane), y = prefix_sum_before(bi, lane);
+        if (lane == 0) more.a_sum[warp] = x;
+        if (lane == 31) more.b_sum[warp] = y + bi;
+        ai = x;
+        bi = y;
+      }
+      __syncthreads();
+      if (tid < p.n) {
+        float w = 0.f;
+        for (int i = 0; i < 16; ++i) w += more.part[i];
+        for (int i = 0; i < 4; ++i) {
+          if (i > warp) ai += more.a_sum[i];
+          if (i < warp) bi += more.b_sum[i];
+        }
+        a.dg[p.gate + tid * a.gT] = w + ((dg + ai) + bi);
+        a.dbeta[p.gate + tid * a.gT] = dbeta;
+      }
+      X_WAIT(sm.bars[XG_MMA], mma, 111);
+      mma ^= 1;
+      // ---- dQ, dK; of a group of heads the sum so far is kept where Y and dR of its first head were ----
+      if (feat)
+#pragma unroll
+        for (int which = 0; which < 2; ++which) {
+          float x[32];
+          load_acc((which ? T1 : T0) + mine + c0, x);
+          float* const kept = reinterpret_cast<float*>(first + (which ? Rec::Y : Rec::DR)) + (size_t)c0 * 128 + row;
+          if (gh > 0)
+#pragma unroll
+            for (int i = 0; i < 32; ++i) x[i] += kept[i * 128];
+          if (gh + 1 < G) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) kept[i * 128] = x[i];
+          } else if (row < p.n) {
+            store_row32(static_cast<TO*>(which ? a.dk : a.dq) + krow, x);
+          }
+        }
+      tc_fence_before_sync();
+      __syncthreads();
+      tc_fence_after_sync();
+    }
+    return true;
+  });
+}
+
+// ---- launches ----------------------------------------------------------------------------------------------------------------------------
+bool make_token_map(CUtensorMap* m, const void* ptr, const DeltaArgs& a, bool shared) {
+  EncodeTiledFn enc = encode_fn();
+  if (!enc) return false;
+  cuuint64_t dims[4] = {(cuuint64_t)a.D, (cuuint64_t)a.N, (cuuint64_t)(shared ? a.Hk : a.H), (cuuint64_t)a.B};
+  cuuint64_t strides[3] = {(cuuint64_t)(shared ? a.sTk : a.sT) * 2, (cuuint64_t)(shared ? a.sHk : a.sH) * 2, (cuuint64_t)(shared ? a.sBk : a.sB) * 2};
+  cuuint32_t box[4] = {64, 128, 1, 1}, es[4] = {1, 1, 1, 1};
+  return enc(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(ptr), dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
+             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <typename SM, typename K, typename... A>
+cudaError_t x_launch(K kern, int kind, dim3 grid, int threads, cudaStream_t stream, const A&... args) {
+  constexpr size_t smem = sizeof(SM) + 1024;
+  static_assert(smem <= 232448, "shared memory of a thread block");
+  cudaError_t err = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  if (err != cudaSuccess) return err;
+  KernelTimer timer(kind, stream);
+  err = launch_early(kern, grid, dim3((unsigned)threads), smem, stream, 1, args...);
+  count_launch();
+  return err != cudaSuccess ? err : cudaGetLastError();
+}
+
+// Thread blocks with 32 value columns each as long as they all run at once (one to an SM), else with 64.
+template <int D, bool REV>
+cudaError_t x_chain(const DeltaArgs& d, cudaStream_t stream) {
+  using Rec = XRec<D>;
+  XChainArgs a{};
+  a.fwd = static_cast<const unsigned char*>(d.ws);
+  a.fwd_stride = Rec::FWD;
+  unsigned char* const bwd = static_cast<unsigned char*>(d.ws_bwd);
+  a.add = REV ? bwd + Rec::B : a.fwd + Rec::N;
+  a.image = REV ? bwd + Rec::E : static_cast<unsigned char*>(d.ws) + Rec::S;
+  a.add_stride = a.image_stride = REV ? Rec::BWD : Rec::FWD;
+  a.in = REV ? d.grad_kv_out : d.kv_in;
+  a.out = REV ? d.grad_kv_in : d.kv_out;
+  a.nchunk = d.nchunk;
+  const int heads = d.B * d.H;
+  if (heads * (D / 32) <= 148)
+    return x_launch<XChainSmem<D, 32>>(x_chain_kernel<D, 32, REV>, K_SCAN, dim3(D / 32, heads), 256, stream, a);
+  return x_launch<XChainSmem<D, 64>>(x_chain_kernel<D, 64, REV>, K_SCAN, dim3(D / 64, heads), 256, stream, a);
+}
+
+template <int D>
+cudaError_t x_states(const XMaps& m, const DeltaArgs& a, cudaStream_t stream) {
+  const cudaError_t err = x_launch<XPrepSmem<D>>(x_prepare_kernel<D>, K_PREPASS, dim3(a.nchunk, a.B * a.H), 256, stream, m, a);
+  return err != cudaSuccess ? err : x_chain<D, false>(a, stream);
+}
+
+template <int D, typename TO>
+cudaError_t x_fwd(const DeltaArgs& a, cudaStream_t stream) {
+  XMaps m{};
+  if (!make_token_map(&m.q, a.q, a, true) || !make_token_map(&m.k, a.k, a, true) || !make_token_map(&m.v, a.v, a, false)) return cudaErrorInvalidValue;
+  m.d_o = m.v;
+  const cudaError_t err = x_states<D>(m, a, stream);
+  if (err != cudaSuccess) return err;
+  return x_launch<XOutSmem<D>>(x_output_kernel<D, TO>, K_WALK, dim3(a.nchunk * (D / 64), a.B * a.H), 256, stream, m, a);
+}
+
+template <int D, typename TO>
+cudaError_t x_bwd(const DeltaArgs& a, bool have_fwd, cudaStream_t stream) {
+  XMaps m{};
+  if (!make_token_map(&m.q, a.q, a, true) || !make_token_map(&m.k, a.k, a, true) || !make_token_map(&m.v, a.v, a, false) ||
+      !make_token_map(&m.d_o, a.d_o, a, false))
+    return cudaErrorInvalidValue;
+  cudaError_t err = have_fwd ? cudaSuccess : x_states<D>(m, a, stream);
+  if (err == cudaSuccess)
+    err = x_launch<XAdjSmem<D>>(x_adjoint_kernel<D>, K_PREPASS, dim3(a.nchunk * (D / 64), a.B * a.H), 256, stream, m, a);
+  if (err == cudaSuccess) err = x_chain<D, true>(a, stream);
+  if (err == cudaSuccess)
+    err = x_launch<XValSmem<D>>(x_values_kernel<D, TO>, K_WALK, dim3(a.nchunk * (D / 64) * 2, a.B * a.H), 256, stream, m, a);
+  if (err == cudaSuccess) err = x_launch<XGradSmem<D>>(x_gradient_kernel<D, TO>, K_WALK_PAIR, dim3(a.nchunk, a.B * a.Hk), 512, stream, m, a);
+  return err;
+}
+
+#undef X_WAIT
+#undef X_HAND_OVER

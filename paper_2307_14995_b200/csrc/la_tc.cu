@@ -14,6 +14,7 @@
 #include <cstddef>
 
 #include "la_common.cuh"
+#include "la_delta.cuh"
 #include "sm100_ptx.cuh"
 
 namespace la {
@@ -167,6 +168,8 @@ bool make_map(CUtensorMap* m, const void* ptr, const OpArgs& a, int D, bool f32 
              CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+#include "la_delta_tc.cuh"
+
 bool make_maps(TcMaps* m, const OpArgs& args, int D) {
   return make_map(&m->a, args.a, args, D, false, 128, args.shared & SHARED_A) &&
          make_map(&m->b, args.b, args, D, false, 128, args.shared & SHARED_B) &&
@@ -276,6 +279,18 @@ cudaError_t launch_tc_prepass(const OpArgs& args, const DecayTable& tab, int D, 
                               cudaStream_t stream) {
   return D == 128 ? launch_states<128>(args, tab, precision, all_segments, stream)
                   : launch_states<64>(args, tab, precision, all_segments, stream);
+}
+
+size_t delta_tc_chunk_bytes(int D, bool bwd) {
+  return D == 128 ? (bwd ? XRec<128>::BWD : XRec<128>::FWD) : (bwd ? XRec<64>::BWD : XRec<64>::FWD);
+}
+cudaError_t launch_delta_tc_fwd(const DeltaArgs& a, int out_dt, cudaStream_t stream) {
+  if (a.D == 128) return out_dt == DT_F32 ? x_fwd<128, float>(a, stream) : x_fwd<128, __nv_bfloat16>(a, stream);
+  return out_dt == DT_F32 ? x_fwd<64, float>(a, stream) : x_fwd<64, __nv_bfloat16>(a, stream);
+}
+cudaError_t launch_delta_tc_bwd(const DeltaArgs& a, bool have_fwd, int out_dt, cudaStream_t stream) {
+  if (a.D == 128) return out_dt == DT_F32 ? x_bwd<128, float>(a, have_fwd, stream) : x_bwd<128, __nv_bfloat16>(a, have_fwd, stream);
+  return out_dt == DT_F32 ? x_bwd<64, float>(a, have_fwd, stream) : x_bwd<64, __nv_bfloat16>(a, have_fwd, stream);
 }
 
 cudaError_t launch_bounded_wait_selftest(long long budget_clocks, cudaStream_t stream) {
