@@ -20,7 +20,8 @@ LIB = os.path.join(HERE, "libla_b200.so")
 CALL = os.path.join(HERE, "_la_call" + sysconfig.get_config_var("EXT_SUFFIX"))
 UNTAGGED_CALL = os.path.join(HERE, "_la_call.so")  # as it was once built: any interpreter would load it
 SOURCES = ["la_api.cu", "la_simt.cu", "la_decode.cu", "la_tc.cu", "la_noalloc.cu", "la_gate.cu", "la_lrpe.cu",
-           "la_extra_api.cu", "la_delta.cu", "la_delta_decode.cu", "la_block_norm.cu"]
+           "la_extra_api.cu", "la_delta.cu", "la_delta_decode.cu", "la_block_norm.cu", "la_block_norm_mixed.cu",
+           "la_block_norm_bf16.cu"]
 HEADERS = ["la_common.cuh", os.path.join("..", "..", "include", "la.h")]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "--expt-relaxed-constexpr", "-Xcompiler", "-fPIC"]

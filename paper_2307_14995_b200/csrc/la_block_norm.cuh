@@ -1,4 +1,4 @@
-// What stands between two blocks: declarations (formulas: la_block_norm.cu).
+// What stands between two blocks: declarations (formulas: la_block_norm_kernels.cuh).
 #pragma once
 #include "la_common.cuh"
 
@@ -20,6 +20,9 @@ struct BlockNormArgs {
   int D, gate, post_norm;
   float eps;
 };
+cudaError_t launch_block_norm_f32(const BlockNormArgs& a, bool backward, cudaStream_t stream);
+cudaError_t launch_block_norm_mixed(const BlockNormArgs& a, bool backward, cudaStream_t stream);  // bf16, residual stream in fp32
+cudaError_t launch_block_norm_bf16(const BlockNormArgs& a, bool backward, cudaStream_t stream);
 cudaError_t launch_block_norm(const BlockNormArgs& a, bool backward, int dt, int res_dt, cudaStream_t stream);
 
 }  // namespace la

@@ -1,0 +1,755 @@
+// What stands between two blocks of a model, one pass over each token's row of D features:
+//   z = y r_y (.) w_post (.) act(u),   h = x + s (.) z,   n = h r_h (.) w_pre,   r_a = 1 / sqrt(mean(a^2) + eps)   (0 for a zero row
+// without eps), and the gradients of <h, dh> + <n, dn>, from x, y and u again:
+//   H = dh + r_h (w_pre dn - n^ mean(w_pre dn n^)),  n^ = h r_h;     dx = H,   ds = sum H z,   dw_pre = sum dn n^,
+//   du = s H y^ w_post act'(u),  y^ = y r_y;     p = s H act(u) w_post,   dw_post = sum s H act(u) y^,   dy = r_y (p - y^ mean(p y^)).
+//
+// HBM bounds both: every input is read once and every output written once, a row stays in registers from the one to the other.  LANES
+// threads share a row (a warp up to 512 features, else a part of a thread block or all of it), each with NV groups of eight
+// features, 16 bytes of bf16 at a time; rows whose width is no multiple of eight are not aligned and take the same features one by
+// one.  The sums over tokens (ds, dw) stay in registers over the rows that a thread block takes, leave it as one part [3][D] in the
+// workspace, and a second kernel adds the parts up in order: no atomics, the same bits every time.
+#pragma once
+#include "la_block_norm.cuh"
+
+namespace la {
+namespace {
+
+constexpr int THREADS = 256;
+
+// eight consecutive features
+template <typename T>
+__device__ __forceinline__ void load8(const T* p, float (&x)[8]) {
+  float a[4], b[4];
+  if constexpr (sizeof(T) == 2) {
+    const uint4 v = *reinterpret_cast<const uint4*>(p);
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[2 * i] = __uint_as_float(w[i] << 16), x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+  } else {
+    Vec4<T>::load(p, a);
+    Vec4<T>::load(p + 4, b);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = a[i], x[4 + i] = b[i];
+  }
+}
+template <typename T>
+__device__ __forceinline__ void store8(T* p, const float (&x)[8]) {
+  if constexpr (sizeof(T) == 2) {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const __nv_bfloat162 v = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
+      w[i] = *reinterpret_cast<const uint32_t*>(&v);
+    }
+    *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+  } else {
+    const float a[4] = {x[0], x[1], x[2], x[3]}, b[4] = {x[4], x[5], x[6], x[7]};
+    Vec4<T>::store(p, a);
+    Vec4<T>::store(p + 4, b);
+  }
+}
+
+// Group v of the thread `lane` of a row: features (v LANES + lane) 8 .. + 7, or, one by one, (8 v + i) LANES + lane.
+template <int LANES, bool VEC>
+struct Cols {
+  int lane, D;
+  template <typename T>
+  __device__ __forceinline__ void load(const T* row, int v, float (&x)[8], float other = 0.f) const {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = other;
+    if (VEC) {
+      const int at = (v * LANES + lane) * 8;
+      if (row && at < D) load8(row + at, x);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int at = (8 * v + i) * LANES + lane;
+        if (row && at < D) x[i] = to_f32(row[at]);
+      }
+    }
+  }
+  template <typename T>
+  __device__ __forceinline__ void store(T* row, int v, const float (&x)[8]) const {
+    if (VEC) {
+      const int at = (v * LANES + lane) * 8;
+      if (at < D) store8(row + at, x);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int at = (8 * v + i) * LANES + lane;
+        if (at < D) row[at] = from_f32<T>(x[i]);
+      }
+    }
+  }
+};
+
+// Sum over the LANES threads of a row, the same in each; `slot` alternates between calls, so one barrier is enough.
+template <int LANES, int ROWS>
+struct RowSum {
+  float part[2][ROWS][LANES <= 32 ? 1 : LANES / 32];
+  __device__ __forceinline__ float operator()(float x, int slot, int row) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+    if (LANES <= 32) return x;
+    if ((threadIdx.x & 31) == 0) part[slot][row][(threadIdx.x / 32) % (LANES / 32)] = x;
+    __syncthreads();
+    x = part[slot][row][0];
+#pragma unroll
+    for (int i = 1; i < LANES / 32; ++i) x += part[slot][row][i];
+    return x;
+  }
+};
+
+__device__ __forceinline__ float inverse_rms(float sum, float inv_d, float eps) {
+  const float m = fmaf(sum, inv_d, eps);
+  return m == 0.f ? 0.f : rsqrtf(m);
+}
+// act(u) and its derivative
+__device__ __forceinline__ float act(int kind, float u, float& slope) {
+  if (kind == GATE_PLAIN) {
+    slope = 1.f;
+    return u;
+  }
+  const float s = 1.f / (1.f + expf(-u));
+  if (kind == GATE_SIGMOID) {
+    slope = s * (1.f - s);
+    return s;
+  }
+  slope = fmaf(u * s, 1.f - s, s);
+  return u * s;
+}
+
+template <typename T, typename TR, int LANES, int NV, bool VEC>
+__global__ void __launch_bounds__(LANES > THREADS ? LANES : THREADS) block_norm_fwd_kernel(const BlockNormArgs a) {
+  constexpr int ROWS = (LANES > THREADS ? LANES : THREADS) / LANES;
+  __shared__ RowSum<LANES, ROWS> sum;
+  grid_dep_wait();
+  grid_dep_launch();
+  const int sub = threadIdx.x / LANES;
+  const Cols<LANES, VEC> cols{(int)threadIdx.x % LANES, a.D};
+  const float inv_d = 1.f / (float)a.D;
+  const long long groups = (a.rows + ROWS - 1) / ROWS;
+  for (long long group = blockIdx.x; group < groups; group += gridDim.x) {
+    const long long row = group * ROWS + sub;
+    const bool mine = row < a.rows;  // (the others keep the barriers company)
+    const long long at = mine ? row * a.D : 0;
+    float y[NV][8], x[NV][8];
+    float ss = 0.f;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      cols.load(static_cast<const T*>(a.y) + at, v, y[v]);
+      cols.load(static_cast<const TR*>(a.x) + at, v, x[v]);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) ss = fmaf(y[v][i], y[v][i], ss);
+    }
+    float ry = 1.f;
+    if (a.post_norm) ry = inverse_rms(sum(ss, 0, sub), inv_d, a.eps);
+    ss = 0.f;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      float w[8], u[8], s[8];
+      cols.load(a.w_post, v, w, 1.f);
+      cols.load(a.s, v, s, 1.f);
+      cols.load(a.u ? static_cast<const T*>(a.u) + at : nullptr, v, u);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        float z = y[v][i] * ry * w[i], slope;
+        if (a.u) z *= act(a.gate, u[i], slope);
+        x[v][i] = fmaf(s[i], z, x[v][i]);
+        ss = fmaf(x[v][i], x[v][i], ss);
+      }
+      if (mine && a.h) cols.store(static_cast<TR*>(a.h) + at, v, x[v]);
+    }
+    if (!a.n) continue;
+    const float rh = inverse_rms(sum(ss, 1, sub), inv_d, a.eps);
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      float w[8];
+      cols.load(a.w_pre, v, w, 1.f);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) w[i] *= x[v][i] * rh;
+      if (mine) cols.store(static_cast<T*>(a.n) + at, v, w);
+    }
+  }
+}
+
+template <typename T, typename TR, int LANES, int NV, bool VEC>
+__global__ void __launch_bounds__(LANES > THREADS ? LANES : THREADS) block_norm_bwd_kernel(const BlockNormArgs a) {
+  constexpr int ROWS = (LANES > THREADS ? LANES : THREADS) / LANES;
+  __shared__ RowSum<LANES, ROWS> sum;
+  grid_dep_wait();
+  grid_dep_launch();
+  const int sub = threadIdx.x / LANES;
+  const Cols<LANES, VEC> cols{(int)threadIdx.x % LANES, a.D};
+  const float inv_d = 1.f / (float)a.D;
+  const long long groups = (a.rows + ROWS - 1) / ROWS;
+  float g_post[NV][8], g_s[NV][8], g_pre[NV][8];
+#pragma unroll
+  for (int v = 0; v < NV; ++v)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) g_post[v][i] = g_s[v][i] = g_pre[v][i] = 0.f;
+  for (long long group = blockIdx.x; group < groups; group += gridDim.x) {
+    const long long row = group * ROWS + sub;
+    const bool mine = row < a.rows;
+    const long long at = mine ? row * a.D : 0;
+    float y[NV][8], h[NV][8], u[NV][8], dn[NV][8];
+    float ss = 0.f;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      cols.load(static_cast<const T*>(a.y) + at, v, y[v]);
+      cols.load(static_cast<const TR*>(a.x) + at, v, h[v]);
+      cols.load(a.u ? static_cast<const T*>(a.u) + at : nullptr, v, u[v]);
+      cols.load(a.dn && mine ? static_cast<const T*>(a.dn) + at : nullptr, v, dn[v]);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) ss = fmaf(y[v][i], y[v][i], ss);
+    }
+    float ry = 1.f;
+    if (a.post_norm) ry = inverse_rms(sum(ss, 0, sub), inv_d, a.eps);
+    ss = 0.f;
+    float dot = 0.f;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      float w[8], s[8], wp[8];
+      cols.load(a.w_post, v, w, 1.f);
+      cols.load(a.s, v, s, 1.f);
+      cols.load(a.w_pre, v, wp, 1.f);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        float z = y[v][i] * ry * w[i], slope;
+        if (a.u) z *= act(a.gate, u[v][i], slope);
+        h[v][i] = fmaf(s[i], z, h[v][i]);
+        ss = fmaf(h[v][i], h[v][i], ss);
+        dot = fmaf(dn[v][i] * wp[i], h[v][i], dot);
+      }
+    }
+    float rh = 0.f, along = 0.f;
+    if (a.dn) {
+      rh = inverse_rms(sum(ss, 1, sub), inv_d, a.eps);
+      along = sum(dot, 0, sub) * rh * inv_d;  // mean(w_pre dn n^)
+    }
+    float py = 0.f;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      float w[8], s[8], wp[8], dh[8], du[8];
+      cols.load(a.w_post, v, w, 1.f);
+      cols.load(a.s, v, s, 1.f);
+      cols.load(a.w_pre, v, wp, 1.f);
+      cols.load(a.dh && mine ? static_cast<const TR*>(a.dh) + at : nullptr, v, dh);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float nh = h[v][i] * rh, yh = y[v][i] * ry;
+        float H = dh[i];
+        if (a.dn) {
+          H = fmaf(rh, dn[v][i] * wp[i] - nh * along, H);
+          g_pre[v][i] = fmaf(dn[v][i], nh, g_pre[v][i]);
+        }
+        dh[i] = H;
+        float gate = 1.f, slope = 0.f;
+        if (a.u) gate = act(a.gate, u[v][i], slope);
+        if (mine) {
+          g_s[v][i] = fmaf(H, yh * w[i] * gate, g_s[v][i]);
+          g_post[v][i] = fmaf(H * s[i], yh * gate, g_post[v][i]);
+        }
+        du[i] = H * s[i] * yh * w[i] * slope;
+        h[v][i] = H * s[i] * gate * w[i];  // p
+        py = fmaf(h[v][i], yh, py);
+      }
+      if (mine) cols.store(static_cast<TR*>(a.dx) + at, v, dh);
+      if (mine && a.u) cols.store(static_cast<T*>(a.du) + at, v, du);
+    }
+    if (a.post_norm) py = sum(py, 1, sub) * inv_d;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      if (a.post_norm) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) h[v][i] = ry * (h[v][i] - y[v][i] * ry * py);
+      }
+      if (mine) cols.store(static_cast<T*>(a.dy) + at, v, h[v]);
+    }
+    __syncthreads();  // (the row's sums have two slots and are used twice)
+  }
+  // the thread block's part; where it has several rows at a time, their threads add up in order
+  float* const part = a.parts + (size_t)blockIdx.x * 3 * a.D;
+  for (int r = 0; r < ROWS; ++r) {
+    if (sub == r) {
+#pragma unroll
+      for (int v = 0; v < NV; ++v)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int c = VEC ? (v * LANES + cols.lane) * 8 + i : (8 * v + i) * LANES + cols.lane;
+          if (c >= a.D) continue;
+          part[c] = g_post[v][i] + (r > 0 ? part[c] : 0.f);
+          part[a.D + c] = g_s[v][i] + (r > 0 ? part[a.D + c] : 0.f);
+          part[2 * a.D + c] = g_pre[v][i] + (r > 0 ? part[2 * a.D + c] : 0.f);
+        }
+    }
+    __syncthreads();
+  }
+}
+
+// ---- many rows -----------------------------------------------------------------------------------------------------------------------------
+// The same with the rows of a thread block's next turns on their way while it works on one: every thread copies what it will read
+// itself into a ring of S stages in shared memory (cp.async), so that nobody waits for anybody but in the row sums.  One thread block
+// of 512 threads to an SM, 512 / LANES rows at a time, each row's threads with a barrier of their own; weights in shared memory,
+// sums over tokens in registers to the end.  65536 x 4096 in bf16, forward and backward, us: the kernels above 740 and 4282, this one 452 and
+// 1194 (409 and 654 at the copy bandwidth).
+//
+// Rows whose width is no multiple of eight move in pairs of features, 4 bytes of bf16: where the width is odd a row begins in the middle
+// of a pair, every second one, and a group of threads takes rows of one kind only, so that a thread's features are the same in all.
+constexpr int RING = 512;
+__device__ __forceinline__ void copy16(uint32_t to, const void* from) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+}
+__device__ __forceinline__ void copy4(uint32_t to, const void* from, int bytes) {  // the rest of the four are zeros
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to), "l"(from), "r"(bytes) : "memory");
+}
+template <int N>
+__device__ __forceinline__ void copies_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+
+// One tensor's place in a stage, and this thread's features of a row: unit u has features (u LANES + lane) F - shift .. + F - 1.
+template <int LANES, int NV, bool VEC>
+struct RingRow {
+  static constexpr int F = VEC ? 8 : 2, U = 8 * NV / F;
+  int lane, D, shift;
+  long long total;  // features of the tensor
+  __device__ __forceinline__ int feature(int u) const { return (u * LANES + lane) * F - shift; }
+  template <typename T>
+  static constexpr int bytes() { return RING * 8 * NV * (int)sizeof(T); }
+  // stage memory: unit u of thread t in 16- (4-) byte pieces at piece (k U + u) RING + t, k the piece of the unit
+  template <typename T>
+  __device__ __forceinline__ void fetch(uint32_t to, const T* base, long long row) const {
+    constexpr int PIECE = VEC ? 16 : 4, K = F * (int)sizeof(T) / PIECE, PER = F / K;  // pieces of a unit, features of a piece
+    const T* const at = base + row * D;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int f = feature(u);
+#pragma unroll
+      for (int k = 0; k < K; ++k) {
+        const uint32_t dst = to + (uint32_t)((k * U + u) * RING + threadIdx.x) * PIECE;
+        const int g = f + k * PER;
+        if (VEC) {
+          if (g < D) copy16(dst, at + g);
+        } else if (sizeof(T) == 4) {
+          if (g >= 0 && g < D) copy4(dst, at + g, 4);
+        } else if (g + 1 >= 0 && g < D) {
+          copy4(dst, at + g, row * D + g + 2 <= total ? 4 : 2);
+        }
+      }
+    }
+  }
+  template <typename T>
+  __device__ __forceinline__ void get(const unsigned char* from, int u, float (&x)[F]) const {
+    constexpr int PIECE = VEC ? 16 : 4, K = F * (int)sizeof(T) / PIECE;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const unsigned char* const src = from + ((k * U + u) * RING + threadIdx.x) * PIECE;
+      if constexpr (VEC && sizeof(T) == 2) {
+        const uint4 v = *reinterpret_cast<const uint4*>(src);
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[2 * i] = __uint_as_float(w[i] << 16), x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+      } else if constexpr (VEC) {
+        const float4 v = *reinterpret_cast<const float4*>(src);
+        x[4 * k] = v.x; x[4 * k + 1] = v.y; x[4 * k + 2] = v.z; x[4 * k + 3] = v.w;
+      } else if constexpr (sizeof(T) == 2) {
+        const uint32_t w = *reinterpret_cast<const uint32_t*>(src);
+        const int f = feature(u);
+        x[0] = f >= 0 && f < D ? __uint_as_float(w << 16) : 0.f;
+        x[1] = f + 1 < D ? __uint_as_float(w & 0xffff0000u) : 0.f;
+      } else {
+        const float w = *reinterpret_cast<const float*>(src);
+        const int f = feature(u) + k;
+        x[k] = f >= 0 && f < D ? w : 0.f;
+      }
+    }
+  }
+  template <typename T>
+  __device__ __forceinline__ void put(T* base, long long row, int u, const float (&x)[F]) const {
+    T* const at = base + row * D;
+    const int f = feature(u);
+    if constexpr (VEC) {
+      if (f < D) store8(at + f, x);
+    } else {
+      if (f >= 0 && f < D) at[f] = from_f32<T>(x[0]);
+      if (f + 1 < D) at[f + 1] = from_f32<T>(x[1]);
+    }
+  }
+  __device__ __forceinline__ void weights(const float* w, int u, float (&x)[F]) const {  // [D] in shared memory, with a margin of 16
+    const int f = feature(u);
+    if constexpr (VEC) {
+      const int at = f < D ? f : 0;
+      const float4 a = *reinterpret_cast<const float4*>(w + at), b = *reinterpret_cast<const float4*>(w + at + 4);
+      x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+    } else {
+      x[0] = w[f >= 0 && f < D ? f : 0];
+      x[1] = w[f + 1 < D ? f + 1 : 0];
+    }
+  }
+};
+
+// Sums of one or two values over a row's threads: over each warp's lanes, then every warp adds up the warps' sums the same way.
+template <int LANES>
+struct RowSums {
+  float part[2][2][RING / 32];
+  template <int N>
+  __device__ __forceinline__ void operator()(float (&x)[N], int& slot) {
+    constexpr int W = LANES / 32;
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) x[n] += __shfl_xor_sync(0xffffffffu, x[n], o);
+    if (W <= 1) return;
+    const int warp = threadIdx.x / 32, lane = threadIdx.x & 31, first = warp / W * W;
+    if (lane < N) part[slot][lane][warp] = lane == 0 ? x[0] : x[N - 1];
+    asm volatile("bar.sync %0, %1;" ::"r"(1 + first / W), "n"(LANES) : "memory");
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      x[n] = part[slot][n][first + lane % W];
+#pragma unroll
+      for (int o = W / 2; o > 0; o >>= 1) x[n] += __shfl_xor_sync(0xffffffffu, x[n], o);
+    }
+    slot ^= 1;  // (written again behind the next sum's barrier)
+  }
+};
+
+// 1 / (1 + exp(-u)), exp and the reciprocal good to an ulp or two (relative 2^-22); where exp is infinite it is 0.
+__device__ __forceinline__ float sigmoid(float u) {
+  float r;
+  asm("{\n\t.reg .f32 e;\n\tmul.f32 e, %1, 0fBFB8AA3B;\n\tex2.approx.f32 e, e;\n\tadd.f32 e, e, 0f3F800000;\n\trcp.approx.f32 %0, e;\n\t}" : "=f"(r) : "f"(u));
+  return r;
+}
+// g becomes act(g), slope act'(g); one branch for all of a unit's features
+template <int F>
+__device__ __forceinline__ void gate_values(int kind, float (&g)[F]) {
+  if (kind == GATE_PLAIN) return;
+  if (kind == GATE_SIGMOID) {
+#pragma unroll
+    for (int i = 0; i < F; ++i) g[i] = sigmoid(g[i]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < F; ++i) g[i] *= sigmoid(g[i]);
+  }
+}
+template <int F>
+__device__ __forceinline__ void gate_values(int kind, float (&g)[F], float (&slope)[F]) {
+  if (kind == GATE_SILU) {
+#pragma unroll
+    for (int i = 0; i < F; ++i) {
+      const float s = sigmoid(g[i]);
+      g[i] *= s;
+      slope[i] = fmaf(g[i], 1.f - s, s);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < F; ++i) {
+      slope[i] = 1.f;
+      if (kind == GATE_SIGMOID) {
+        g[i] = sigmoid(g[i]);
+        slope[i] = g[i] * (1.f - g[i]);
+      }
+    }
+  }
+}
+
+template <typename T, typename TR, int LANES, int NV, bool VEC, bool BWD>
+__global__ void __launch_bounds__(RING, 1) block_norm_ring_kernel(const BlockNormArgs a, const int S) {
+  using Row = RingRow<LANES, NV, VEC>;
+  constexpr int F = Row::F, U = Row::U, ROWS = RING / LANES;
+  constexpr int BT = Row::template bytes<T>(), BR = Row::template bytes<TR>();
+  extern __shared__ __align__(16) unsigned char ring[];
+  __shared__ RowSums<LANES> sums;
+  grid_dep_wait();
+  grid_dep_launch();
+  // the stages: y, x, u and backward dn, dh; behind them the weights
+  const int stage_bytes = BT + BR + (a.u ? BT : 0) + (BWD ? BT + BR : 0);
+  const int at_x = BT, at_u = BT + BR, at_dn = at_u + (a.u ? BT : 0), at_dh = at_dn + BT;
+  float* const w_post = reinterpret_cast<float*>(ring + S * stage_bytes);
+  const int wd = (a.D + 19) / 4 * 4;
+  float *const w_s = w_post + wd, *const w_pre = w_s + wd;
+  for (int i = threadIdx.x; i < S * stage_bytes / 16; i += RING) reinterpret_cast<uint4*>(ring)[i] = make_uint4(0u, 0u, 0u, 0u);  // units past the end stay zeros
+  for (int i = threadIdx.x; i < wd; i += RING) {
+    w_post[i] = a.w_post && i < a.D ? a.w_post[i] : 1.f;
+    w_s[i] = a.s && i < a.D ? a.s[i] : 1.f;
+    w_pre[i] = a.w_pre && i < a.D ? a.w_pre[i] : 1.f;
+  }
+  __syncthreads();
+  const int sub = threadIdx.x / LANES;
+  const long long first = (long long)blockIdx.x * ROWS + sub, step = (long long)gridDim.x * ROWS;
+  const Row my{(int)threadIdx.x % LANES, a.D, VEC ? 0 : (int)((first * a.D) & 1), a.rows * a.D};
+  const float inv_d = 1.f / (float)a.D;
+  const uint32_t ring_at = static_cast<uint32_t>(__cvta_generic_to_shared(ring));
+  auto fetch = [&](long long row, int s) {
+    if (row < a.rows) {
+      const uint32_t to = ring_at + s * stage_bytes;
+      my.fetch(to, static_cast<const T*>(a.y), row);
+      my.fetch(to + at_x, static_cast<const TR*>(a.x), row);
+      if (a.u) my.fetch(to + at_u, static_cast<const T*>(a.u), row);
+      if (BWD && a.dn) my.fetch(to + at_dn, static_cast<const T*>(a.dn), row);
+      if (BWD && a.dh) my.fetch(to + at_dh, static_cast<const TR*>(a.dh), row);
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  float g_post[BWD ? U : 1][F], g_s[BWD ? U : 1][F], g_pre[BWD ? U : 1][F];
+#pragma unroll
+  for (int u = 0; u < (BWD ? U : 1); ++u)
+#pragma unroll
+    for (int i = 0; i < F; ++i) g_post[u][i] = g_s[u][i] = g_pre[u][i] = 0.f;
+  for (int s = 0; s < S; ++s) fetch(first + s * step, s);
+  int s = 0, slot = 0;
+  for (long long row = first; row < a.rows; row += step) {
+    if (S == 3) copies_wait<2>();
+    else if (S == 2) copies_wait<1>();
+    else copies_wait<0>();
+    const unsigned char* const in = ring + s * stage_bytes;
+    // With eight features to a thread what is read stays in registers; with sixteen it is read again where it is used.
+    constexpr bool KEEP = NV == 1;
+    float y[U][F], g[U][F], slope[U][F], dn[U][F], h[U][F];
+    auto get_y = [&](int u) { my.template get<T>(in, u, y[u]); };
+    auto get_gate = [&](int u) {
+      if (a.u) {
+        my.template get<T>(in + at_u, u, g[u]);
+        if (BWD) gate_values(a.gate, g[u], slope[u]);
+        else gate_values(a.gate, g[u]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < F; ++i) g[u][i] = 1.f, slope[u][i] = 0.f;
+      }
+    };
+    float ry = 1.f;
+    if (KEEP || a.post_norm) {
+      float ss[1] = {0.f};
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        get_y(u);
+#pragma unroll
+        for (int i = 0; i < F; ++i) ss[0] = fmaf(y[u][i], y[u][i], ss[0]);
+      }
+      if (a.post_norm) {
+        sums(ss, slot);
+        ry = inverse_rms(ss[0], inv_d, a.eps);
+      }
+    }
+    float both[2] = {0.f, 0.f};  // of h squared, of w_pre dn h
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      float x[F], w[F], sc[F];
+      if (!KEEP) get_y(u);
+      my.template get<TR>(in + at_x, u, x);
+      get_gate(u);
+      my.weights(w_post, u, w);
+      my.weights(w_s, u, sc);
+#pragma unroll
+      for (int i = 0; i < F; ++i) {
+        h[u][i] = fmaf(sc[i], y[u][i] * ry * w[i] * g[u][i], x[i]);
+        both[0] = fmaf(h[u][i], h[u][i], both[0]);
+      }
+      if (BWD) {
+        my.template get<T>(in + at_dn, u, dn[u]);
+        my.weights(w_pre, u, w);
+#pragma unroll
+        for (int i = 0; i < F; ++i) both[1] = fmaf(dn[u][i] * w[i], h[u][i], both[1]);
+      }
+      if (!BWD && a.h) my.put(static_cast<TR*>(a.h), row, u, h[u]);
+    }
+    if (!BWD) {
+      fetch(row + S * step, s);
+      if (a.n) {
+        float ss[1] = {both[0]};
+        sums(ss, slot);
+        const float rh = inverse_rms(ss[0], inv_d, a.eps);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          float w[F];
+          my.weights(w_pre, u, w);
+#pragma unroll
+          for (int i = 0; i < F; ++i) w[i] *= h[u][i] * rh;
+          my.put(static_cast<T*>(a.n), row, u, w);
+        }
+      }
+    } else {
+      float rh = 0.f, along = 0.f, py[1] = {0.f};
+      if (a.dn) {
+        sums(both, slot);
+        rh = inverse_rms(both[0], inv_d, a.eps);
+        along = both[1] * rh * inv_d;  // mean(w_pre dn n^)
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        float w[F], sc[F], dh[F];
+        if (!KEEP) {
+          get_y(u);
+          get_gate(u);
+          my.template get<T>(in + at_dn, u, dn[u]);
+        }
+        my.template get<TR>(in + at_dh, u, dh);
+        my.weights(w_pre, u, w);
+#pragma unroll
+        for (int i = 0; i < F; ++i) {
+          const float nh = h[u][i] * rh;
+          dh[i] = fmaf(rh, fmaf(-nh, along, dn[u][i] * w[i]), dh[i]);  // H
+          g_pre[u][i] = fmaf(dn[u][i], nh, g_pre[u][i]);
+        }
+        my.put(static_cast<TR*>(a.dx), row, u, dh);
+        my.weights(w_post, u, w);
+        my.weights(w_s, u, sc);
+#pragma unroll
+        for (int i = 0; i < F; ++i) {
+          const float yh = y[u][i] * ry, Hg = dh[i] * g[u][i], Hsg = Hg * sc[i], yw = yh * w[i];
+          g_s[u][i] = fmaf(Hg, yw, g_s[u][i]);
+          g_post[u][i] = fmaf(Hsg, yh, g_post[u][i]);
+          slope[u][i] *= dh[i] * sc[i] * yw;  // du
+          h[u][i] = Hsg * w[i];               // p
+          py[0] = fmaf(h[u][i], yh, py[0]);
+        }
+        if (a.u) my.put(static_cast<T*>(a.du), row, u, slope[u]);
+      }
+      if (KEEP) fetch(row + S * step, s);
+      if (a.post_norm) sums(py, slot);
+      const float along_y = a.post_norm ? py[0] * inv_d * ry : 0.f;
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if (!KEEP) get_y(u);
+#pragma unroll
+        for (int i = 0; i < F; ++i) h[u][i] = ry * fmaf(-y[u][i], along_y, h[u][i]);
+        my.put(static_cast<T*>(a.dy), row, u, h[u]);
+      }
+      if (!KEEP) fetch(row + S * step, s);
+    }
+    if (++s == S) s = 0;
+  }
+  if (!BWD) return;
+  // the thread block's part: its rows' threads add up in order
+  copies_wait<0>();
+  __syncthreads();
+  float* const mine = reinterpret_cast<float*>(ring) + (size_t)sub * 3 * a.D;
+  float* const part = a.parts + (size_t)blockIdx.x * 3 * a.D;
+#pragma unroll
+  for (int u = 0; u < U; ++u)
+#pragma unroll
+    for (int i = 0; i < F; ++i) {
+      const int f = my.feature(u) + i;
+      if (f < 0 || f >= a.D) continue;
+      mine[f] = g_post[BWD ? u : 0][i];
+      mine[a.D + f] = g_s[BWD ? u : 0][i];
+      mine[2 * a.D + f] = g_pre[BWD ? u : 0][i];
+    }
+  __syncthreads();
+  for (int c = threadIdx.x; c < 3 * a.D; c += RING) {
+    float x = reinterpret_cast<const float*>(ring)[c];
+    for (int r = 1; r < ROWS; ++r) x += reinterpret_cast<const float*>(ring)[(size_t)r * 3 * a.D + c];
+    part[c] = x;
+  }
+}
+
+// Adds up the parts: 32 features to a thread block, the parts shared by its eight warps.
+__global__ void __launch_bounds__(THREADS) block_norm_sum_kernel(const float* parts, int nparts, int D, float* dw_post, float* ds, float* dw_pre) {
+  __shared__ float red[THREADS / 32][32];
+  grid_dep_wait();
+  grid_dep_launch();
+  const int c = blockIdx.x * 32 + (threadIdx.x & 31), w = threadIdx.x / 32;
+  float x = 0.f;
+  if (c < 3 * D) {
+#pragma unroll 8
+    for (int p = w; p < nparts; p += THREADS / 32) x += parts[(size_t)p * 3 * D + c];
+  }
+  red[w][threadIdx.x & 31] = x;
+  __syncthreads();
+  if (w == 0 && c < 3 * D) {
+#pragma unroll
+    for (int i = 1; i < THREADS / 32; ++i) x += red[i][threadIdx.x];
+    float* const to = c < D ? dw_post : c < 2 * D ? ds : dw_pre;
+    if (to) to[c % D] = x;
+  }
+}
+
+cudaError_t sum_parts(const BlockNormArgs& a, int n, cudaStream_t stream);
+
+template <typename T, typename TR, int LANES, int NV, bool VEC>
+cudaError_t run(const BlockNormArgs& a, bool backward, cudaStream_t stream) {
+  constexpr int BLOCK = LANES > THREADS ? LANES : THREADS, ROWS = BLOCK / LANES;
+  const long long groups = (a.rows + ROWS - 1) / ROWS;
+  KernelTimer timer(K_GATE, stream);
+  cudaError_t err;
+  if (backward) {
+    err = launch_early(block_norm_bwd_kernel<T, TR, LANES, NV, VEC>, dim3((unsigned)(groups < a.nparts ? groups : a.nparts)), dim3(BLOCK), 0, stream, 1, a);
+  } else {
+    const long long cap = 148LL * 64;  // a few waves, then each thread block takes further rows
+    err = launch_early(block_norm_fwd_kernel<T, TR, LANES, NV, VEC>, dim3((unsigned)(groups < cap ? groups : cap)), dim3(BLOCK), 0, stream, 1, a);
+  }
+  count_launch();
+  if (err == cudaSuccess) err = cudaGetLastError();
+  if (err != cudaSuccess || !backward) return err;
+  return sum_parts(a, (int)(groups < a.nparts ? groups : a.nparts), stream);
+}
+
+cudaError_t sum_parts(const BlockNormArgs& a, int n, cudaStream_t stream) {
+  KernelTimer timer(K_GATE, stream);
+  const cudaError_t err = launch_early(block_norm_sum_kernel, dim3((unsigned)((3 * a.D + 31) / 32)), dim3(THREADS), 0, stream, 1,
+                                       (const float*)a.parts, n, a.D, a.dw_post, a.ds, a.dw_pre);
+  count_launch();
+  return err != cudaSuccess ? err : cudaGetLastError();
+}
+
+template <typename T, typename TR, int LANES, int NV, bool VEC, bool BWD>
+cudaError_t run_ring(const BlockNormArgs& a, cudaStream_t stream) {
+  using Row = RingRow<LANES, NV, VEC>;
+  constexpr int ROWS = RING / LANES, BT = Row::template bytes<T>(), BR = Row::template bytes<TR>();
+  const int stage = BT + BR + (a.u ? BT : 0) + (BWD ? BT + BR : 0), weights = 3 * ((a.D + 19) / 4 * 4) * 4;
+  const int most = 227 * 1024 - 512;
+  const int stages = 3 * stage + weights <= most ? 3 : 2 * stage + weights <= most ? 2 : 1;
+  int smem = stages * stage + weights;
+  if (BWD && smem < ROWS * 3 * a.D * 4) smem = ROWS * 3 * a.D * 4;
+  if (smem > most) return cudaErrorNotSupported;
+  auto kern = block_norm_ring_kernel<T, TR, LANES, NV, VEC, BWD>;
+  cudaError_t err = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  if (err != cudaSuccess) return err;
+  long long grid = (a.rows + ROWS - 1) / ROWS;
+  grid = grid < 148 ? (grid + 1) / 2 * 2 : 148;  // even: see RingRow::shift
+  if (BWD && grid > a.nparts) return cudaErrorInvalidValue;
+  {
+    KernelTimer timer(K_GATE, stream);
+    err = launch_early(kern, dim3((unsigned)grid), dim3(RING), smem, stream, 1, a, stages);
+    count_launch();
+    if (err == cudaSuccess) err = cudaGetLastError();
+  }
+  return err != cudaSuccess || !BWD ? err : sum_parts(a, (int)grid, stream);
+}
+
+// Backward eight features to a thread as far as 512 threads go: with sixteen its sums over tokens leave too few registers.
+template <typename T, typename TR, bool VEC, bool BWD>
+cudaError_t ring_by_width(const BlockNormArgs& a, cudaStream_t stream) {
+  if (a.D <= 256) return run_ring<T, TR, 32, 1, VEC, BWD>(a, stream);
+  if (a.D <= 512) return run_ring<T, TR, BWD ? 64 : 32, BWD ? 1 : 2, VEC, BWD>(a, stream);
+  if (a.D <= 1024) return run_ring<T, TR, 128, 1, VEC, BWD>(a, stream);
+  if (a.D <= 2048) return run_ring<T, TR, BWD ? 256 : 128, BWD ? 1 : 2, VEC, BWD>(a, stream);
+  if (a.D <= 4096) return run_ring<T, TR, BWD ? 512 : 256, BWD ? 1 : 2, VEC, BWD>(a, stream);
+  return run_ring<T, TR, 512, 2, VEC, BWD>(a, stream);
+}
+
+template <typename T, typename TR, bool VEC>
+cudaError_t by_width(const BlockNormArgs& a, bool backward, cudaStream_t stream) {
+  // few rows end before a ring is full; wide ones in fp32 do not fit in it
+  if (a.D <= 8192 && a.rows >= 296) {
+    const cudaError_t err = backward ? ring_by_width<T, TR, VEC, true>(a, stream) : ring_by_width<T, TR, VEC, false>(a, stream);
+    if (err != cudaErrorNotSupported) return err;
+  }
+  if (a.D <= 256) return run<T, TR, 32, 1, VEC>(a, backward, stream);
+  if (a.D <= 512) return run<T, TR, 32, 2, VEC>(a, backward, stream);
+  if (a.D <= 1024) return run<T, TR, 128, 1, VEC>(a, backward, stream);
+  if (a.D <= 2048) return run<T, TR, 128, 2, VEC>(a, backward, stream);
+  if (a.D <= 4096) return run<T, TR, 256, 2, VEC>(a, backward, stream);
+  if (a.D <= 8192) return run<T, TR, 512, 2, VEC>(a, backward, stream);
+  if (a.D <= BLOCK_NORM_MAX_D) return run<T, TR, 1024, 2, VEC>(a, backward, stream);
+  return cudaErrorInvalidValue;
+}
+template <typename T, typename TR>
+cudaError_t by_alignment(const BlockNormArgs& a, bool backward, cudaStream_t stream) {
+  return a.D % 8 == 0 ? by_width<T, TR, true>(a, backward, stream) : by_width<T, TR, false>(a, backward, stream);
+}
+
+}  // namespace
+
+}  // namespace la

@@ -29,8 +29,9 @@
 template <int D>
 struct XRec {
   static constexpr size_t STATE = (size_t)D * D * 4;  // an image of a state or a state in fp32
-  static constexpr size_t ALL = 0;                     // e^G_end
-  static constexpr size_t U = 256, X = U + 65536, M = X + 65536, N = M + STATE, S = N + STATE, FWD = S + STATE;
+  static constexpr size_t ALL = 0, END = 8;            // e^G_end, and its logarithm as two terms
+  static constexpr size_t GATES = 256;                 // XGateTable
+  static constexpr size_t U = GATES + 2560, X = U + 65536, M = X + 65536, N = M + STATE, S = N + STATE, FWD = S + STATE;
   static constexpr size_t TOK = (size_t)128 * D * 4;  // an image or fp32 values of all tokens
   static constexpr size_t Z = 0, DR = Z + TOK, Y = DR + TOK, B = Y + TOK, E = B + STATE, BWD = E + STATE;
 };
@@ -67,12 +68,12 @@ __device__ __forceinline__ void join8(const uint4& h, const uint4& l, float* x) 
   x[4] = bf_lo(h.z) + bf_lo(l.z); x[5] = bf_hi(h.z) + bf_hi(l.z);
   x[6] = bf_lo(h.w) + bf_lo(l.w); x[7] = bf_hi(h.w) + bf_hi(l.w);
 }
-// 32 accumulator columns of this thread's lane
+// 16 accumulator columns of this thread's lane (a wait has to follow), or 32
+__device__ __forceinline__ void load_acc16(uint32_t taddr, float (&x)[16]) { tmem_ld_x16(taddr, *reinterpret_cast<uint32_t(*)[16]>(&x)); }
 __device__ __forceinline__ void load_acc(uint32_t taddr, float (&x)[32]) {
   tmem_ld_x32(taddr, *reinterpret_cast<uint32_t(*)[32]>(&x));
   tmem_ld_wait();
 }
-__device__ __forceinline__ float (&half32(float (&x)[64], int i))[32] { return *reinterpret_cast<float(*)[32]>(&x[32 * i]); }
 // 32 values as an A operand: 16 columns of hi terms, 16 of lo terms
 __device__ __forceinline__ void store_operand(uint32_t hi, uint32_t lo, const float (&x)[32]) {
   uint32_t h[16], l[16];
@@ -83,35 +84,56 @@ __device__ __forceinline__ void store_operand(uint32_t hi, uint32_t lo, const fl
 }
 
 // Decay sums of a chunk in units of log2, as two fp32 terms each: their differences keep the accuracy of the small ones among large.
-struct alignas(16) XGates {
+// A decay from token j to token i of another block of 32 is the product of the one from j to its block's last token (or to the first of
+// i's) and the rest, one factor per row and block and one per column, both at most 1 and made once; inside a block of 32 it is an
+// exponential of its own.
+struct alignas(16) XGateTable {
   float2 sum[128];
   float beta[128];
-  double part[4];
+  float to_last[128];     // beta_j times the decay from j to the last token of its block of 32
+  float from_first[128];  // decay from the first token of i's block of 32 to i
 };
+static_assert(sizeof(XGateTable) == 2560, "as the workspace has it");
 __device__ __forceinline__ float decay2(const float2& a, const float2& b) { return ex2_approx((a.x - b.x) + (a.y - b.y)); }
 __device__ __forceinline__ float2 two_terms(double x) {
   const float h = (float)x;
   return make_float2(h, (float)(x - (double)h));
 }
-// Threads 0 .. 127 (whole warps) sum up; every thread of the block calls, a barrier has to follow.  end: the whole chunk's sum.
-__device__ __forceinline__ void load_gates2(XGates& s, const DeltaArgs& a, long long gate, int n, int tid, float2& end) {
+// Threads 0 .. 127 make a chunk's table, in shared memory and in its record, from where the other kernels take it; every thread of
+// the block calls, a barrier has to follow.  part: four doubles.  end: the whole chunk's sum.
+__device__ __forceinline__ void make_gates(XGateTable& s, double* part, unsigned char* rec, size_t table, float g, float beta, int tid, float2& end) {
   double x = 0.0;
   if (tid < 128) {
-    if (tid < n) x = clamped_log_decay(a.g[gate + tid * a.gT]) * 1.4426950408889634;
-    s.beta[tid] = tid < n ? a.beta[gate + tid * a.gT] : 0.f;
+    x = clamped_log_decay(g) * 1.4426950408889634;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
       const double y = __shfl_up_sync(0xffffffffu, x, o);
       if ((tid & 31) >= o) x += y;
     }
-    if ((tid & 31) == 31) s.part[tid >> 5] = x;
+    if ((tid & 31) == 31) part[tid >> 5] = x;
   }
   __syncthreads();
+  end = two_terms(((part[0] + part[1]) + part[2]) + part[3]);
   if (tid < 128) {
-    for (int w = 0; w < (tid >> 5); ++w) x += s.part[w];
-    s.sum[tid] = two_terms(x);
+    for (int w = 0; w < (tid >> 5); ++w) x += part[w];
+    const float2 own = two_terms(x);
+    const float2 last = make_float2(__shfl_sync(0xffffffffu, own.x, 31), __shfl_sync(0xffffffffu, own.y, 31));
+    const float2 first = make_float2(__shfl_sync(0xffffffffu, own.x, 0), __shfl_sync(0xffffffffu, own.y, 0));
+    const float to_last = beta * decay2(last, own), from_first = decay2(own, first);
+    s.sum[tid] = own;
+    s.beta[tid] = beta;
+    s.to_last[tid] = to_last;
+    s.from_first[tid] = from_first;
+    XGateTable& kept = *reinterpret_cast<XGateTable*>(rec + table);
+    kept.sum[tid] = own;
+    kept.beta[tid] = beta;
+    kept.to_last[tid] = to_last;
+    kept.from_first[tid] = from_first;
+    if (tid == 0) {
+      *reinterpret_cast<float*>(rec) = ex2_approx(end.x + end.y);
+      *reinterpret_cast<float2*>(rec + 8) = end;
+    }
   }
-  end = two_terms(((s.part[0] + s.part[1]) + s.part[2]) + s.part[3]);
 }
 
 struct XPlace {
@@ -131,13 +153,19 @@ __device__ __forceinline__ XPlace x_place(const DeltaArgs& a, int bh, int c) {
   return p;
 }
 
-#define X_WAIT(bar, par, code)                                              \
-  do {                                                                      \
-    const bool ok_ = wait_or_abort(&(bar), (par), &sm.abort);               \
-    if (!ok_ && !sm.abort) atomicCAS(&g_tc_status, 0u, (unsigned)(code));   \
-    if (!ok_) sm.abort = 1;                                                 \
-    if (!__syncthreads_and(ok_)) return false;                              \
-    tc_fence_after_sync();                                                  \
+// One warp looks, the others stand at the block's barrier: sixteen that look take the instruction slots of the thread block beside them
+// (half of the prepare kernel's instructions were such looks).  Then each sees the completed phase for itself.
+#define X_WAIT(bar, par, code)                                                \
+  do {                                                                        \
+    bool ok_ = true;                                                          \
+    if (threadIdx.x < 32) {                                                   \
+      ok_ = wait_or_abort(&(bar), (par), &sm.abort);                          \
+      if (!ok_ && !sm.abort) atomicCAS(&g_tc_status, 0u, (unsigned)(code));   \
+      if (!ok_) sm.abort = 1;                                                 \
+    }                                                                         \
+    if (!__syncthreads_and(ok_)) return false;                                \
+    if (threadIdx.x >= 32) (void)mbar_try_wait(&(bar), (par));                \
+    tc_fence_after_sync();                                                    \
   } while (0)
 
 // Operands written to shared memory (or tensor memory) are handed to the tensor cores: fences and a barrier.
@@ -201,21 +229,27 @@ __device__ __forceinline__ uint32_t kmaj(const void* p) { return umma_desc_lo(sm
 __device__ __forceinline__ uint32_t mnmaj(const void* p, uint32_t panel = 16384) { return umma_desc_lo(smem_u32(p), panel); }
 
 // ---- prepare ---------------------------------------------------------------------------------------------------------------------------
-// One thread block of 256 threads per chunk; 97 KB of shared memory and 256 columns of tensor memory, so that two share an SM and one's
-// products run beside the other's conversions.  Thread (q, lane) of half `half` has row q * 32 + lane of every accumulator and of every
-// image, columns half * 64 .. + 63.
+// One thread block of 512 threads per chunk; 101 KB of shared memory and 256 columns of tensor memory, so that two share an SM and one's
+// products run beside the other's conversions.  Thread (q, lane) of quarter w has row q * 32 + lane of every accumulator and of every
+// image, columns w * 32 .. + 31: one block of 32 tokens.
 //
-// The inverse U of the upper triangular I + (n diag(beta))^T, in fp32 as far as the CUDA cores make it: columns of the four diagonal
-// blocks of 32 by back substitution (a warp each), then U12 = -U11 A12 U22 for the two blocks of 64, then the same once more on the
-// tensor cores for the whole.  Powers of the triangle would need no order of rows, but grow far beyond the inverse where keys are alike.
+// The inverse U of the upper triangular I + (n diag(beta))^T, in fp32 as far as the CUDA cores make it: columns of the eight diagonal
+// blocks of 16 by back substitution (a warp each), then U12 = -U11 A12 U22 for the blocks of 32 and of 64, then the same once more on
+// the tensor cores for the whole.  Powers of the triangle would need no order of rows, but grow far beyond the inverse where keys are
+// alike.
+//
+// What it costs is the latency of its eleven dependent steps, of which seven wait for a product, and the instructions between them: with
+// 256 threads to a block and all loops unrolled it was 100 KB of instructions, each executed once and fetched for it, and took 68 us
+// a chunk and SM; with decays as products of factors and most loops left as loops 18; with 512 threads see the table of measurements.
 enum { XP_LOAD = 0, XP_V, XP_MMA, XP_DRAIN, XP_BARS };
 template <int D>
 struct alignas(1024) XPrepSmem {
   unsigned char k[32768];  // (D = 64: the keys twice)
-  unsigned char x[65536];  // q; blocks of A and U in fp32; image of U; v; image of M
-  XGates gates;
+  unsigned char x[65536];  // q; blocks of A and U in fp32; images of U and X; v; image of M
+  XGateTable gates;
   float until[128];        // beta e^(G_end - G)
   float since[128];        // e^G
+  double part[4];
   uint64_t bars[XP_BARS];
   int armed[XP_BARS];
   uint32_t tmem_slot;
@@ -226,29 +260,34 @@ struct alignas(1024) XPrepSmem {
 __device__ __forceinline__ int block_at(int i, int m) { return i * 64 + ((((m >> 2) ^ i) & 15) << 2) + (m & 3); }
 
 template <int D>
-__global__ void __launch_bounds__(256, 2)
+__global__ void __launch_bounds__(512, 2)
 x_prepare_kernel(const __grid_constant__ XMaps maps, const __grid_constant__ DeltaArgs a) {
   extern __shared__ unsigned char smem_raw[];
   using Rec = XRec<D>;
   XPrepSmem<D>& sm = *reinterpret_cast<XPrepSmem<D>*>(smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u));
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, q = warp & 3, half = warp >> 2, row = q * 32 + lane;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, q = warp & 3, w4 = warp >> 2, row = q * 32 + lane, c0 = w4 * 32;
   x_run<256>(sm, XP_BARS, [&](const uint32_t tmem) -> bool {
     const XPlace p = x_place(a, blockIdx.y, blockIdx.x);
     unsigned char* const rec = static_cast<unsigned char*>(a.ws) + p.rec * Rec::FWD;
     const uint32_t R = tmem, P = tmem + 128, mine = (uint32_t)(q * 32) << 16;
     constexpr int PANELS = D / 64;
+    float g_own = 0.f, beta_own = 0.f;
+    if (tid < p.n) {
+      g_own = ld_f1(a.g + p.gate + tid * a.gT);
+      beta_own = ld_f1(a.beta + p.gate + tid * a.gT);
+    }
     if (tid == 0) {
       uint64_t* const bar = expect(sm, XP_LOAD, (2 + PANELS) * 16384);
       for (int x = 0; x < 2; ++x) tma_load_4d(sm.k + x * 16384, &maps.k, bar, D == 128 ? x * 64 : 0, blockIdx.x * 128, p.hk, p.b);
       for (int x = 0; x < PANELS; ++x) tma_load_4d(sm.x + x * 16384, &maps.q, bar, x * 64, blockIdx.x * 128, p.hk, p.b);
+      for (int x = 0; x < PANELS; ++x) tma_prefetch_4d(&maps.v, x * 64, blockIdx.x * 128, p.h, p.b);
     }
     float2 end;
-    load_gates2(sm.gates, a, p.gate, p.n, tid, end);
+    make_gates(sm.gates, sm.part, rec, Rec::GATES, g_own, beta_own, tid, end);
     if (tid < 128) {
       const float2 s = sm.gates.sum[tid];
       sm.since[tid] = ex2_approx(s.x + s.y);
-      sm.until[tid] = sm.gates.beta[tid] * decay2(end, s);
-      if (tid == 0) *reinterpret_cast<float*>(rec + Rec::ALL) = ex2_approx(end.x + end.y);
+      sm.until[tid] = beta_own * decay2(end, s);
     }
     constexpr uint32_t ID_KK = umma_idesc_bf16(128, 128, false, false);
     constexpr uint32_t ID_KN64 = umma_idesc_bf16(128, 64, false, true);
@@ -268,58 +307,79 @@ x_prepare_kernel(const __grid_constant__ XMaps maps, const __grid_constant__ Del
     par ^= 1;
 
     // A = (n diag(beta))^T: row j, columns i > j
-    float* const fa = reinterpret_cast<float*>(sm.x);           // two blocks on the diagonal
-    float* const fu = reinterpret_cast<float*>(sm.x + 32768);   // the same of U
+    float* const fa = reinterpret_cast<float*>(sm.x);          // two blocks on the diagonal; below its diagonal what a merge has in brackets
+    float* const fu = reinterpret_cast<float*>(sm.x + 32768);  // the same of U
     const float2 own = sm.gates.sum[row];
-    if (half >= (q >> 1)) {
-      const float bt = sm.gates.beta[row];
-      float x[64];
-      load_acc(R + mine + half * 64, half32(x, 0));
-      load_acc(R + mine + half * 64 + 32, half32(x, 1));
-#pragma unroll
-      for (int c = 0; c < 64; ++c) {
-        const int i = half * 64 + c;
-        x[c] = i > row ? x[c] * decay2(sm.gates.sum[i], own) * bt : 0.f;
-      }
-      if (half == (q >> 1)) {
-#pragma unroll
-        for (int c = 0; c < 64; c += 4)
-          *reinterpret_cast<float4*>(fa + half * 4096 + block_at(row & 63, c)) = make_float4(x[c], x[c + 1], x[c + 2], x[c + 3]);
-      } else {  // A12, in place of its scores
-        store_operand(R + mine + 64, R + mine + 96, half32(x, 0));
-        store_operand(R + mine + 80, R + mine + 112, half32(x, 1));
-      }
-    }
-    // P = scale ((Q K^T) (.) D) diag(beta): row i, columns m <= i, an A operand in place of its scores
+    const float bt = sm.gates.beta[row];
     {
-      float x[64];
-      load_acc(P + mine + half * 64, half32(x, 0));
-      load_acc(P + mine + half * 64 + 32, half32(x, 1));
-      if (half <= (q >> 1)) {
+      float x[32];
+      uint32_t h[16], l[16];
+      const bool on_diagonal = (w4 >> 1) == (q >> 1), corner = q < 2 && w4 >= 2;
+      if (w4 >= q) {
+        load_acc(R + mine + c0, x);
+        if (w4 > q) {
+          const float f = bt * decay2(sm.gates.sum[c0], own);
 #pragma unroll
-        for (int c = 0; c < 64; ++c) {
-          const int m = half * 64 + c;
-          x[c] = m <= row ? x[c] * (decay2(own, sm.gates.sum[m]) * (a.scale * sm.gates.beta[m])) : 0.f;
+          for (int c = 0; c < 32; ++c) x[c] *= f * sm.gates.from_first[c0 + c];
+        } else {
+#pragma unroll
+          for (int c = 0; c < 32; ++c) x[c] = c > lane ? x[c] * (decay2(sm.gates.sum[c0 + c], own) * bt) : 0.f;
         }
-      } else {
+      }
+      if (on_diagonal) {
 #pragma unroll
-        for (int c = 0; c < 64; ++c) x[c] = 0.f;
+        for (int c = 0; c < 32; c += 4) {
+          const int at = (q >> 1) * 4096 + block_at(row & 63, (c0 & 63) + c);
+          if (w4 >= q) *reinterpret_cast<float4*>(fa + at) = make_float4(x[c], x[c + 1], x[c + 2], x[c + 3]);
+          *reinterpret_cast<float4*>(fu + at) = make_float4(0.f, 0.f, 0.f, 0.f);
+        }
+      } else if (corner) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) split2(f2_pack(x[2 * i], x[2 * i + 1]), h[i], l[i]);
       }
       tc_fence_before_sync();
-      __syncthreads();  // (the other half's columns are read; and A is written)
+      __syncthreads();  // (the scores are read)
       tc_fence_after_sync();
-      store_operand(P + mine + half * 32, P + mine + 64 + half * 32, half32(x, 0));
-      store_operand(P + mine + half * 32 + 16, P + mine + 64 + half * 32 + 16, half32(x, 1));
+      if (corner) {  // A12, an A operand of lanes 0 .. 63
+        tmem_st_x16(R + mine + 64 + (w4 - 2) * 16, h);
+        tmem_st_x16(R + mine + 96 + (w4 - 2) * 16, l);
+      }
     }
-    if (warp < 4) {  // blocks of 32: column `lane` of the inverse, from the diagonal upwards
-      const float* const blk = fa + (warp >> 1) * 4096;
-      const int o = (warp & 1) * 32;
-      float x[32];
+    {  // P = scale ((Q K^T) (.) D) diag(beta), row i, columns m <= i, as an A operand in place of its scores
+      uint32_t h[16], l[16];
+      if (w4 <= q) {
+        float x[32];
+        load_acc(P + mine + c0, x);
+        if (w4 < q) {
+          const float f = a.scale * decay2(own, sm.gates.sum[c0 + 31]);
 #pragma unroll
-      for (int i = 31; i >= 0; --i) {
-        float v[4] = {i == lane ? 1.f : 0.f, 0.f, 0.f, 0.f};
+          for (int c = 0; c < 32; ++c) x[c] *= f * sm.gates.to_last[c0 + c];
+        } else {
 #pragma unroll
-        for (int m4 = (i + 1) / 4 * 4; m4 < 32; m4 += 4) {
+          for (int c = 0; c < 32; ++c) x[c] = c <= lane ? x[c] * (decay2(own, sm.gates.sum[c0 + c]) * (a.scale * sm.gates.beta[c0 + c])) : 0.f;
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) split2(f2_pack(x[2 * i], x[2 * i + 1]), h[i], l[i]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) h[i] = l[i] = 0u;
+      }
+      tc_fence_before_sync();
+      __syncthreads();
+      tc_fence_after_sync();
+      tmem_st_x16(P + mine + w4 * 16, h);
+      tmem_st_x16(P + mine + 64 + w4 * 16, l);
+    }
+    if (warp < 8) {  // blocks of 16, one to a warp: column lane % 16 of the inverse, from the diagonal upwards
+      const int o = (warp & 3) * 16, col = lane & 15;
+      const float* const blk = fa + (warp >> 2) * 4096;
+      float* const to = fu + (warp >> 2) * 4096;
+      float x[16];
+#pragma unroll
+      for (int i = 15; i >= 0; --i) {
+        float v[4] = {i == col ? 1.f : 0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int m4 = (i + 1) / 4 * 4; m4 < 16; m4 += 4) {
           const float4 w = *reinterpret_cast<const float4*>(blk + block_at(o + i, o + m4));
           if (m4 + 0 > i) v[0] = fmaf(-w.x, x[m4 + 0], v[0]);
           if (m4 + 1 > i) v[1] = fmaf(-w.y, x[m4 + 1], v[1]);
@@ -327,61 +387,54 @@ x_prepare_kernel(const __grid_constant__ XMaps maps, const __grid_constant__ Del
           if (m4 + 3 > i) v[3] = fmaf(-w.w, x[m4 + 3], v[3]);
         }
         x[i] = (v[0] + v[1]) + (v[2] + v[3]);
-        fu[(warp >> 1) * 4096 + block_at(o + i, o + lane)] = x[i];
+        if (lane < 16) to[block_at(o + i, o + col)] = x[i];
       }
     }
     __syncthreads();
-    {  // blocks of 64: the upper right quarter is -U11 (A12 U22); the lower left one holds what is in brackets
-      const float* const fab = fa + (tid >> 7) * 4096;
-      float* const fub = fu + (tid >> 7) * 4096;
-      const int r = (tid & 127) >> 2, c0 = (tid & 3) * 8;
-#pragma unroll
+    // blocks of 32, then of 64: the upper right quarter is -U11 (A12 U22), two rows and four columns to a thread
+#pragma unroll 1
+    for (int s = 16; s <= 32; s *= 2) {
+      const int tb = s == 16 ? 5 : 7;  // threads of a merge: 2^tb
+      const int mi = tid >> tb, o = s == 16 ? (mi & 1) * 32 : 0, b = (s == 16 ? mi >> 1 : mi) & 1;
+      const int r = ((tid & ((1 << tb) - 1)) >> (s == 16 ? 2 : 3)) * 2, c = (tid & (s == 16 ? 3 : 7)) * 4;
+#pragma unroll 1
       for (int step = 0; step < 2; ++step) {
-        float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-#pragma unroll 2
-        for (int m = 0; m < 32; m += 4) {
-          const float4 w = *reinterpret_cast<const float4*>(step == 0 ? fab + block_at(r, 32 + m) : fub + block_at(r, m));
-          const float ww[4] = {w.x, w.y, w.z, w.w};
+        const float* const left = (step == 0 ? fa : fu) + b * 4096;
+        const float* right = (step == 0 ? fu : fa) + b * 4096 + (o + s) * 64;
+        float* const to = (step == 0 ? fa : fu) + b * 4096;
+        const int lc = o + (step == 0 ? s : 0), rc = (lc + c) >> 2;
+        if (tid < (s == 32 ? 256 : 128)) {
+          float4 v = make_float4(0.f, 0.f, 0.f, 0.f), u = v;
+#pragma unroll 1
+          for (int m = 0; m < s; m += 16, right += 1024) {
 #pragma unroll
-          for (int x = 0; x < 4; ++x) {
-            const int at = step == 0 ? 32 : 0;
-            const float4 b0 = *reinterpret_cast<const float4*>(fub + block_at(32 + m + x, at + c0));
-            const float4 b1 = *reinterpret_cast<const float4*>(fub + block_at(32 + m + x, at + c0 + 4));
-            v[0] = fmaf(ww[x], b0.x, v[0]); v[1] = fmaf(ww[x], b0.y, v[1]); v[2] = fmaf(ww[x], b0.z, v[2]); v[3] = fmaf(ww[x], b0.w, v[3]);
-            v[4] = fmaf(ww[x], b1.x, v[4]); v[5] = fmaf(ww[x], b1.y, v[5]); v[6] = fmaf(ww[x], b1.z, v[6]); v[7] = fmaf(ww[x], b1.w, v[7]);
+            for (int x = 0; x < 16; x += 4) {
+              const float4 w0 = *reinterpret_cast<const float4*>(left + block_at(o + r, lc + m + x));
+              const float4 w1 = *reinterpret_cast<const float4*>(left + block_at(o + r + 1, lc + m + x));
+              const float a0[4] = {w0.x, w0.y, w0.z, w0.w}, a1[4] = {w1.x, w1.y, w1.z, w1.w};
+#pragma unroll
+              for (int k = 0; k < 4; ++k) {
+                const float4 y = *reinterpret_cast<const float4*>(right + (x + k) * 64 + (((rc ^ (x + k)) & 15) << 2));
+                v.x = fmaf(a0[k], y.x, v.x); v.y = fmaf(a0[k], y.y, v.y); v.z = fmaf(a0[k], y.z, v.z); v.w = fmaf(a0[k], y.w, v.w);
+                u.x = fmaf(a1[k], y.x, u.x); u.y = fmaf(a1[k], y.y, u.y); u.z = fmaf(a1[k], y.z, u.z); u.w = fmaf(a1[k], y.w, u.w);
+              }
+            }
           }
+          const float sign = step == 0 ? 1.f : -1.f;
+          const int tr = o + (step == 0 ? s : 0) + r, tcol = o + (step == 0 ? 0 : s) + c;
+          *reinterpret_cast<float4*>(to + block_at(tr, tcol)) = make_float4(sign * v.x, sign * v.y, sign * v.z, sign * v.w);
+          *reinterpret_cast<float4*>(to + block_at(tr + 1, tcol)) = make_float4(sign * u.x, sign * u.y, sign * u.z, sign * u.w);
         }
-        const float sign = step == 0 ? 1.f : -1.f;
-        float* const to = fub + (step == 0 ? block_at(32 + r, c0) : block_at(r, 32 + c0));
-        float* const to4 = fub + (step == 0 ? block_at(32 + r, c0 + 4) : block_at(r, 32 + c0 + 4));
-        *reinterpret_cast<float4*>(to) = make_float4(sign * v[0], sign * v[1], sign * v[2], sign * v[3]);
-        *reinterpret_cast<float4*>(to4) = make_float4(sign * v[4], sign * v[5], sign * v[6], sign * v[7]);
         __syncthreads();
       }
     }
-    // row `row & 63` of a diagonal block of U, as it is now
-    auto block_row = [&](int blk, float (&x)[64]) {
-      const int r = row & 63;
-#pragma unroll
-      for (int c = 0; c < 64; c += 4) {
-        const float4 w = *reinterpret_cast<const float4*>(fu + blk * 4096 + block_at(r, c));
-        const bool in = c >= 32 || r < 32;
-        x[c] = in ? w.x : 0.f;
-        x[c + 1] = in ? w.y : 0.f;
-        x[c + 2] = in ? w.z : 0.f;
-        x[c + 3] = in ? w.w : 0.f;
-      }
-    };
-    // 64 x 64 operand in A's place: rows are those of the product's K
-    auto put_square = [&](const float (&x)[64]) {
-#pragma unroll
-      for (int c = 0; c < 8; ++c) {
-        uint4 h, l;
-        split8(&x[8 * c], h, l);
-        const uint32_t at = image_at(row & 63, c, 64);
-        *reinterpret_cast<uint4*>(sm.x + at) = h;
-        *reinterpret_cast<uint4*>(sm.x + 8192 + at) = l;
-      }
+    // a row of a 64 x 64 operand in A's place (rows are those of the product's K), eight values at a time
+    auto put_square = [&](int c, const float (&x)[8]) {
+      uint4 h, l;
+      split8(x, h, l);
+      const uint32_t at = image_at(row & 63, c, 64);
+      *reinterpret_cast<uint4*>(sm.x + at) = h;
+      *reinterpret_cast<uint4*>(sm.x + 8192 + at) = l;
     };
     auto square_product = [&](uint32_t hi, uint32_t lo) {  // to columns 0 .. 63 of R
       if (warp == 0) {
@@ -391,54 +444,75 @@ x_prepare_kernel(const __grid_constant__ XMaps maps, const __grid_constant__ Del
         umma_commit_if(&sm.bars[XP_MMA], go);
       }
     };
-    if (q >= 2 && half == 1) {
-      float x[64];
-      block_row(1, x);
-      put_square(x);
+    auto block8 = [&](int blk, int c, float (&x)[8]) {  // columns 8 c .. of row `row & 63` of a diagonal block of U
+      const float4 w0 = *reinterpret_cast<const float4*>(fu + blk * 4096 + block_at(row & 63, 8 * c));
+      const float4 w1 = *reinterpret_cast<const float4*>(fu + blk * 4096 + block_at(row & 63, 8 * c + 4));
+      x[0] = w0.x; x[1] = w0.y; x[2] = w0.z; x[3] = w0.w; x[4] = w1.x; x[5] = w1.y; x[6] = w1.z; x[7] = w1.w;
+    };
+    if (q >= 2) {
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        float x[8];
+        block8(1, w4 * 2 + c, x);
+        put_square(w4 * 2 + c, x);
+      }
     }
     X_HAND_OVER();
     square_product(R + 64, R + 96);  // A12 U22 (lanes 64 .. 127: whatever)
     X_WAIT(sm.bars[XP_MMA], par, 52);
     par ^= 1;
     if (q < 2) {
-      float x[64];
-      if (half == 0) {
-        load_acc(R + mine, half32(x, 0));
-        load_acc(R + mine + 32, half32(x, 1));
-        put_square(x);
-      } else {
-        block_row(0, x);
-        store_operand(R + mine + 64, R + mine + 96, half32(x, 0));
-        store_operand(R + mine + 80, R + mine + 112, half32(x, 1));
+      float y[16];
+      load_acc16(R + mine + w4 * 16, y);
+      tmem_ld_wait();
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        float x[8];
+        uint4 h, l;
+        put_square(w4 * 2 + c, *reinterpret_cast<const float(*)[8]>(&y[8 * c]));
+        block8(0, w4 * 2 + c, x);
+        split8(x, h, l);
+        tmem_st_x4(R + mine + 64 + (w4 * 2 + c) * 4, h);
+        tmem_st_x4(R + mine + 96 + (w4 * 2 + c) * 4, l);
       }
     }
     X_HAND_OVER();
     square_product(R + 64, R + 96);  // U11 (A12 U22)
     X_WAIT(sm.bars[XP_MMA], par, 53);
     par ^= 1;
-    {  // the image of U
-      float x[64];
-      if (q < 2 && half == 1) {
-        load_acc(R + mine, half32(x, 0));
-        load_acc(R + mine + 32, half32(x, 1));
+    auto put_image = [&](const uint4 (&h)[4], const uint4 (&l)[4], int r, int c, int rows, uint32_t lo) {
 #pragma unroll
-        for (int c = 0; c < 64; ++c) x[c] = -x[c];
-      } else if (q >= 2 && half == 0) {
-#pragma unroll
-        for (int c = 0; c < 64; ++c) x[c] = 0.f;
-      } else {
-        block_row(half, x);
+      for (int k = 0; k < 4; ++k) {
+        const uint32_t at = image_at(r, c + k, rows);
+        *reinterpret_cast<uint4*>(sm.x + at) = h[k];
+        *reinterpret_cast<uint4*>(sm.x + lo + at) = l[k];
       }
-      __syncthreads();  // (every block has been read)
+    };
+    uint4 h[4], l[4];
+    auto terms = [&](const float (&x)[32]) {
 #pragma unroll
-      for (int c = 0; c < 8; ++c) {
-        uint4 h, l;
-        split8(&x[8 * c], h, l);
-        const uint32_t at = image_at(row, half * 8 + c, 128);
-        *reinterpret_cast<uint4*>(sm.x + at) = h;
-        *reinterpret_cast<uint4*>(sm.x + 32768 + at) = l;
+      for (int k = 0; k < 4; ++k) split8(&x[8 * k], h[k], l[k]);
+    };
+    // the image of U, over all of its blocks once they have been read
+    if (q < 2 && w4 >= 2) {
+      float x[32];
+      load_acc(R + mine + (w4 - 2) * 32, x);
+#pragma unroll
+      for (int i = 0; i < 32; ++i) x[i] = -x[i];
+      terms(x);
+    } else if (q >= 2 && w4 < 2) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) h[k] = l[k] = make_uint4(0u, 0u, 0u, 0u);
+    } else {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        float x[8];
+        block8(q >> 1, (w4 & 1) * 4 + k, x);
+        split8(x, h[k], l[k]);
       }
     }
+    __syncthreads();
+    put_image(h, l, row, w4 * 4, 128, 32768);
     X_HAND_OVER();
     if (tid == 0) {
       bulk_store(rec + Rec::U, sm.x, 65536);
@@ -452,116 +526,98 @@ x_prepare_kernel(const __grid_constant__ XMaps maps, const __grid_constant__ Del
       if (tid == 0) tma_store_wait_read();
       __syncwarp();
     }
+    // U's columns times beta e^(G_end - G)
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      float x[8];
+      join8(h[k], l[k], x);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] *= sm.until[c0 + 8 * k + i];
+      split8(x, h[k], l[k]);
+    }
     X_WAIT(sm.bars[XP_MMA], par, 54);
     par ^= 1;
-    // X leaves as an image; U's columns take beta e^(G_end - G)
-#pragma unroll
-    for (int pc = 0; pc < 2; ++pc) {
-      float x[32];
-      load_acc(R + mine + half * 64 + pc * 32, x);
-#pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        uint4 h, l;
-        split8(&x[8 * c], h, l);
-        const uint32_t at = image_at(row, half * 8 + pc * 4 + c, 128);
-        *reinterpret_cast<uint4*>(rec + Rec::X + at) = h;
-        *reinterpret_cast<uint4*>(rec + Rec::X + 32768 + at) = l;
-      }
-    }
-#pragma unroll
-    for (int c = 0; c < 8; ++c) {
-      const uint32_t at = image_at(row, half * 8 + c, 128);
-      uint4 h = *reinterpret_cast<const uint4*>(sm.x + at), l = *reinterpret_cast<const uint4*>(sm.x + 32768 + at);
-      float x[8];
-      join8(h, l, x);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] *= sm.until[half * 64 + 8 * c + i];
-      split8(x, h, l);
-      *reinterpret_cast<uint4*>(sm.x + at) = h;
-      *reinterpret_cast<uint4*>(sm.x + 32768 + at) = l;
-    }
+    put_image(h, l, row, w4 * 4, 128, 32768);
     X_HAND_OVER();
     if (warp == 0) {  // J^T [d, j] = K^T U'^T
-      umma_group_ss<8, false, true>(R, mnmaj(sm.k), kmaj(sm.x), XHI, ID_NK, 0, go);
-      umma_group_ss<8, false, true>(R, mnmaj(sm.k), kmaj(sm.x + 32768), XHI, ID_NK, 1, go);
+      umma_group_ss<8, false, true>(P, mnmaj(sm.k), kmaj(sm.x), XHI, ID_NK, 0, go);
+      umma_group_ss<8, false, true>(P, mnmaj(sm.k), kmaj(sm.x + 32768), XHI, ID_NK, 1, go);
       umma_commit_if(&sm.bars[XP_MMA], go);
+    }
+    {  // X leaves as an image
+      float x[32];
+      load_acc(R + mine + c0, x);
+      terms(x);
     }
     X_WAIT(sm.bars[XP_MMA], par, 55);
     par ^= 1;
+    put_image(h, l, row, w4 * 4, 128, 32768);
+    X_HAND_OVER();
+    if (tid == 0) {
+      bulk_store(rec + Rec::X, sm.x, 65536);
+      tma_store_commit();
+    }
+    {  // J^T as an A operand in X's place; D = 64: lanes 64 .. 127 have J^T once more, for M, times e^G
+      float x[32];
+      load_acc(P + mine + c0, x);
+      if (D == 64 && q >= 2) {
+#pragma unroll
+        for (int c = 0; c < 32; ++c) x[c] *= sm.since[c0 + c];
+      }
+      store_operand(R + mine + w4 * 16, R + mine + 64 + w4 * 16, x);
+    }
     if (tid == 0) {  // (D = 64: [V | K])
+      tma_store_wait_read();
       uint64_t* const bar = expect(sm, XP_V, 32768);
       tma_load_4d(sm.x, &maps.v, bar, 0, blockIdx.x * 128, p.h, p.b);
       if (D == 128) tma_load_4d(sm.x + 16384, &maps.v, bar, 64, blockIdx.x * 128, p.h, p.b);
       else tma_load_4d(sm.x + 16384, &maps.k, bar, 0, blockIdx.x * 128, p.hk, p.b);
     }
-    // J^T as an A operand; D = 64: lanes 64 .. 127 have it once more, for M, times e^G
-#pragma unroll
-    for (int pc = 0; pc < 2; ++pc) {
-      float x[32];
-      load_acc(R + mine + half * 64 + pc * 32, x);
-      if (D == 64 && q >= 2) {
-#pragma unroll
-        for (int c = 0; c < 32; ++c) x[c] *= sm.since[half * 64 + pc * 32 + c];
-      }
-      store_operand(P + mine + half * 32 + pc * 16, P + mine + 64 + half * 32 + pc * 16, x);
-    }
     X_HAND_OVER();
     X_WAIT(sm.bars[XP_V], 0, 56);
     if (warp == 0) {  // N = J^T V
-      umma_group_tsd<false>(R, P, mnmaj(sm.x), XHI, ID_KN, 0, go);
-      umma_group_tsd<false>(R, P + 64, mnmaj(sm.x), XHI, ID_KN, 1, go);
+      umma_group_tsd<false>(P, R, mnmaj(sm.x), XHI, ID_KN, 0, go);
+      umma_group_tsd<false>(P, R + 64, mnmaj(sm.x), XHI, ID_KN, 1, go);
       umma_commit_if(&sm.bars[XP_MMA], go);
     }
     X_WAIT(sm.bars[XP_MMA], par, 57);
     par ^= 1;
-    const bool has_n = D == 128 || (q < 2 && half == 0), has_m = D == 128 || (q >= 2 && half == 1);
-    if (has_n) {  // column by column: a warp stores 128 consecutive bytes
-      float* const to = reinterpret_cast<float*>(rec + Rec::N) + row;
+    float* const n_to = reinterpret_cast<float*>(rec + Rec::N) + row;  // column by column: a warp stores 128 consecutive bytes
+    float x[32];
+    if (D == 128) {  // N is stored while M is made of J^T diag(e^G)
+      tmem_ld_x32(P + mine + c0, *reinterpret_cast<uint32_t(*)[32]>(&x));
 #pragma unroll
       for (int pc = 0; pc < 2; ++pc) {
-        float x[32];
-        load_acc(R + mine + half * 64 + pc * 32, x);
-#pragma unroll
-        for (int c = 0; c < 32; ++c) to[(half * 64 + pc * 32 + c) * D] = x[c];
-      }
-    }
-    if (D == 128) {  // J^T diag(e^G), and M
-#pragma unroll
-      for (int pc = 0; pc < 2; ++pc) {
-        uint32_t h[16], l[16];
-        float x[32];
-        tmem_ld_x16(P + mine + half * 32 + pc * 16, h);
-        tmem_ld_x16(P + mine + 64 + half * 32 + pc * 16, l);
+        uint32_t jh[8], jl[8];
+        tmem_ld_x8(R + mine + w4 * 16 + pc * 8, jh);
+        tmem_ld_x8(R + mine + 64 + w4 * 16 + pc * 8, jl);
         tmem_ld_wait();
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          x[2 * i] = (bf_lo(h[i]) + bf_lo(l[i])) * sm.since[half * 64 + pc * 32 + 2 * i];
-          x[2 * i + 1] = (bf_hi(h[i]) + bf_hi(l[i])) * sm.since[half * 64 + pc * 32 + 2 * i + 1];
+        for (int i = 0; i < 8; ++i) {
+          const float2 s = *reinterpret_cast<const float2*>(&sm.since[c0 + pc * 16 + 2 * i]);
+          split2(f2_pack((bf_lo(jh[i]) + bf_lo(jl[i])) * s.x, (bf_hi(jh[i]) + bf_hi(jl[i])) * s.y), jh[i], jl[i]);
         }
-        store_operand(P + mine + half * 32 + pc * 16, P + mine + 64 + half * 32 + pc * 16, x);
+        tmem_st_x8(R + mine + w4 * 16 + pc * 8, jh);
+        tmem_st_x8(R + mine + 64 + w4 * 16 + pc * 8, jl);
       }
       X_HAND_OVER();
       if (warp == 0) {
-        umma_group_tsd<false>(R, P, mnmaj(sm.k), XHI, ID_KN, 0, go);
-        umma_group_tsd<false>(R, P + 64, mnmaj(sm.k), XHI, ID_KN, 1, go);
+        umma_group_tsd<false>(P, R, mnmaj(sm.k), XHI, ID_KN, 0, go);
+        umma_group_tsd<false>(P, R + 64, mnmaj(sm.k), XHI, ID_KN, 1, go);
         umma_commit_if(&sm.bars[XP_MMA], go);
       }
+#pragma unroll
+      for (int c = 0; c < 32; ++c) n_to[(c0 + c) * D] = x[c];
       X_WAIT(sm.bars[XP_MMA], par, 58);
+    } else if (q < 2 && w4 < 2) {
+      load_acc(P + mine + c0, x);
+#pragma unroll
+      for (int c = 0; c < 32; ++c) n_to[(c0 + c) * D] = x[c];
     }
-    if (has_m) {
-#pragma unroll
-      for (int pc = 0; pc < 2; ++pc) {
-        float x[32];
-        load_acc(R + mine + half * 64 + pc * 32, x);
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          uint4 h, l;
-          split8(&x[8 * c], h, l);
-          const uint32_t at = image_at(row & (D - 1), (half * 8 + pc * 4 + c) & (D / 8 - 1), D);
-          *reinterpret_cast<uint4*>(sm.x + at) = h;
-          *reinterpret_cast<uint4*>(sm.x + D * D * 2 + at) = l;
-        }
-      }
+    if (D == 128 || (q >= 2 && w4 >= 2)) {
+      load_acc(P + mine + c0, x);
+      terms(x);
+      put_image(h, l, row & (D - 1), (w4 * 4) & (D / 8 - 1), D, D * D * 2);
     }
     X_HAND_OVER();
     if (tid == 0) {
@@ -728,21 +784,28 @@ template <int D>
 struct alignas(1024) XOutSmem {
   unsigned char qk[65536];  // q, k; then X
   unsigned char s[32768];   // [hi | lo] of the state's columns, then of the bracket
-  XGates gates;
+  XGateTable gates;
   uint64_t bars[XO_BARS];
   int armed[XO_BARS];
   uint32_t tmem_slot;
   int abort;
 };
 
-// 32 values of row (D features of T apart) as fp32, or zeros
-__device__ __forceinline__ void load_row32(const __nv_bfloat16* p, bool in, float (&x)[32]) {
+// 8 N values of a token's row as they are (or zeros), and what to do with each
+template <int N>
+__device__ __forceinline__ void load_raw32(const __nv_bfloat16* p, bool in, uint4 (&w)[N]) {
 #pragma unroll
-  for (int c = 0; c < 4; ++c) {
-    uint4 w = make_uint4(0u, 0u, 0u, 0u);
-    if (in) w = *reinterpret_cast<const uint4*>(p + 8 * c);
-    x[8 * c] = bf_lo(w.x); x[8 * c + 1] = bf_hi(w.x); x[8 * c + 2] = bf_lo(w.y); x[8 * c + 3] = bf_hi(w.y);
-    x[8 * c + 4] = bf_lo(w.z); x[8 * c + 5] = bf_hi(w.z); x[8 * c + 6] = bf_lo(w.w); x[8 * c + 7] = bf_hi(w.w);
+  for (int c = 0; c < N; ++c) {
+    w[c] = make_uint4(0u, 0u, 0u, 0u);
+    if (in) w[c] = *reinterpret_cast<const uint4*>(p + 8 * c);
+  }
+}
+template <int N, typename F>
+__device__ __forceinline__ void each32(const uint4 (&w)[N], F f) {
+#pragma unroll
+  for (int c = 0; c < N; ++c) {
+    f(8 * c, bf_lo(w[c].x)); f(8 * c + 1, bf_hi(w[c].x)); f(8 * c + 2, bf_lo(w[c].y)); f(8 * c + 3, bf_hi(w[c].y));
+    f(8 * c + 4, bf_lo(w[c].z)); f(8 * c + 5, bf_hi(w[c].z)); f(8 * c + 6, bf_lo(w[c].w)); f(8 * c + 7, bf_hi(w[c].w));
   }
 }
 template <typename T>
@@ -786,22 +849,20 @@ x_output_kernel(const __grid_constant__ XMaps maps, const __grid_constant__ Delt
     const unsigned char* const rec = static_cast<const unsigned char*>(a.ws) + p.rec * Rec::FWD;
     const uint32_t mine = (uint32_t)(q * 32) << 16;
     if (tid == 0) {
-      uint64_t* const bar = expect(sm, XO_LOAD, 2 * PANELS * 16384 + 2 * D * 128);
+      uint64_t* const bar = expect(sm, XO_LOAD, 2 * PANELS * 16384 + 2 * D * 128 + 2560);
+      bulk_load(&sm.gates, rec + Rec::GATES, 2560, bar);
       for (int x = 0; x < PANELS; ++x) tma_load_4d(sm.qk + x * 16384, &maps.q, bar, x * 64, c * 128, p.hk, p.b);
       for (int x = 0; x < PANELS; ++x) tma_load_4d(sm.qk + 32768 + x * 16384, &maps.k, bar, x * 64, c * 128, p.hk, p.b);
       bulk_load(sm.s, rec + Rec::S + eh * D * 128, D * 128, bar);
       bulk_load(sm.s + D * 128, rec + Rec::S + D * D * 2 + eh * D * 128, D * 128, bar);
     }
-    float v[32];
-    load_row32(static_cast<const __nv_bfloat16*>(a.v) + p.row + row * a.sT + eh * 64 + half * 32, row < p.n, v);
-    float2 end;
-    load_gates2(sm.gates, a, p.gate, p.n, tid, end);
-    __syncthreads();
-    const float since = ex2_approx(sm.gates.sum[row].x + sm.gates.sum[row].y);
+    uint4 raw[4];
+    load_raw32(static_cast<const __nv_bfloat16*>(a.v) + p.row + row * a.sT + eh * 64 + half * 32, row < p.n, raw);
     __syncwarp();
     const uint32_t go = warp == 0 ? elect_one() : 0;
     constexpr uint32_t ID2 = umma_idesc_bf16(128, 128, false, true), ID1 = umma_idesc_bf16(128, 64, false, true);
     X_WAIT(sm.bars[XO_LOAD], 0, 70);
+    const float since = ex2_approx(sm.gates.sum[row].x + sm.gates.sum[row].y);
     if (warp == 0) {
       umma_group_ss<NK, true, false>(tmem, kmaj(sm.qk + 32768), mnmaj(sm.s, D * 128), XHI, ID2, 0, go);
       umma_group_ss<NK, true, false>(tmem + 128, kmaj(sm.qk), mnmaj(sm.s, D * 128), XHI, ID2, 0, go);
@@ -812,8 +873,7 @@ x_output_kernel(const __grid_constant__ XMaps maps, const __grid_constant__ Delt
     {
       float x[32];
       load_both(tmem + mine + half * 32, x);
-#pragma unroll
-      for (int i = 0; i < 32; ++i) x[i] = fmaf(-since, x[i], v[i]);
+      each32(raw, [&](int i, float v) { x[i] = fmaf(-since, x[i], v); });
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         uint4 h, l;
@@ -830,6 +890,7 @@ x_output_kernel(const __grid_constant__ XMaps maps, const __grid_constant__ Delt
       umma_group_ss<8, true, false>(tmem, kmaj(sm.qk + 32768), mnmaj(sm.s), XHI, ID1, 1, go);
       umma_commit_if(&sm.bars[XO_MMA], go);
     }
+    float v[32];
     load_both(tmem + 128 + mine + half * 32, v);
 #pragma unroll
     for (int i = 0; i < 32; ++i) v[i] *= a.scale * since;
@@ -851,7 +912,7 @@ template <int D>
 struct alignas(1024) XAdjSmem {
   unsigned char x[65536];   // X; then q, k (D = 64: and the lo terms of the B operand)
   unsigned char t[32768];   // dO in the second half; the B operand [hi | lo] (D = 64: its hi terms)
-  XGates gates;
+  XGateTable gates;
   uint64_t bars[XA_BARS];
   int armed[XA_BARS];
   uint32_t tmem_slot;
@@ -873,18 +934,16 @@ x_adjoint_kernel(const __grid_constant__ XMaps maps, const __grid_constant__ Del
     unsigned char* const bwd = static_cast<unsigned char*>(a.ws_bwd) + p.rec * Rec::BWD;
     const uint32_t mine = (uint32_t)(q * 32) << 16, R = tmem + 128;
     if (tid == 0) {
-      uint64_t* const bar = expect(sm, XA_LOAD, 65536 + 16384);
+      uint64_t* const bar = expect(sm, XA_LOAD, 65536 + 16384 + 2560);
+      bulk_load(&sm.gates, fwd + Rec::GATES, 2560, bar);
       bulk_load(sm.x, fwd + Rec::X, 65536, bar);
       tma_load_4d(sm.t + 16384, &maps.d_o, bar, eh * 64, c * 128, p.h, p.b);
     }
-    float2 end;
-    load_gates2(sm.gates, a, p.gate, p.n, tid, end);
-    __syncthreads();
-    const float since = ex2_approx(sm.gates.sum[row].x + sm.gates.sum[row].y);
     __syncwarp();
     const uint32_t go = warp == 0 ? elect_one() : 0;
     constexpr uint32_t ID1 = umma_idesc_bf16(128, 64, true, true), ID2 = umma_idesc_bf16(128, 128, true, true);
     X_WAIT(sm.bars[XA_LOAD], 0, 80);
+    const float since = ex2_approx(sm.gates.sum[row].x + sm.gates.sum[row].y);
     if (warp == 0) {
       umma_group_ss<8, false, false>(tmem, mnmaj(sm.x), mnmaj(sm.t + 16384), XHI, ID1, 0, go);
       umma_group_ss<8, false, false>(tmem, mnmaj(sm.x + 32768), mnmaj(sm.t + 16384), XHI, ID1, 1, go);
@@ -976,7 +1035,7 @@ template <int D>
 struct alignas(1024) XValSmem {
   unsigned char u[65536];  // k; then U
   unsigned char s[32768];  // [hi | lo] of the state's columns, of the bracket, of the result
-  XGates gates;
+  XGateTable gates;
   uint64_t bars[XV_BARS];
   int armed[XV_BARS];
   uint32_t tmem_slot;
@@ -999,30 +1058,31 @@ x_values_kernel(const __grid_constant__ XMaps maps, const __grid_constant__ Delt
     unsigned char* const bwd = static_cast<unsigned char*>(a.ws_bwd) + p.rec * Rec::BWD;
     const uint32_t mine = (uint32_t)(q * 32) << 16;
     if (tid == 0) {
-      uint64_t* const bar = expect(sm, XV_LOAD, PANELS * 16384 + 2 * D * 128);
+      uint64_t* const bar = expect(sm, XV_LOAD, PANELS * 16384 + 2 * D * 128 + 2560);
+      bulk_load(&sm.gates, fwd + Rec::GATES, 2560, bar);
       for (int x = 0; x < PANELS; ++x) tma_load_4d(sm.u + x * 16384, &maps.k, bar, x * 64, c * 128, p.hk, p.b);
       const unsigned char* const state = grad ? bwd + Rec::E : fwd + Rec::S;
       bulk_load(sm.s, state + eh * D * 128, D * 128, bar);
       bulk_load(sm.s + D * 128, state + D * D * 2 + eh * D * 128, D * 128, bar);
     }
+    const float2 end = *reinterpret_cast<const float2*>(fwd + Rec::END);
     float add[32];
     if (grad) {
       const float* const z = reinterpret_cast<const float*>(bwd + Rec::Z) + (size_t)(eh * 64 + half * 32) * 128 + row;
 #pragma unroll
       for (int i = 0; i < 32; ++i) add[i] = ld_f1(z + i * 128);
     } else {
-      load_row32(static_cast<const __nv_bfloat16*>(a.v) + p.row + row * a.sT + eh * 64 + half * 32, row < p.n, add);
+      uint4 raw[4];
+      load_raw32(static_cast<const __nv_bfloat16*>(a.v) + p.row + row * a.sT + eh * 64 + half * 32, row < p.n, raw);
+      each32(raw, [&](int i, float v) { add[i] = v; });
     }
-    float2 end;
-    load_gates2(sm.gates, a, p.gate, p.n, tid, end);
-    __syncthreads();
-    const float2 own = sm.gates.sum[row];
-    const float times = grad ? sm.gates.beta[row] * decay2(end, own) : -ex2_approx(own.x + own.y);
     __syncwarp();
     const uint32_t go = warp == 0 ? elect_one() : 0;
     constexpr uint32_t ID2 = umma_idesc_bf16(128, 128, false, true), ID1 = umma_idesc_bf16(128, 64, false, true);
     constexpr uint32_t ID2T = umma_idesc_bf16(128, 128, true, true), ID1T = umma_idesc_bf16(128, 64, true, true);
     X_WAIT(sm.bars[XV_LOAD], 0, 90);
+    const float2 own = sm.gates.sum[row];
+    const float times = grad ? sm.gates.beta[row] * decay2(end, own) : -ex2_approx(own.x + own.y);
     if (warp == 0) {
       umma_group_ss<NK, true, false>(tmem, kmaj(sm.u), mnmaj(sm.s, D * 128), XHI, ID2, 0, go);
       umma_commit_if(&sm.bars[XV_MMA], go);
@@ -1150,8 +1210,6 @@ __device__ __forceinline__ void load_row16(const __nv_bfloat16* p, bool in, floa
     x[8 * c + 4] = bf_lo(w.z); x[8 * c + 5] = bf_hi(w.z); x[8 * c + 6] = bf_lo(w.w); x[8 * c + 7] = bf_hi(w.w);
   }
 }
-__device__ __forceinline__ void load_acc16(uint32_t taddr, float (&x)[16]) { tmem_ld_x16(taddr, *reinterpret_cast<uint32_t(*)[16]>(&x)); }
-
 template <int D, typename TO>
 __global__ void __launch_bounds__(512, 1)
 x_gradient_kernel(const __grid_constant__ XMaps maps, const __grid_constant__ DeltaArgs a) {
@@ -1189,14 +1247,12 @@ x_gradient_kernel(const __grid_constant__ XMaps maps, const __grid_constant__ De
         bulk_load(sm.y, bwd + Rec::Y, 2 * TOK, bar);
       }
       // gates: the sums stay in shared memory, the rest in registers
-      float2 end;
-      XGates& gates = *reinterpret_cast<XGates*>(sm.s);
-      load_gates2(gates, a, p.gate, p.n, tid, end);
-      __syncthreads();
+      const XGateTable& gates = *reinterpret_cast<const XGateTable*>(fwd + Rec::GATES);
+      const float2 end = *reinterpret_cast<const float2*>(fwd + Rec::END);
       const float2 own = gates.sum[row];
       const float beta_row = gates.beta[row], since = ex2_approx(own.x + own.y), until = decay2(end, own), all = ex2_approx(end.x + end.y);
       if (tid < 128) sm.sum[tid] = gates.sum[tid];
-      float beta_tid = tid < 128 ? gates.beta[tid] : 0.f;
+      const float beta_tid = tid < 128 ? gates.beta[tid] : 0.f, bcol = gates.beta[c0 + lane];
       X_WAIT(sm.bars[XG_QK], 0, 100);
       X_WAIT(sm.bars[XG_Y], second, 101);
       if (warp == 0) {
@@ -1218,8 +1274,6 @@ x_gradient_kernel(const __grid_constant__ XMaps maps, const __grid_constant__ De
         umma_group_ss<NK, true, true>(T3, kmaj(sm.a + TOK), kmaj(sm.y), XHI, ID_SC, 1, go);
         umma_commit_if(&sm.bars[XG_MMA], go);
       }
-      // beta of this thread's columns is read from the gates before the state comes over them
-      float bcol = gates.beta[c0 + lane];
       X_WAIT(sm.bars[XG_MMA], mma, 104);
       mma ^= 1;
       if (tid == 0) bulk_load(sm.s, fwd + Rec::S, D * D * 2, expect(sm, XG_SH, D * D * 2));
@@ -1486,7 +1540,7 @@ cudaError_t x_chain(const DeltaArgs& d, cudaStream_t stream) {
 
 template <int D>
 cudaError_t x_states(const XMaps& m, const DeltaArgs& a, cudaStream_t stream) {
-  const cudaError_t err = x_launch<XPrepSmem<D>>(x_prepare_kernel<D>, K_PREPASS, dim3(a.nchunk, a.B * a.H), 256, stream, m, a);
+  const cudaError_t err = x_launch<XPrepSmem<D>>(x_prepare_kernel<D>, K_PREPASS, dim3(a.nchunk, a.B * a.H), 512, stream, m, a);
   return err != cudaSuccess ? err : x_chain<D, false>(a, stream);
 }
 
