@@ -37,7 +37,8 @@ struct XRec {
 };
 
 struct XMaps {
-  CUtensorMap q, k, v, d_o;
+  CUtensorMap q, k, v, d_o;    // boxes of 64 features x 128 tokens
+  CUtensorMap o, dq, dk, dv;   // results: boxes of 128 bytes x 128 tokens; tokens behind the last one are not written
 };
 
 __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
@@ -47,6 +48,9 @@ __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t b
 }
 __device__ __forceinline__ void bulk_store(void* dst, const void* src, uint32_t bytes) {
   asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(dst), "r"(smem_u32(src)), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void prefetch(const void* src, uint32_t bytes) {  // to L2
+  asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(src), "r"(bytes) : "memory");
 }
 __device__ __forceinline__ void bulk_store_done() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
 
@@ -89,8 +93,8 @@ __device__ __forceinline__ void store_operand(uint32_t hi, uint32_t lo, const fl
 // exponential of its own.
 struct alignas(16) XGateTable {
   float2 sum[128];
+  float to_last[128];     // decay from j to the last token of its block of 32
   float beta[128];
-  float to_last[128];     // beta_j times the decay from j to the last token of its block of 32
   float from_first[128];  // decay from the first token of i's block of 32 to i
 };
 static_assert(sizeof(XGateTable) == 2560, "as the workspace has it");
@@ -119,7 +123,7 @@ __device__ __forceinline__ void make_gates(XGateTable& s, double* part, unsigned
     const float2 own = two_terms(x);
     const float2 last = make_float2(__shfl_sync(0xffffffffu, own.x, 31), __shfl_sync(0xffffffffu, own.y, 31));
     const float2 first = make_float2(__shfl_sync(0xffffffffu, own.x, 0), __shfl_sync(0xffffffffu, own.y, 0));
-    const float to_last = beta * decay2(last, own), from_first = decay2(own, first);
+    const float to_last = decay2(last, own), from_first = decay2(own, first);
     s.sum[tid] = own;
     s.beta[tid] = beta;
     s.to_last[tid] = to_last;
@@ -151,6 +155,15 @@ __device__ __forceinline__ XPlace x_place(const DeltaArgs& a, int bh, int c) {
   p.gate = p.b * a.gB + p.h * a.gH + (long long)c * 128 * a.gT;
   p.rec = (size_t)bh * a.nchunk + c;
   return p;
+}
+
+// The thread block `ahead` places after this one: what it will load is fetched to L2 while this one computes, so that HBM is busy all the
+// time and not only while blocks begin.  (false: there is none)
+__device__ __forceinline__ bool later_block(unsigned ahead, unsigned& x, unsigned& y) {
+  const unsigned n = blockIdx.x + ahead;
+  x = n % gridDim.x;
+  y = blockIdx.y + n / gridDim.x;
+  return y < gridDim.y;
 }
 
 // One warp looks, the others stand at the block's barrier: sixteen that look take the instruction slots of the thread block beside them
@@ -233,12 +246,12 @@ __device__ __forceinline__ uint32_t mnmaj(const void* p, uint32_t panel = 16384)
 // products run beside the other's conversions.  Thread (q, lane) of quarter w has row q * 32 + lane of every accumulator and of every
 // image, columns w * 32 .. + 31: one block of 32 tokens.
 //
-// The inverse U of the upper triangular I + (n diag(beta))^T, in fp32 as far as the CUDA cores make it: columns of the eight diagonal
-// blocks of 16 by back substitution (a warp each), then U12 = -U11 A12 U22 for the blocks of 32 and of 64, then the same once more on
-// the tensor cores for the whole.  Powers of the triangle would need no order of rows, but grow far beyond the inverse where keys are
+// The inverse U of the upper triangular I + (n diag(beta))^T: columns of the four diagonal blocks of 32 by back substitution in fp32 (a
+// warp each), then U12 = -U11 A12 U22 on the tensor cores for the two blocks of 64 at once, then for the whole.  (On the CUDA cores the
+// step from 16 to 64 took 11000 clocks with two thread blocks to an SM.)  Powers of the triangle would need no order of rows, but grow far beyond the inverse where keys are
 // alike.
 //
-// What it costs is the latency of its eleven dependent steps, of which seven wait for a product, and the instructions between them: with
+// What it costs is the latency of its dependent steps, of which nine wait for a product, and the instructions between them: with
 // 256 threads to a block and all loops unrolled it was 100 KB of instructions, each executed once and fetched for it, and took 68 us
 // a chunk and SM; with decays as products of factors and most loops left as loops 18; with 512 threads see the table of measurements.
 enum { XP_LOAD = 0, XP_V, XP_MMA, XP_DRAIN, XP_BARS };
@@ -249,6 +262,7 @@ struct alignas(1024) XPrepSmem {
   XGateTable gates;
   float until[128];        // beta e^(G_end - G)
   float since[128];        // e^G
+  float last_beta[128];    // gates.to_last times beta
   double part[4];
   uint64_t bars[XP_BARS];
   int armed[XP_BARS];
@@ -256,8 +270,8 @@ struct alignas(1024) XPrepSmem {
   int abort;
 };
 
-// element (i, m) of a 64 x 64 fp32 block whose 16-byte groups are permuted by row, so that a thread per row stores without conflicts
-__device__ __forceinline__ int block_at(int i, int m) { return i * 64 + ((((m >> 2) ^ i) & 15) << 2) + (m & 3); }
+// element (i, m) of a 32 x 32 fp32 block whose 16-byte groups are permuted by row, so that a thread per row stores without conflicts
+__device__ __forceinline__ int block_at(int i, int m) { return i * 32 + ((((m >> 2) ^ i) & 7) << 2) + (m & 3); }
 
 template <int D>
 __global__ void __launch_bounds__(512, 2)
@@ -288,9 +302,10 @@ x_prepare_kernel(const __grid_constant__ XMaps maps, const __grid_constant__ Del
       const float2 s = sm.gates.sum[tid];
       sm.since[tid] = ex2_approx(s.x + s.y);
       sm.until[tid] = beta_own * decay2(end, s);
+      sm.last_beta[tid] = beta_own * sm.gates.to_last[tid];
     }
     constexpr uint32_t ID_KK = umma_idesc_bf16(128, 128, false, false);
-    constexpr uint32_t ID_KN64 = umma_idesc_bf16(128, 64, false, true);
+    constexpr uint32_t ID_KN64 = umma_idesc_bf16(128, 64, false, true), ID_KN32 = umma_idesc_bf16(128, 32, false, true);
     constexpr uint32_t ID_KN = umma_idesc_bf16(128, 128, false, true);
     constexpr uint32_t ID_NK = umma_idesc_bf16(128, 128, true, false);
     constexpr int NK = D / 16;
@@ -306,128 +321,165 @@ x_prepare_kernel(const __grid_constant__ XMaps maps, const __grid_constant__ Del
     X_WAIT(sm.bars[XP_MMA], par, 51);
     par ^= 1;
 
-    // A = (n diag(beta))^T: row j, columns i > j
-    float* const fa = reinterpret_cast<float*>(sm.x);          // two blocks on the diagonal; below its diagonal what a merge has in brackets
-    float* const fu = reinterpret_cast<float*>(sm.x + 32768);  // the same of U
+    // A = (n diag(beta))^T: row j, columns i > j.  Shared memory by turns: blocks of 32 on A's and on U's diagonal, U's blocks beside them,
+    // and a B operand of two times 32 rows.
+    float* const fa = reinterpret_cast<float*>(sm.x);
+    float* const fu = reinterpret_cast<float*>(sm.x + 16384);
+    float* const fu12 = reinterpret_cast<float*>(sm.x + 32768);
+    unsigned char* const pair = sm.x + 40960;
     const float2 own = sm.gates.sum[row];
     const float bt = sm.gates.beta[row];
-    {
+    // A's columns of this thread where they are of a later block of 32: one factor for the row, one for each column
+    auto later_columns = [&](uint32_t(&h)[16], uint32_t(&l)[16]) {
       float x[32];
-      uint32_t h[16], l[16];
-      const bool on_diagonal = (w4 >> 1) == (q >> 1), corner = q < 2 && w4 >= 2;
-      if (w4 >= q) {
-        load_acc(R + mine + c0, x);
-        if (w4 > q) {
-          const float f = bt * decay2(sm.gates.sum[c0], own);
+      load_acc(R + mine + c0, x);
+      const float f = bt * decay2(sm.gates.sum[c0], own);
+      const uint64_t ff = f2_pack(f, f);
 #pragma unroll
-          for (int c = 0; c < 32; ++c) x[c] *= f * sm.gates.from_first[c0 + c];
-        } else {
-#pragma unroll
-          for (int c = 0; c < 32; ++c) x[c] = c > lane ? x[c] * (decay2(sm.gates.sum[c0 + c], own) * bt) : 0.f;
-        }
+      for (int i = 0; i < 16; ++i) {
+        const float2 d = *reinterpret_cast<const float2*>(&sm.gates.from_first[c0 + 2 * i]);
+        split2(f2_mul(f2_mul(f2_pack(d.x, d.y), ff), f2_pack(x[2 * i], x[2 * i + 1])), h[i], l[i]);
       }
-      if (on_diagonal) {
+    };
+    {
+      uint32_t h[16], l[16];
+      const bool corner = q < 2 && w4 >= 2;
+      if (w4 == q) {
+        float x[32];
+        load_acc(R + mine + c0, x);
 #pragma unroll
-        for (int c = 0; c < 32; c += 4) {
-          const int at = (q >> 1) * 4096 + block_at(row & 63, (c0 & 63) + c);
-          if (w4 >= q) *reinterpret_cast<float4*>(fa + at) = make_float4(x[c], x[c + 1], x[c + 2], x[c + 3]);
-          *reinterpret_cast<float4*>(fu + at) = make_float4(0.f, 0.f, 0.f, 0.f);
-        }
+        for (int c = 0; c < 32; ++c) x[c] = c > lane ? x[c] * (decay2(sm.gates.sum[c0 + c], own) * bt) : 0.f;
+#pragma unroll
+        for (int c = 0; c < 32; c += 4)
+          *reinterpret_cast<float4*>(fa + q * 1024 + block_at(lane, c)) = make_float4(x[c], x[c + 1], x[c + 2], x[c + 3]);
       } else if (corner) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) split2(f2_pack(x[2 * i], x[2 * i + 1]), h[i], l[i]);
+        later_columns(h, l);
       }
       tc_fence_before_sync();
       __syncthreads();  // (the scores are read)
       tc_fence_after_sync();
-      if (corner) {  // A12, an A operand of lanes 0 .. 63
+      if (corner) {  // the corner of 64 x 64, an A operand of lanes 0 .. 63
         tmem_st_x16(R + mine + 64 + (w4 - 2) * 16, h);
         tmem_st_x16(R + mine + 96 + (w4 - 2) * 16, l);
       }
     }
     {  // P = scale ((Q K^T) (.) D) diag(beta), row i, columns m <= i, as an A operand in place of its scores
       uint32_t h[16], l[16];
-      if (w4 <= q) {
+      if (w4 < q) {
         float x[32];
         load_acc(P + mine + c0, x);
-        if (w4 < q) {
-          const float f = a.scale * decay2(own, sm.gates.sum[c0 + 31]);
+        const float f = a.scale * decay2(own, sm.gates.sum[c0 + 31]);
+        const uint64_t ff = f2_pack(f, f);
 #pragma unroll
-          for (int c = 0; c < 32; ++c) x[c] *= f * sm.gates.to_last[c0 + c];
-        } else {
-#pragma unroll
-          for (int c = 0; c < 32; ++c) x[c] = c <= lane ? x[c] * (decay2(own, sm.gates.sum[c0 + c]) * (a.scale * sm.gates.beta[c0 + c])) : 0.f;
+        for (int i = 0; i < 16; ++i) {
+          const float2 d = *reinterpret_cast<const float2*>(&sm.last_beta[c0 + 2 * i]);
+          split2(f2_mul(f2_mul(f2_pack(d.x, d.y), ff), f2_pack(x[2 * i], x[2 * i + 1])), h[i], l[i]);
         }
+      } else if (w4 == q) {
+        float x[32];
+        load_acc(P + mine + c0, x);
+#pragma unroll
+        for (int c = 0; c < 32; ++c) x[c] = c <= lane ? x[c] * (decay2(own, sm.gates.sum[c0 + c]) * (a.scale * sm.gates.beta[c0 + c])) : 0.f;
 #pragma unroll
         for (int i = 0; i < 16; ++i) split2(f2_pack(x[2 * i], x[2 * i + 1]), h[i], l[i]);
       } else {
 #pragma unroll
         for (int i = 0; i < 16; ++i) h[i] = l[i] = 0u;
       }
+      // The corner of 32 x 32 of the blocks of 64, lanes 0 .. 31 and 64 .. 95, lies for a while where P is zero in those rows
+      const bool small = (q == 0 && w4 == 1) || (q == 2 && w4 == 3);
       tc_fence_before_sync();
       __syncthreads();
       tc_fence_after_sync();
-      tmem_st_x16(P + mine + w4 * 16, h);
-      tmem_st_x16(P + mine + 64 + w4 * 16, l);
+      if (!(w4 == 3 && (q & 1) == 0)) {
+        tmem_st_x16(P + mine + w4 * 16, h);
+        tmem_st_x16(P + mine + 64 + w4 * 16, l);
+      }
+      if (small) {
+        later_columns(h, l);
+        tmem_st_x16(P + mine + 48, h);
+        tmem_st_x16(P + mine + 112, l);
+      }
     }
-    if (warp < 8) {  // blocks of 16, one to a warp: column lane % 16 of the inverse, from the diagonal upwards
-      const int o = (warp & 3) * 16, col = lane & 15;
-      const float* const blk = fa + (warp >> 2) * 4096;
-      float* const to = fu + (warp >> 2) * 4096;
-      float x[16];
+    if (warp < 4) {  // blocks of 32, one to a warp: column `lane` of the inverse, from the diagonal upwards
+      const float* const blk = fa + warp * 1024;
+      float* const to = fu + warp * 1024;
+      float x[32];
 #pragma unroll
-      for (int i = 15; i >= 0; --i) {
-        float v[4] = {i == col ? 1.f : 0.f, 0.f, 0.f, 0.f};
+      for (int i = 31; i >= 0; --i) {
+        float v[4] = {i == lane ? 1.f : 0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int m4 = (i + 1) / 4 * 4; m4 < 16; m4 += 4) {
-          const float4 w = *reinterpret_cast<const float4*>(blk + block_at(o + i, o + m4));
+        for (int m4 = (i + 1) / 4 * 4; m4 < 32; m4 += 4) {
+          const float4 w = *reinterpret_cast<const float4*>(blk + block_at(i, m4));
           if (m4 + 0 > i) v[0] = fmaf(-w.x, x[m4 + 0], v[0]);
           if (m4 + 1 > i) v[1] = fmaf(-w.y, x[m4 + 1], v[1]);
           if (m4 + 2 > i) v[2] = fmaf(-w.z, x[m4 + 2], v[2]);
           if (m4 + 3 > i) v[3] = fmaf(-w.w, x[m4 + 3], v[3]);
         }
         x[i] = (v[0] + v[1]) + (v[2] + v[3]);
-        if (lane < 16) to[block_at(o + i, o + col)] = x[i];
+        to[block_at(i, lane)] = x[i];
       }
     }
     __syncthreads();
-    // blocks of 32, then of 64: the upper right quarter is -U11 (A12 U22), two rows and four columns to a thread
-#pragma unroll 1
-    for (int s = 16; s <= 32; s *= 2) {
-      const int tb = s == 16 ? 5 : 7;  // threads of a merge: 2^tb
-      const int mi = tid >> tb, o = s == 16 ? (mi & 1) * 32 : 0, b = (s == 16 ? mi >> 1 : mi) & 1;
-      const int r = ((tid & ((1 << tb) - 1)) >> (s == 16 ? 2 : 3)) * 2, c = (tid & (s == 16 ? 3 : 7)) * 4;
-#pragma unroll 1
-      for (int step = 0; step < 2; ++step) {
-        const float* const left = (step == 0 ? fa : fu) + b * 4096;
-        const float* right = (step == 0 ? fu : fa) + b * 4096 + (o + s) * 64;
-        float* const to = (step == 0 ? fa : fu) + b * 4096;
-        const int lc = o + (step == 0 ? s : 0), rc = (lc + c) >> 2;
-        if (tid < (s == 32 ? 256 : 128)) {
-          float4 v = make_float4(0.f, 0.f, 0.f, 0.f), u = v;
-#pragma unroll 1
-          for (int m = 0; m < s; m += 16, right += 1024) {
+    // blocks of 64: the corner is -U11 (A12 U22), both at once: lanes 0 .. 31 and 64 .. 95 of one A operand, a B operand for each
+    auto put_pair = [&](int b, int r, int c, const float (&x)[8]) {
+      uint4 h, l;
+      split8(x, h, l);
+      const uint32_t at = b * 4096 + image_at(r, c, 32);
+      *reinterpret_cast<uint4*>(pair + at) = h;
+      *reinterpret_cast<uint4*>(pair + 8192 + at) = l;
+    };
+    auto row8 = [&](const float* blk, int r, int c, float (&x)[8]) {
+      const float4 w0 = *reinterpret_cast<const float4*>(blk + block_at(r, 8 * c)), w1 = *reinterpret_cast<const float4*>(blk + block_at(r, 8 * c + 4));
+      x[0] = w0.x; x[1] = w0.y; x[2] = w0.z; x[3] = w0.w; x[4] = w1.x; x[5] = w1.y; x[6] = w1.z; x[7] = w1.w;
+    };
+    auto pair_product = [&]() {  // to columns 0 .. 31 and 32 .. 63 of R
+      if (warp == 0) {
 #pragma unroll
-            for (int x = 0; x < 16; x += 4) {
-              const float4 w0 = *reinterpret_cast<const float4*>(left + block_at(o + r, lc + m + x));
-              const float4 w1 = *reinterpret_cast<const float4*>(left + block_at(o + r + 1, lc + m + x));
-              const float a0[4] = {w0.x, w0.y, w0.z, w0.w}, a1[4] = {w1.x, w1.y, w1.z, w1.w};
-#pragma unroll
-              for (int k = 0; k < 4; ++k) {
-                const float4 y = *reinterpret_cast<const float4*>(right + (x + k) * 64 + (((rc ^ (x + k)) & 15) << 2));
-                v.x = fmaf(a0[k], y.x, v.x); v.y = fmaf(a0[k], y.y, v.y); v.z = fmaf(a0[k], y.z, v.z); v.w = fmaf(a0[k], y.w, v.w);
-                u.x = fmaf(a1[k], y.x, u.x); u.y = fmaf(a1[k], y.y, u.y); u.z = fmaf(a1[k], y.z, u.z); u.w = fmaf(a1[k], y.w, u.w);
-              }
-            }
-          }
-          const float sign = step == 0 ? 1.f : -1.f;
-          const int tr = o + (step == 0 ? s : 0) + r, tcol = o + (step == 0 ? 0 : s) + c;
-          *reinterpret_cast<float4*>(to + block_at(tr, tcol)) = make_float4(sign * v.x, sign * v.y, sign * v.z, sign * v.w);
-          *reinterpret_cast<float4*>(to + block_at(tr + 1, tcol)) = make_float4(sign * u.x, sign * u.y, sign * u.z, sign * u.w);
+        for (int b = 0; b < 2; ++b) {
+          umma_group_tsd2(R + 32 * b, P + 48, mnmaj(pair + b * 4096), XHI, ID_KN32, 0, go);
+          umma_group_tsd2(R + 32 * b, P + 48, mnmaj(pair + 8192 + b * 4096), XHI, ID_KN32, 1, go);
+          umma_group_tsd2(R + 32 * b, P + 112, mnmaj(pair + b * 4096), XHI, ID_KN32, 1, go);
         }
-        __syncthreads();
+        umma_commit_if(&sm.bars[XP_MMA], go);
       }
+    };
+    if (tid < 256) {
+      float x[8];
+      row8(fu + ((tid >> 7) * 2 + 1) * 1024, (tid >> 2) & 31, tid & 3, x);
+      put_pair(tid >> 7, (tid >> 2) & 31, tid & 3, x);
     }
+    X_HAND_OVER();
+    pair_product();
+    X_WAIT(sm.bars[XP_MMA], par, 59);
+    par ^= 1;
+    const bool upper = (q & 1) == 0;
+    float y8[8];
+    if (upper) {
+      float x[8];
+      uint4 h, l;
+      tmem_ld_x8(R + mine + 16 * q + w4 * 8, *reinterpret_cast<uint32_t(*)[8]>(&y8));
+      tmem_ld_wait();
+      put_pair(q >> 1, lane, w4, y8);
+      row8(fu + q * 1024, lane, w4, x);
+      split8(x, h, l);
+      tmem_st_x4(P + mine + 48 + w4 * 4, h);
+      tmem_st_x4(P + mine + 112 + w4 * 4, l);
+    }
+    X_HAND_OVER();
+    pair_product();
+    X_WAIT(sm.bars[XP_MMA], par, 60);
+    par ^= 1;
+    if (upper) {
+      tmem_ld_x8(R + mine + 16 * q + w4 * 8, *reinterpret_cast<uint32_t(*)[8]>(&y8));
+      tmem_ld_wait();
+      float* const to = fu12 + (q >> 1) * 1024;
+      *reinterpret_cast<float4*>(to + block_at(lane, 8 * w4)) = make_float4(-y8[0], -y8[1], -y8[2], -y8[3]);
+      *reinterpret_cast<float4*>(to + block_at(lane, 8 * w4 + 4)) = make_float4(-y8[4], -y8[5], -y8[6], -y8[7]);
+      tmem_st_x4(P + mine + 48 + w4 * 4, make_uint4(0u, 0u, 0u, 0u));
+      tmem_st_x4(P + mine + 112 + w4 * 4, make_uint4(0u, 0u, 0u, 0u));
+    }
+    __syncthreads();
     // a row of a 64 x 64 operand in A's place (rows are those of the product's K), eight values at a time
     auto put_square = [&](int c, const float (&x)[8]) {
       uint4 h, l;
@@ -444,10 +496,15 @@ x_prepare_kernel(const __grid_constant__ XMaps maps, const __grid_constant__ Del
         umma_commit_if(&sm.bars[XP_MMA], go);
       }
     };
-    auto block8 = [&](int blk, int c, float (&x)[8]) {  // columns 8 c .. of row `row & 63` of a diagonal block of U
-      const float4 w0 = *reinterpret_cast<const float4*>(fu + blk * 4096 + block_at(row & 63, 8 * c));
-      const float4 w1 = *reinterpret_cast<const float4*>(fu + blk * 4096 + block_at(row & 63, 8 * c + 4));
-      x[0] = w0.x; x[1] = w0.y; x[2] = w0.z; x[3] = w0.w; x[4] = w1.x; x[5] = w1.y; x[6] = w1.z; x[7] = w1.w;
+    auto block8 = [&](int blk, int c, float (&x)[8]) {  // columns 8 c .. of row `row & 63` of a diagonal block of 64 of U
+      if (c >= 4) {
+        row8(upper ? fu12 + blk * 1024 : fu + (2 * blk + 1) * 1024, lane, c - 4, x);
+      } else if (upper) {
+        row8(fu + 2 * blk * 1024, lane, c, x);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = 0.f;
+      }
     };
     if (q >= 2) {
 #pragma unroll
@@ -529,11 +586,12 @@ x_prepare_kernel(const __grid_constant__ XMaps maps, const __grid_constant__ Del
     // U's columns times beta e^(G_end - G)
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      float x[8];
-      join8(h[k], l[k], x);
+      uint32_t *const hw = &h[k].x, *const lw = &l[k].x;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] *= sm.until[c0 + 8 * k + i];
-      split8(x, h[k], l[k]);
+      for (int i = 0; i < 4; ++i) {
+        const float2 u = *reinterpret_cast<const float2*>(&sm.until[c0 + 8 * k + 2 * i]);
+        split2(f2_mul(f2_add(f2_pack(bf_lo(hw[i]), bf_hi(hw[i])), f2_pack(bf_lo(lw[i]), bf_hi(lw[i]))), f2_pack(u.x, u.y)), hw[i], lw[i]);
+      }
     }
     X_WAIT(sm.bars[XP_MMA], par, 54);
     par ^= 1;
@@ -595,7 +653,7 @@ x_prepare_kernel(const __grid_constant__ XMaps maps, const __grid_constant__ Del
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           const float2 s = *reinterpret_cast<const float2*>(&sm.since[c0 + pc * 16 + 2 * i]);
-          split2(f2_pack((bf_lo(jh[i]) + bf_lo(jl[i])) * s.x, (bf_hi(jh[i]) + bf_hi(jl[i])) * s.y), jh[i], jl[i]);
+          split2(f2_mul(f2_add(f2_pack(bf_lo(jh[i]), bf_hi(jh[i])), f2_pack(bf_lo(jl[i]), bf_hi(jl[i]))), f2_pack(s.x, s.y)), jh[i], jl[i]);
         }
         tmem_st_x8(R + mine + w4 * 16 + pc * 8, jh);
         tmem_st_x8(R + mine + 64 + w4 * 16 + pc * 8, jl);
@@ -730,7 +788,7 @@ x_chain_kernel(const __grid_constant__ XChainArgs a) {
           }
           umma_commit_if(&sm.bars[XC_MMA], go);
         } else {
-          if (!ok && !sm.abort) atomicCAS(&g_tc_status, 0u, 60u);
+          if (!ok && !sm.abort) atomicCAS(&g_tc_status, 0u, 62u);
           sm.abort = 1;
         }
       }
@@ -808,8 +866,10 @@ __device__ __forceinline__ void each32(const uint4 (&w)[N], F f) {
     f(8 * c + 4, bf_lo(w[c].z)); f(8 * c + 5, bf_hi(w[c].z)); f(8 * c + 6, bf_lo(w[c].w)); f(8 * c + 7, bf_hi(w[c].w));
   }
 }
+// 32 values of a row of a result, columns c0 .. + 31, to a tile of 128-byte rows in the swizzle (panels of 64 bf16 or 32 fp32 columns): a
+// thread that stored its row itself would touch as many lines as there are lanes with every instruction.
 template <typename T>
-__device__ __forceinline__ void store_row32(T* p, const float (&x)[32]) {
+__device__ __forceinline__ void put_row32(unsigned char* tile, int row, int c0, const float (&x)[32]) {
   if constexpr (sizeof(T) == 2) {
 #pragma unroll
     for (int c = 0; c < 4; ++c) {
@@ -819,12 +879,19 @@ __device__ __forceinline__ void store_row32(T* p, const float (&x)[32]) {
         const __nv_bfloat162 v = __floats2bfloat162_rn(x[8 * c + 2 * i], x[8 * c + 2 * i + 1]);
         w[i] = *reinterpret_cast<const uint32_t*>(&v);
       }
-      *reinterpret_cast<uint4*>(p + 8 * c) = make_uint4(w[0], w[1], w[2], w[3]);
+      *reinterpret_cast<uint4*>(tile + image_at(row, c0 / 8 + c, 128)) = make_uint4(w[0], w[1], w[2], w[3]);
     }
   } else {
 #pragma unroll
-    for (int c = 0; c < 8; ++c) *reinterpret_cast<float4*>(p + 4 * c) = make_float4(x[4 * c], x[4 * c + 1], x[4 * c + 2], x[4 * c + 3]);
+    for (int c = 0; c < 8; ++c)
+      *reinterpret_cast<float4*>(tile + image_at(row, c0 / 4 + c, 128)) = make_float4(x[4 * c], x[4 * c + 1], x[4 * c + 2], x[4 * c + 3]);
   }
+}
+// One thread: the tile's `cols` columns to columns x0 .. of the result.
+template <typename T>
+__device__ __forceinline__ void store_tile(const CUtensorMap* map, const unsigned char* tile, int x0, int cols, int token, int head, int batch) {
+  constexpr int PER = 128 / (int)sizeof(T);
+  for (int x = 0; x < cols; x += PER) tma_store_4d(map, tile + x / PER * 16384, x0 + x, token, head, batch);
 }
 // The sum of the two halves [hi | lo], 64 columns each, of a product: columns c0 .. c0 + 31
 __device__ __forceinline__ void load_both(uint32_t taddr, float (&x)[32]) {
@@ -855,6 +922,17 @@ x_output_kernel(const __grid_constant__ XMaps maps, const __grid_constant__ Delt
       for (int x = 0; x < PANELS; ++x) tma_load_4d(sm.qk + 32768 + x * 16384, &maps.k, bar, x * 64, c * 128, p.hk, p.b);
       bulk_load(sm.s, rec + Rec::S + eh * D * 128, D * 128, bar);
       bulk_load(sm.s + D * 128, rec + Rec::S + D * D * 2 + eh * D * 128, D * 128, bar);
+      prefetch(rec + Rec::X, 65536);
+      unsigned nx, ny;
+      if (later_block(296, nx, ny) && nx % PANELS == 0) {
+        const XPlace o = x_place(a, ny, nx / PANELS);
+        for (int x = 0; x < PANELS; ++x) {
+          tma_prefetch_4d(&maps.q, x * 64, nx / PANELS * 128, o.hk, o.b);
+          tma_prefetch_4d(&maps.k, x * 64, nx / PANELS * 128, o.hk, o.b);
+          tma_prefetch_4d(&maps.v, x * 64, nx / PANELS * 128, o.h, o.b);
+        }
+        prefetch(static_cast<const unsigned char*>(a.ws) + o.rec * Rec::FWD + Rec::S, Rec::STATE);
+      }
     }
     uint4 raw[4];
     load_raw32(static_cast<const __nv_bfloat16*>(a.v) + p.row + row * a.sT + eh * 64 + half * 32, row < p.n, raw);
@@ -899,7 +977,12 @@ x_output_kernel(const __grid_constant__ XMaps maps, const __grid_constant__ Delt
     load_both(tmem + mine + half * 32, x);
 #pragma unroll
     for (int i = 0; i < 32; ++i) x[i] += v[i];
-    if (row < p.n) store_row32(static_cast<TO*>(a.o) + p.row + row * a.sT + eh * 64 + half * 32, x);
+    put_row32<TO>(sm.qk, row, half * 32, x);
+    X_HAND_OVER();
+    if (tid == 0) {
+      store_tile<TO>(&maps.o, sm.qk, eh * 64, 64, c * 128, p.h, p.b);
+      tma_store_commit();
+    }
     return true;
   });
 }
@@ -1064,6 +1147,20 @@ x_values_kernel(const __grid_constant__ XMaps maps, const __grid_constant__ Delt
       const unsigned char* const state = grad ? bwd + Rec::E : fwd + Rec::S;
       bulk_load(sm.s, state + eh * D * 128, D * 128, bar);
       bulk_load(sm.s + D * 128, state + D * D * 2 + eh * D * 128, D * 128, bar);
+      unsigned nx, ny;
+      if (later_block(296, nx, ny) && nx % (2 * PANELS) == 0) {
+        const XPlace o = x_place(a, ny, nx / (2 * PANELS));
+        for (int x = 0; x < PANELS; ++x) {
+          tma_prefetch_4d(&maps.k, x * 64, nx / (2 * PANELS) * 128, o.hk, o.b);
+          tma_prefetch_4d(&maps.v, x * 64, nx / (2 * PANELS) * 128, o.h, o.b);
+        }
+        const unsigned char* const of = static_cast<const unsigned char*>(a.ws) + o.rec * Rec::FWD;
+        const unsigned char* const ob = static_cast<const unsigned char*>(a.ws_bwd) + o.rec * Rec::BWD;
+        prefetch(of + Rec::S, Rec::STATE);
+        prefetch(of + Rec::U, 65536);
+        prefetch(ob + Rec::E, Rec::STATE);
+        prefetch(ob + Rec::Z, Rec::TOK);
+      }
     }
     const float2 end = *reinterpret_cast<const float2*>(fwd + Rec::END);
     float add[32];
@@ -1121,11 +1218,12 @@ x_values_kernel(const __grid_constant__ XMaps maps, const __grid_constant__ Delt
     if (grad) {
 #pragma unroll
       for (int i = 0; i < 32; ++i) x[i] += add[i];
-      if (row < p.n) store_row32(static_cast<TO*>(a.dv) + p.row + row * a.sT + eh * 64 + half * 32, x);
+      put_row32<TO>(sm.u, row, half * 32, x);
     }
     put();
     X_HAND_OVER();
     if (tid == 0) {
+      if (grad) store_tile<TO>(&maps.dv, sm.u, eh * 64, 64, c * 128, p.h, p.b);
       unsigned char* const to = bwd + (grad ? Rec::DR : Rec::Y) + eh * 16384;
       bulk_store(to, sm.s, 16384);
       bulk_store(to + PANELS * 16384, sm.s + 16384, 16384);
@@ -1138,27 +1236,31 @@ x_values_kernel(const __grid_constant__ XMaps maps, const __grid_constant__ Delt
 // ---- gradients ---------------------------------------------------------------------------------------------------------------------------
 // dQ, dK, dg and dbeta of a chunk of a key head: one thread block of 512 threads, which takes the value heads of the group one after
 // the other.  Thread (q, lane) of quarter w has row q * 32 + lane, columns w * 32 .. + 31 of every accumulator.
-//   1  Q K^T, K K^T, dO Y^T, then dR Y^T                    scores: F and -H stay in registers as two terms; Z's sums (dg, dbeta)
-//   2  dO S^T, dR S^T, then Y E'^T                          what the state has of dQ and dK, scaled by rows; a_i, b_j
-//   3  dQ += F K,   dK += F^T Q - H^T K - H K               F and -H as images, one of each for both orientations
+//   1  dO S^T, dR S^T, then Y E'^T                          what the states have of dQ and dK, scaled by rows; a_i, b_j, <S, E'>
+//   2  Q K^T, dO Y^T, then K K^T, dR Y^T                    scores: F and -H as images; Z's sums (dg, dbeta)
+//   3  dQ += F K,   dK += F^T Q - H^T K - H K               one image of each for both orientations
 // Sums over columns of a chunk's [128, 128] matrix go by butterflies over the lanes (16 values, 16 shuffles); sums over s run by scans.
-enum { XG_QK = 0, XG_Y, XG_DR, XG_SH, XG_SL, XG_E, XG_MMA, XG_DRAIN, XG_BARS };
+// 224 KB of operands come first, E' takes the place of S, q and k that of E', F and -H those of Y and dR, so that there is one thread
+// block to an SM.  The order is what keeps its threads within 128 registers: with the scores first F and -H (64 registers) waited for
+// the rest to be made, and what was spilled for them went to L2, since there is no L1 beside 227 KB of shared memory (480 us for 2048
+// chunks).
+enum { XG_LOAD = 0, XG_E, XG_QK, XG_MMA, XG_DRAIN, XG_BARS };
 template <int D>
 struct alignas(1024) XGradSmem {
-  static constexpr int TOK = 128 * D * 2;  // 128 rows of bf16
-  unsigned char a[4 * TOK > 65536 ? 65536 : 65536];  // q, k; dR; q, k
-  unsigned char o[32768];                               // dO
-  unsigned char y[65536];                               // Y; F
-  unsigned char s[65536];                               // sums; S; E'; -H
-  float2 sum[128];
+  unsigned char a[65536];  // S; E'; q, k
+  unsigned char o[32768];  // dO; sums
+  unsigned char y[65536];  // Y; F
+  unsigned char s[65536];  // dR; -H
+  float2 sum[128];         // the head of the gate table
+  float to_last[128];
   uint64_t bars[XG_BARS];
   int armed[XG_BARS];
   uint32_t tmem_slot;
   int abort;
 };
-struct XSums {  // (in the second half of s)
-  float col[4][128], pre[4][128], rows[4][128], total[4][4], suffix[128];
-  float a[4][128], b[4][128], a_sum[128], b_sum[128], part[16];
+struct alignas(16) XSums {
+  float beta[128], col[4][128], pre[128], rows[4][128], total[4][4];
+  float a[4][128], b[4][128], a_sum[4], b_sum[4], part[16];
 };
 
 // Over the 32 lanes, sums of each of 16 values per lane: lane l returns that of value l / 2.
@@ -1201,23 +1303,14 @@ __device__ __forceinline__ float prefix_sum_before(float x, int lane) {
   const float y = __shfl_up_sync(0xffffffffu, x, 1);
   return lane == 0 ? 0.f : y;
 }
-__device__ __forceinline__ void load_row16(const __nv_bfloat16* p, bool in, float (&x)[16]) {
-#pragma unroll
-  for (int c = 0; c < 2; ++c) {
-    uint4 w = make_uint4(0u, 0u, 0u, 0u);
-    if (in) w = *reinterpret_cast<const uint4*>(p + 8 * c);
-    x[8 * c] = bf_lo(w.x); x[8 * c + 1] = bf_hi(w.x); x[8 * c + 2] = bf_lo(w.y); x[8 * c + 3] = bf_hi(w.y);
-    x[8 * c + 4] = bf_lo(w.z); x[8 * c + 5] = bf_hi(w.z); x[8 * c + 6] = bf_lo(w.w); x[8 * c + 7] = bf_hi(w.w);
-  }
-}
 template <int D, typename TO>
 __global__ void __launch_bounds__(512, 1)
 x_gradient_kernel(const __grid_constant__ XMaps maps, const __grid_constant__ DeltaArgs a) {
   extern __shared__ unsigned char smem_raw[];
   using Rec = XRec<D>;
   XGradSmem<D>& sm = *reinterpret_cast<XGradSmem<D>*>(smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u));
-  XSums& sums = *reinterpret_cast<XSums*>(sm.s + 32768);
-  static_assert(sizeof(XSums) <= 32768, "sums");
+  XSums& sums = *reinterpret_cast<XSums*>(sm.o);
+  static_assert(sizeof(XSums) <= 16384, "sums");
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, q = warp & 3, w4 = warp >> 2, row = q * 32 + lane, c0 = w4 * 32;
   x_run<512>(sm, XG_BARS, [&](const uint32_t tmem) -> bool {
     constexpr int PANELS = D / 64, NK = D / 16, TOK = 128 * D * 2;  // bytes of 128 rows of bf16, and half of their image
@@ -1225,14 +1318,12 @@ x_gradient_kernel(const __grid_constant__ XMaps maps, const __grid_constant__ De
     constexpr uint32_t ID_N = umma_idesc_bf16(128, D, false, true), ID_T = umma_idesc_bf16(128, D, true, true);
     const int c = blockIdx.x, b = blockIdx.y / a.Hk, hk = blockIdx.y % a.Hk, G = a.H / a.Hk;
     const uint32_t mine = (uint32_t)(q * 32) << 16, T0 = tmem, T1 = tmem + 128, T2 = tmem + 256, T3 = tmem + 384;
-    const long long krow = b * a.sBk + hk * a.sHk + (long long)(c * 128 + row) * a.sTk + c0;
     __syncwarp();
     const uint32_t go = warp == 0 ? elect_one() : 0;
     const bool feat = c0 < D;  // has columns of features
     int mma = 0, second = 0;   // parities
     unsigned char* const first = static_cast<unsigned char*>(a.ws_bwd) + ((size_t)(b * a.H + hk * G) * a.nchunk + c) * Rec::BWD;
-    auto load_qk = [&]() {
-      uint64_t* const bar = expect(sm, XG_QK, 2 * TOK);
+    auto load_qk = [&](uint64_t* bar) {
       for (int x = 0; x < PANELS; ++x) tma_load_4d(sm.a + x * 16384, &maps.q, bar, x * 64, c * 128, hk, b);
       for (int x = 0; x < PANELS; ++x) tma_load_4d(sm.a + TOK + x * 16384, &maps.k, bar, x * 64, c * 128, hk, b);
     };
@@ -1241,194 +1332,210 @@ x_gradient_kernel(const __grid_constant__ XMaps maps, const __grid_constant__ De
       const unsigned char* const fwd = static_cast<const unsigned char*>(a.ws) + p.rec * Rec::FWD;
       const unsigned char* const bwd = static_cast<const unsigned char*>(a.ws_bwd) + p.rec * Rec::BWD;
       if (tid == 0) {
-        load_qk();
-        uint64_t* const bar = expect(sm, XG_Y, 3 * TOK);
+        uint64_t* const bar = expect(sm, XG_LOAD, 5 * TOK + D * D * 4 + 1536);
+        bulk_load(sm.a, fwd + Rec::S, D * D * 4, bar);
         for (int x = 0; x < PANELS; ++x) tma_load_4d(sm.o + x * 16384, &maps.d_o, bar, x * 64, c * 128, p.h, p.b);
+        bulk_load(sm.s, bwd + Rec::DR, 2 * TOK, bar);
         bulk_load(sm.y, bwd + Rec::Y, 2 * TOK, bar);
+        bulk_load(sm.sum, fwd + Rec::GATES, 1536, bar);
       }
-      // gates: the sums stay in shared memory, the rest in registers
       const XGateTable& gates = *reinterpret_cast<const XGateTable*>(fwd + Rec::GATES);
       const float2 end = *reinterpret_cast<const float2*>(fwd + Rec::END);
-      const float2 own = gates.sum[row];
-      const float beta_row = gates.beta[row], since = ex2_approx(own.x + own.y), until = decay2(end, own), all = ex2_approx(end.x + end.y);
-      if (tid < 128) sm.sum[tid] = gates.sum[tid];
-      const float beta_tid = tid < 128 ? gates.beta[tid] : 0.f, bcol = gates.beta[c0 + lane];
-      X_WAIT(sm.bars[XG_QK], 0, 100);
-      X_WAIT(sm.bars[XG_Y], second, 101);
+      const float beta_row = gates.beta[row], beta_tid = tid < 128 ? gates.beta[tid] : 0.f;
+      X_WAIT(sm.bars[XG_LOAD], second, 101);
+      // ---- what the states have ----
       if (warp == 0) {
-        umma_group_ss<NK, true, true>(T0, kmaj(sm.a), kmaj(sm.a + TOK), XHI, ID_SC, 0, go);
-        umma_group_ss<NK, true, true>(T1, kmaj(sm.a + TOK), kmaj(sm.a + TOK), XHI, ID_SC, 0, go);
-        umma_group_ss<NK, true, true>(T2, kmaj(sm.o), kmaj(sm.y), XHI, ID_SC, 0, go);
-        umma_group_ss<NK, true, true>(T2, kmaj(sm.o), kmaj(sm.y + TOK), XHI, ID_SC, 1, go);
+        umma_group_ss<NK, true, true>(T0, kmaj(sm.o), kmaj(sm.a), XHI, ID_ST, 0, go);
+        umma_group_ss<NK, true, true>(T0, kmaj(sm.o), kmaj(sm.a + D * D * 2), XHI, ID_ST, 1, go);
+        umma_group_ss<NK, true, true>(T1, kmaj(sm.s), kmaj(sm.a), XHI, ID_ST, 0, go);
+        umma_group_ss<NK, true, true>(T1, kmaj(sm.s), kmaj(sm.a + D * D * 2), XHI, ID_ST, 1, go);
+        umma_group_ss<NK, true, true>(T1, kmaj(sm.s + TOK), kmaj(sm.a), XHI, ID_ST, 1, go);
         umma_commit_if(&sm.bars[XG_MMA], go);
+      }
+      if (tid == 0) {
+        prefetch(bwd + Rec::E, Rec::STATE);
+        for (int x = 0; x < PANELS; ++x) tma_prefetch_4d(&maps.q, x * 64, c * 128, hk, b);
+        for (int x = 0; x < PANELS; ++x) tma_prefetch_4d(&maps.k, x * 64, c * 128, hk, b);
+        unsigned nx, ny;
+        if (gh + 1 == G && later_block(148, nx, ny)) {
+          const XPlace o = x_place(a, ny / a.Hk * a.H + ny % a.Hk * G, nx);
+          const unsigned char* const ob = static_cast<const unsigned char*>(a.ws_bwd) + o.rec * Rec::BWD;
+          prefetch(static_cast<const unsigned char*>(a.ws) + o.rec * Rec::FWD + Rec::S, Rec::STATE);
+          prefetch(ob + Rec::DR, Rec::TOK);
+          prefetch(ob + Rec::Y, Rec::TOK);
+          for (int x = 0; x < PANELS; ++x) tma_prefetch_4d(&maps.d_o, x * 64, nx * 128, o.h, o.b);
+        }
+      }
+      __syncwarp();
+      const float2 own = sm.sum[row];
+      const float since = ex2_approx(own.x + own.y), until = decay2(end, own);
+      constexpr int IT = D * D / 8 / 512;
+      uint4 sh[IT], sl[IT];  // this thread's part of S for <S, E'>
+#pragma unroll
+      for (int n = 0; n < IT; ++n) {
+        sh[n] = reinterpret_cast<const uint4*>(sm.a)[tid + n * 512];
+        sl[n] = reinterpret_cast<const uint4*>(sm.a)[tid + n * 512 + D * D / 8];
       }
       X_WAIT(sm.bars[XG_MMA], mma, 102);
       mma ^= 1;
-      if (tid == 0) {
-        bulk_load(sm.a, bwd + Rec::DR, 2 * TOK, expect(sm, XG_DR, 2 * TOK));
-      }
-      X_WAIT(sm.bars[XG_DR], second, 103);
+      if (tid == 0) bulk_load(sm.a, bwd + Rec::E, D * D * 4, expect(sm, XG_E, D * D * 4));
+      X_WAIT(sm.bars[XG_E], second, 103);
       if (warp == 0) {
-        umma_group_ss<NK, true, true>(T3, kmaj(sm.a), kmaj(sm.y), XHI, ID_SC, 0, go);
-        umma_group_ss<NK, true, true>(T3, kmaj(sm.a), kmaj(sm.y + TOK), XHI, ID_SC, 1, go);
-        umma_group_ss<NK, true, true>(T3, kmaj(sm.a + TOK), kmaj(sm.y), XHI, ID_SC, 1, go);
+        umma_group_ss<NK, true, true>(T2, kmaj(sm.y), kmaj(sm.a), XHI, ID_ST, 0, go);
+        umma_group_ss<NK, true, true>(T2, kmaj(sm.y), kmaj(sm.a + D * D * 2), XHI, ID_ST, 1, go);
+        umma_group_ss<NK, true, true>(T2, kmaj(sm.y + TOK), kmaj(sm.a), XHI, ID_ST, 1, go);
         umma_commit_if(&sm.bars[XG_MMA], go);
       }
-      X_WAIT(sm.bars[XG_MMA], mma, 104);
-      mma ^= 1;
-      if (tid == 0) bulk_load(sm.s, fwd + Rec::S, D * D * 2, expect(sm, XG_SH, D * D * 2));
-
-      // ---- scores ----
-      uint32_t fh[16], fl[16], nh[16], nl[16];
-      float before = 0.f;  // Z's sum over this thread's columns so far
-#pragma unroll
-      for (int pc = 0; pc < 2; ++pc) {
-        float qk[16], kk[16], f[16], h[16];
-        load_acc16(T0 + mine + c0 + pc * 16, qk);
-        load_acc16(T1 + mine + c0 + pc * 16, kk);
-        load_acc16(T2 + mine + c0 + pc * 16, f);
-        load_acc16(T3 + mine + c0 + pc * 16, h);
-        tmem_ld_wait();
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int j = c0 + pc * 16 + i;
-          const float bj = __shfl_sync(0xffffffffu, bcol, pc * 16 + i);
-          const float dec = j <= row ? decay2(own, sm.sum[j]) : 0.f;
-          f[i] = j <= row ? a.scale * dec * f[i] : 0.f;
-          h[i] = j < row ? dec * h[i] : 0.f;
-          qk[i] = f[i] * qk[i] - h[i] * kk[i];   // Z without beta_j
-          kk[i] = row >= j ? before : 0.f;       // of the columns before j
-          before = fmaf(bj, qk[i], before);
-          f[i] *= bj;
-          h[i] *= -bj;
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          split2(f2_pack(f[2 * i], f[2 * i + 1]), fh[pc * 8 + i], fl[pc * 8 + i]);
-          split2(f2_pack(h[2 * i], h[2 * i + 1]), nh[pc * 8 + i], nl[pc * 8 + i]);
-        }
-        const float col = lane_sums16(qk, lane), pre = lane_sums16(kk, lane);
-        if ((lane & 1) == 0) {
-          sums.col[q][c0 + pc * 16 + (lane >> 1)] = col;
-          sums.pre[q][c0 + pc * 16 + (lane >> 1)] = pre;
-        }
-      }
-      sums.rows[w4][row] = before;
-      __syncthreads();
-      {
-        float off = 0.f;
-        for (int w = 0; w < w4; ++w) off += sums.rows[w][row];
-        const float x = suffix_sum(off, lane);
-        if (lane == 0) sums.total[w4][q] = x;
-        if (q == w4) sums.suffix[row] = x;
-      }
-      __syncthreads();
-      float dbeta = 0.f, dg = 0.f;
-      if (tid < 128) {  // token tid, in the quarter tid / 32
-        dg = sums.suffix[tid];
-#pragma unroll
-        for (int x = 0; x < 4; ++x) {
-          dbeta += sums.col[x][tid];
-          dg += sums.pre[x][tid];
-          if (x > (tid >> 5)) dg += sums.total[tid >> 5][x];
-        }
-      }
-      tc_fence_before_sync();
-      __syncthreads();
-      tc_fence_after_sync();
-      // ---- what the states have ----
-      if (tid == 0) bulk_load(sm.s + D * D * 2, fwd + Rec::S + D * D * 2, D * D * 2, expect(sm, XG_SL, D * D * 2));
-      X_WAIT(sm.bars[XG_SH], second, 105);
-      X_WAIT(sm.bars[XG_SL], second, 106);
-      if (warp == 0) {
-        umma_group_ss<NK, true, true>(T0, kmaj(sm.o), kmaj(sm.s), XHI, ID_ST, 0, go);
-        umma_group_ss<NK, true, true>(T0, kmaj(sm.o), kmaj(sm.s + D * D * 2), XHI, ID_ST, 1, go);
-        umma_group_ss<NK, true, true>(T1, kmaj(sm.a), kmaj(sm.s), XHI, ID_ST, 0, go);
-        umma_group_ss<NK, true, true>(T1, kmaj(sm.a), kmaj(sm.s + D * D * 2), XHI, ID_ST, 1, go);
-        umma_group_ss<NK, true, true>(T1, kmaj(sm.a + TOK), kmaj(sm.s), XHI, ID_ST, 1, go);
-        umma_commit_if(&sm.bars[XG_MMA], go);
-      }
-      // <S, E'> meanwhile, from the images
       float whole = 0.f;
-      for (int i = tid; i < D * D / 8; i += 512) {
-        const uint4* const s = reinterpret_cast<const uint4*>(fwd + Rec::S) + i;
-        const uint4* const e = reinterpret_cast<const uint4*>(bwd + Rec::E) + i;
-        float x[8], y[8];
-        join8(s[0], s[D * D / 8], x);
-        join8(e[0], e[D * D / 8], y);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) whole = fmaf(x[k], y[k], whole);
+      for (int n = 0; n < IT; ++n) {
+        float x[8], y[8];
+        join8(sh[n], sl[n], x);
+        join8(reinterpret_cast<const uint4*>(sm.a)[tid + n * 512], reinterpret_cast<const uint4*>(sm.a)[tid + n * 512 + D * D / 8], y);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) whole = fmaf(x[i], y[i], whole);
       }
-      whole *= all;
+      whole *= ex2_approx(end.x + end.y);
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) whole += __shfl_xor_sync(0xffffffffu, whole, o);
-      X_WAIT(sm.bars[XG_MMA], mma, 107);
+      X_WAIT(sm.bars[XG_MMA], mma, 104);
       mma ^= 1;
-      if (tid == 0) bulk_load(sm.s, bwd + Rec::E, D * D * 4, expect(sm, XG_E, D * D * 4));
+      if (tid == 0) {
+        uint64_t* const bar = expect(sm, XG_QK, 2 * TOK);
+        for (int x = 0; x < PANELS; ++x) tma_load_4d(sm.a + x * 16384, &maps.q, bar, x * 64, c * 128, hk, b);
+        for (int x = 0; x < PANELS; ++x) tma_load_4d(sm.a + TOK + x * 16384, &maps.k, bar, x * 64, c * 128, hk, b);
+      }
+      X_WAIT(sm.bars[XG_QK], second, 105);
       float dot_a = 0.f, dot_b = 0.f;
       if (feat)
 #pragma unroll
         for (int pc = 0; pc < 2; ++pc) {
-          float x[16], w[16];
-          load_acc16(T0 + mine + c0 + pc * 16, x);
-          load_row16(static_cast<const __nv_bfloat16*>(a.q) + krow + pc * 16, row < p.n, w);
-          tmem_ld_wait();
+          float x[16], y[16];
+          uint4 kr[2], qr[2];
 #pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            x[i] *= a.scale * since;
-            dot_a = fmaf(x[i], w[i], dot_a);
+          for (int k = 0; k < 2; ++k) {
+            const uint32_t at = image_at(row, w4 * 4 + pc * 2 + k, 128);
+            qr[k] = *reinterpret_cast<const uint4*>(sm.a + at);
+            kr[k] = *reinterpret_cast<const uint4*>(sm.a + TOK + at);
           }
+          load_acc16(T0 + mine + c0 + pc * 16, x);
+          tmem_ld_wait();
+          each32(qr, [&](int i, float w) {
+            x[i] *= a.scale * since;
+            dot_a = fmaf(x[i], w, dot_a);
+          });
           tmem_st_x16(T0 + mine + c0 + pc * 16, *reinterpret_cast<uint32_t(*)[16]>(&x));
           load_acc16(T1 + mine + c0 + pc * 16, x);
-          load_row16(static_cast<const __nv_bfloat16*>(a.k) + krow + pc * 16, row < p.n, w);
+          load_acc16(T2 + mine + c0 + pc * 16, y);
           tmem_ld_wait();
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
+          each32(kr, [&](int i, float w) {
             x[i] *= -since;
-            dot_a = fmaf(x[i], w[i], dot_a);
-          }
+            dot_a = fmaf(x[i], w, dot_a);
+            y[i] *= until;
+            dot_b = fmaf(y[i], w, dot_b);
+            x[i] = fmaf(beta_row, y[i], x[i]);
+          });
           tmem_st_x16(T1 + mine + c0 + pc * 16, *reinterpret_cast<uint32_t(*)[16]>(&x));
         }
-      X_WAIT(sm.bars[XG_E], second, 108);
+      X_HAND_OVER();
+      // ---- scores ----
       if (warp == 0) {
-        umma_group_ss<NK, true, true>(T2, kmaj(sm.y), kmaj(sm.s), XHI, ID_ST, 0, go);
-        umma_group_ss<NK, true, true>(T2, kmaj(sm.y), kmaj(sm.s + D * D * 2), XHI, ID_ST, 1, go);
-        umma_group_ss<NK, true, true>(T2, kmaj(sm.y + TOK), kmaj(sm.s), XHI, ID_ST, 1, go);
+        umma_group_ss<NK, true, true>(T2, kmaj(sm.a), kmaj(sm.a + TOK), XHI, ID_SC, 0, go);
+        umma_group_ss<NK, true, true>(T3, kmaj(sm.o), kmaj(sm.y), XHI, ID_SC, 0, go);
+        umma_group_ss<NK, true, true>(T3, kmaj(sm.o), kmaj(sm.y + TOK), XHI, ID_SC, 1, go);
         umma_commit_if(&sm.bars[XG_MMA], go);
       }
-      X_WAIT(sm.bars[XG_MMA], mma, 109);
+      X_WAIT(sm.bars[XG_MMA], mma, 106);
       mma ^= 1;
-      if (tid == 0) load_qk();
-      if (feat)
+      // F, and Z without beta_j; then -H and the rest of Z (two values to an instruction where they are of another block of 32)
+      uint64_t z[16];
+      const float to_block = w4 < q ? decay2(own, sm.sum[c0 + 31]) : 0.f;
+      if (tid < 128) sums.beta[tid] = beta_tid;  // (dO is read)
+      __syncthreads();
+      auto scores = [&](int pc, float times, float sign, bool diagonal, uint4(&hi)[2], uint4(&lo)[2]) {  // columns 16 pc .. + 15
+        float u[16], f[16];
+        load_acc16(T2 + mine + c0 + pc * 16, u);
+        load_acc16(T3 + mine + c0 + pc * 16, f);
+        tmem_ld_wait();
+        if (w4 < q) {
+          const uint64_t all = f2_pack(times * to_block, times * to_block);
 #pragma unroll
-        for (int pc = 0; pc < 2; ++pc) {
-          float x[16], w[16];
-          load_acc16(T2 + mine + c0 + pc * 16, x);
-          load_row16(static_cast<const __nv_bfloat16*>(a.k) + krow + pc * 16, row < p.n, w);
-          tmem_ld_wait();
+          for (int i = 0; i < 16; i += 2) {
+            const float2 d = *reinterpret_cast<const float2*>(&sm.to_last[c0 + pc * 16 + i]);
+            const uint64_t v = f2_mul(f2_mul(f2_pack(d.x, d.y), all), f2_pack(f[i], f[i + 1]));
+            f2_unpack(v, f[i], f[i + 1]);
+          }
+        } else {
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
-            x[i] *= until;
-            dot_b = fmaf(x[i], w[i], dot_b);
+            const int n = pc * 16 + i;
+            f[i] = n < lane || (diagonal && n == lane) ? f[i] * (times * decay2(own, sm.sum[c0 + n])) : 0.f;
           }
-          load_acc16(T1 + mine + c0 + pc * 16, w);
-          tmem_ld_wait();
-#pragma unroll
-          for (int i = 0; i < 16; ++i) w[i] = fmaf(beta_row, x[i], w[i]);
-          tmem_st_x16(T1 + mine + c0 + pc * 16, *reinterpret_cast<uint32_t(*)[16]>(&w));
         }
-      // (Y and E' are read) F and -H as images
+        const uint64_t s2 = f2_pack(sign, sign);
+        uint32_t h[8], l[8];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const uint32_t at = image_at(row, w4 * 4 + i, 128);
-        *reinterpret_cast<uint4*>(sm.y + at) = make_uint4(fh[4 * i], fh[4 * i + 1], fh[4 * i + 2], fh[4 * i + 3]);
-        *reinterpret_cast<uint4*>(sm.y + 32768 + at) = make_uint4(fl[4 * i], fl[4 * i + 1], fl[4 * i + 2], fl[4 * i + 3]);
-        *reinterpret_cast<uint4*>(sm.s + at) = make_uint4(nh[4 * i], nh[4 * i + 1], nh[4 * i + 2], nh[4 * i + 3]);
-        *reinterpret_cast<uint4*>(sm.s + 32768 + at) = make_uint4(nl[4 * i], nl[4 * i + 1], nl[4 * i + 2], nl[4 * i + 3]);
+        for (int i = 0; i < 8; ++i) {
+          const float2 bt = *reinterpret_cast<const float2*>(&sums.beta[c0 + pc * 16 + 2 * i]);
+          const uint64_t v = f2_mul(f2_pack(f[2 * i], f[2 * i + 1]), s2);
+          z[pc * 8 + i] = f2_fma(v, f2_pack(u[2 * i], u[2 * i + 1]), z[pc * 8 + i]);
+          split2(f2_mul(v, f2_pack(bt.x, bt.y)), h[i], l[i]);
+        }
+        hi[0] = make_uint4(h[0], h[1], h[2], h[3]);
+        hi[1] = make_uint4(h[4], h[5], h[6], h[7]);
+        lo[0] = make_uint4(l[0], l[1], l[2], l[3]);
+        lo[1] = make_uint4(l[4], l[5], l[6], l[7]);
+      };
+      auto put = [&](unsigned char* image, int c, const uint4& h, const uint4& l) {
+        const uint32_t at = image_at(row, w4 * 4 + c, 128);
+        *reinterpret_cast<uint4*>(image + at) = h;
+        *reinterpret_cast<uint4*>(image + 32768 + at) = l;
+      };
+#pragma unroll
+      for (int i = 0; i < 16; ++i) z[i] = 0;
+      uint4 fh[4], fl[4];
+#pragma unroll
+      for (int pc = 0; pc < 2; ++pc) {
+        fh[2 * pc] = fh[2 * pc + 1] = fl[2 * pc] = fl[2 * pc + 1] = make_uint4(0u, 0u, 0u, 0u);
+        if (w4 <= q) scores(pc, a.scale, 1.f, true, *reinterpret_cast<uint4(*)[2]>(&fh[2 * pc]), *reinterpret_cast<uint4(*)[2]>(&fl[2 * pc]));
+      }
+      tc_fence_before_sync();
+      __syncthreads();
+      tc_fence_after_sync();
+      if (warp == 0) {
+        umma_group_ss<NK, true, true>(T2, kmaj(sm.a + TOK), kmaj(sm.a + TOK), XHI, ID_SC, 0, go);
+        umma_group_ss<NK, true, true>(T3, kmaj(sm.s), kmaj(sm.y), XHI, ID_SC, 0, go);
+        umma_group_ss<NK, true, true>(T3, kmaj(sm.s), kmaj(sm.y + TOK), XHI, ID_SC, 1, go);
+        umma_group_ss<NK, true, true>(T3, kmaj(sm.s + TOK), kmaj(sm.y), XHI, ID_SC, 1, go);
+        umma_commit_if(&sm.bars[XG_MMA], go);
+      }
+      X_WAIT(sm.bars[XG_MMA], mma, 107);
+      mma ^= 1;
+      // (Y and dR are read) F and -H as images
+#pragma unroll
+      for (int k = 0; k < 4; ++k) put(sm.y, k, fh[k], fl[k]);
+#pragma unroll
+      for (int pc = 0; pc < 2; ++pc) {
+        uint4 h[2], l[2];
+        h[0] = h[1] = l[0] = l[1] = make_uint4(0u, 0u, 0u, 0u);
+        if (w4 <= q) scores(pc, 1.f, -1.f, false, h, l);
+        put(sm.s, 2 * pc, h[0], l[0]);
+        put(sm.s, 2 * pc + 1, h[1], l[1]);
+      }
+      // The last products are issued by a warp whose scores are above the diagonal, so that it has no part in Z: an issuing warp waits as long
+      // as its products run, here 4100 clocks, and the others sum up Z meanwhile, at a barrier of their own.
+      constexpr int ISSUER = 12;
+      sums.a[w4][row] = dot_a;
+      sums.b[w4][row] = dot_b;
+      if (lane == 0) sums.part[warp] = whole;
+      if (warp == ISSUER) {
+        sums.rows[w4][row] = 0.f;
+        sums.col[q][c0 + lane] = 0.f;
+        if (lane == 0) sums.total[w4][q] = 0.f;
       }
       X_HAND_OVER();
-      X_WAIT(sm.bars[XG_QK], 1, 110);
-      if (warp == 0) {
+      if (warp == ISSUER) {
+        const uint32_t go = elect_one();
         const unsigned char *const qt = sm.a, *const kt = sm.a + TOK;
 #pragma unroll
         for (int term = 0; term < 2; ++term) {
@@ -1438,35 +1545,72 @@ x_gradient_kernel(const __grid_constant__ XMaps maps, const __grid_constant__ De
           umma_group_ss<8, true, false>(T1, kmaj(sm.s + term * 32768), mnmaj(kt), XHI, ID_N, 1, go);
         }
         umma_commit_if(&sm.bars[XG_MMA], go);
-      }
-      // ---- dg, dbeta: in dO's place, which nothing reads any more ----
-      XSums& more = *reinterpret_cast<XSums*>(sm.o);
-      more.a[w4][row] = dot_a;
-      more.b[w4][row] = dot_b;
-      if (lane == 0) more.part[warp] = whole;
-      __syncthreads();
-      float ai = 0.f, bi = 0.f;
-      if (tid < 128) {
-        ai = (more.a[0][tid] + more.a[1][tid]) + (more.a[2][tid] + more.a[3][tid]);
-        bi = (more.b[0][tid] + more.b[1][tid]) + (more.b[2][tid] + more.b[3][tid]);
-        dbeta += bi;
-        bi *= beta_tid;
-        const float x = suffix_sum(ai, lane), y = prefix_sum_before(bi, lane);
-        if (lane == 0) more.a_sum[warp] = x;
-        if (lane == 31) more.b_sum[warp] = y + bi;
-        ai = x;
-        bi = y;
-      }
-      __syncthreads();
-      if (tid < p.n) {
-        float w = 0.f;
-        for (int i = 0; i < 16; ++i) w += more.part[i];
-        for (int i = 0; i < 4; ++i) {
-          if (i > warp) ai += more.a_sum[i];
-          if (i < warp) bi += more.b_sum[i];
+      } else {
+        // ---- dg, dbeta meanwhile, in dO's place.  For s in block b of 32: of Z's rows i >= s and columns j < s those of row blocks after b
+        // and column blocks before b as sums of whole blocks, the others of one or the other as scans of rows' or columns' sums, and those
+        // of block b in both as the sums over rows i >= s of what a row has before s.
+        float row_sum = 0.f;
+#pragma unroll
+        for (int pc = 0; pc < 2; ++pc) {
+          float v[16], u[16];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) f2_unpack(z[pc * 8 + i], v[2 * i], v[2 * i + 1]);
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            u[i] = lane >= pc * 16 + i ? row_sum : 0.f;
+            row_sum = fmaf(sums.beta[c0 + pc * 16 + i], v[i], row_sum);
+          }
+          if (w4 == q) {
+            const float pre = lane_sums16(u, lane);
+            if ((lane & 1) == 0) sums.pre[c0 + pc * 16 + (lane >> 1)] = pre;
+          }
+          const float col = w4 <= q ? lane_sums16(v, lane) : 0.f;
+          if ((lane & 1) == 0) sums.col[q][c0 + pc * 16 + (lane >> 1)] = col;
         }
-        a.dg[p.gate + tid * a.gT] = w + ((dg + ai) + bi);
-        a.dbeta[p.gate + tid * a.gT] = dbeta;
+        sums.rows[w4][row] = row_sum;
+        asm volatile("bar.sync 1, 480;" ::: "memory");
+        float ai = 0.f, bi = 0.f, dbeta = 0.f, dg = 0.f;
+        if (tid < 128) {  // token tid, in block `warp`
+          ai = (sums.a[0][tid] + sums.a[1][tid]) + (sums.a[2][tid] + sums.a[3][tid]);
+          bi = (sums.b[0][tid] + sums.b[1][tid]) + (sums.b[2][tid] + sums.b[3][tid]);
+          dbeta = bi;
+          bi *= beta_tid;
+          float left = 0.f, below = 0.f;  // of row tid the column blocks before its own, of column tid the row blocks after it
+          for (int w = 0; w < warp; ++w) left += sums.rows[w][tid];
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            const float col = sums.col[x][tid];
+            dbeta += col;
+            if (x > warp) below += col;
+          }
+          below *= beta_tid;
+          ai = suffix_sum(ai, lane);
+          const float b_before = prefix_sum_before(bi, lane);
+          dg = sums.pre[tid] + suffix_sum(left, lane) + prefix_sum_before(below, lane);
+          if (lane == 0) sums.a_sum[warp] = ai;
+          if (lane == 31) sums.b_sum[warp] = b_before + bi;
+          bi = b_before;
+        }
+        {  // sums of whole blocks
+          const float x = suffix_sum(row_sum, lane);
+          if (lane == 0) sums.total[w4][q] = x;
+        }
+        asm volatile("bar.sync 1, 480;" ::: "memory");
+        if (tid < p.n && tid < 128) {
+          float w = 0.f;
+#pragma unroll
+          for (int i = 0; i < 16; ++i) w += sums.part[i];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            if (i > warp) {
+              ai += sums.a_sum[i];
+              for (int k = 0; k < warp; ++k) dg += sums.total[k][i];
+            }
+            if (i < warp) bi += sums.b_sum[i];
+          }
+          a.dg[p.gate + tid * a.gT] = w + ((dg + ai) + bi);
+          a.dbeta[p.gate + tid * a.gT] = dbeta;
+        }
       }
       X_WAIT(sm.bars[XG_MMA], mma, 111);
       mma ^= 1;
@@ -1483,27 +1627,32 @@ x_gradient_kernel(const __grid_constant__ XMaps maps, const __grid_constant__ De
           if (gh + 1 < G) {
 #pragma unroll
             for (int i = 0; i < 32; ++i) kept[i * 128] = x[i];
-          } else if (row < p.n) {
-            store_row32(static_cast<TO*>(which ? a.dk : a.dq) + krow, x);
+          } else {
+            put_row32<TO>(which ? sm.s : sm.y, row, c0, x);
           }
         }
-      tc_fence_before_sync();
-      __syncthreads();
-      tc_fence_after_sync();
+      X_HAND_OVER();
+      if (tid == 0 && gh + 1 == G) {
+        store_tile<TO>(&maps.dq, sm.y, 0, D, c * 128, hk, b);
+        store_tile<TO>(&maps.dk, sm.s, 0, D, c * 128, hk, b);
+        tma_store_commit();
+      }
     }
     return true;
   });
 }
 
 // ---- launches ----------------------------------------------------------------------------------------------------------------------------
-bool make_token_map(CUtensorMap* m, const void* ptr, const DeltaArgs& a, bool shared) {
+bool make_token_map(CUtensorMap* m, const void* ptr, const DeltaArgs& a, bool shared, bool f32 = false) {
   EncodeTiledFn enc = encode_fn();
   if (!enc) return false;
+  const cuuint64_t esz = f32 ? 4 : 2;
   cuuint64_t dims[4] = {(cuuint64_t)a.D, (cuuint64_t)a.N, (cuuint64_t)(shared ? a.Hk : a.H), (cuuint64_t)a.B};
-  cuuint64_t strides[3] = {(cuuint64_t)(shared ? a.sTk : a.sT) * 2, (cuuint64_t)(shared ? a.sHk : a.sH) * 2, (cuuint64_t)(shared ? a.sBk : a.sB) * 2};
-  cuuint32_t box[4] = {64, 128, 1, 1}, es[4] = {1, 1, 1, 1};
-  return enc(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(ptr), dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
-             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+  cuuint64_t strides[3] = {(cuuint64_t)(shared ? a.sTk : a.sT) * esz, (cuuint64_t)(shared ? a.sHk : a.sH) * esz, (cuuint64_t)(shared ? a.sBk : a.sB) * esz};
+  cuuint32_t box[4] = {(cuuint32_t)(128 / esz), 128, 1, 1}, es[4] = {1, 1, 1, 1};
+  return enc(m, f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(ptr), dims, strides, box, es,
+             CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 template <typename SM, typename K, typename... A>
@@ -1547,8 +1696,9 @@ cudaError_t x_states(const XMaps& m, const DeltaArgs& a, cudaStream_t stream) {
 template <int D, typename TO>
 cudaError_t x_fwd(const DeltaArgs& a, cudaStream_t stream) {
   XMaps m{};
-  if (!make_token_map(&m.q, a.q, a, true) || !make_token_map(&m.k, a.k, a, true) || !make_token_map(&m.v, a.v, a, false)) return cudaErrorInvalidValue;
-  m.d_o = m.v;
+  if (!make_token_map(&m.q, a.q, a, true) || !make_token_map(&m.k, a.k, a, true) || !make_token_map(&m.v, a.v, a, false) ||
+      !make_token_map(&m.o, a.o, a, false, sizeof(TO) == 4))
+    return cudaErrorInvalidValue;
   const cudaError_t err = x_states<D>(m, a, stream);
   if (err != cudaSuccess) return err;
   return x_launch<XOutSmem<D>>(x_output_kernel<D, TO>, K_WALK, dim3(a.nchunk * (D / 64), a.B * a.H), 256, stream, m, a);
@@ -1557,8 +1707,10 @@ cudaError_t x_fwd(const DeltaArgs& a, cudaStream_t stream) {
 template <int D, typename TO>
 cudaError_t x_bwd(const DeltaArgs& a, bool have_fwd, cudaStream_t stream) {
   XMaps m{};
+  constexpr bool F32 = sizeof(TO) == 4;
   if (!make_token_map(&m.q, a.q, a, true) || !make_token_map(&m.k, a.k, a, true) || !make_token_map(&m.v, a.v, a, false) ||
-      !make_token_map(&m.d_o, a.d_o, a, false))
+      !make_token_map(&m.d_o, a.d_o, a, false) || !make_token_map(&m.dq, a.dq, a, true, F32) || !make_token_map(&m.dk, a.dk, a, true, F32) ||
+      !make_token_map(&m.dv, a.dv, a, false, F32))
     return cudaErrorInvalidValue;
   cudaError_t err = have_fwd ? cudaSuccess : x_states<D>(m, a, stream);
   if (err == cudaSuccess)
