@@ -161,7 +161,7 @@ def load():
             raise RuntimeError("extension module _la_call is missing; run `python -m paper_2307_14995_b200.build`") from e
         address = {name: ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in EXPORTS}
         address["la_bwd"] = address["la_bwd_reuse"]  # (the same with a NULL fwd_workspace)
-        _la_call.bind(LaShape, _handle, LaDeltaShape, LaBlockNormShape)
+        _la_call.bind(LaShape, _handle, LaDeltaShape, LaBlockNormShape, lambda: _current_device(), torch.bfloat16, torch.float32)
         # whoever sees _call finds the whole table behind it
         _address = address
         _call = _la_call.call
@@ -171,7 +171,7 @@ def load():
 
 def _enter(name: str, kinds: str, *args) -> None:
     """Calls a C function; kinds has a letter for each argument (s, d, n: shape of the core, the delta rule, the norms; t: tensor or None,
-    i: integer, h: host memory, r: stream)."""
+    capitals and w: the same, held to the delta rule's or the norms' shape, see la_call.c; i: integer, h: host memory, r: stream)."""
     if _call is None:
         load()
     rc = _call(_address[name], kinds, *args)
@@ -401,21 +401,6 @@ def la_lrpe_bwd(shape: LaShape, q, k, v, do, theta, lam, dq, dk, dv, dtheta, pos
 
 
 # ---- the gated delta rule, and the norms between two blocks -------------------------------
-# Their gates, weights and shared heads make it easy to hand over a tensor of another type or size than the shape says, which would be
-# read out of bounds; so types, sizes and device are looked at here (1 us for a decode step).
-_TORCH = {LA_BF16: torch.bfloat16, LA_F32: torch.float32}
-
-
-def _matches(name, device, tensors, dtype, numel):
-    for what, t in tensors.items():
-        if t is None:
-            continue
-        if t.dtype is not dtype or t.numel() != numel:
-            raise ValueError("%s: %s has to be %s with %d elements, not %s with %d" % (name, what, dtype, numel, t.dtype, t.numel()))
-        if t.get_device() != device:
-            raise ValueError("%s: %s has to be on the current CUDA device" % (name, what))
-
-
 def _current_device() -> int:
     return torch.cuda.current_device() if _CURRENT_DEVICE is None or not torch.cuda.is_initialized() else _CURRENT_DEVICE()
 
@@ -436,45 +421,26 @@ def alloc_delta_workspace(op: int, shape: LaDeltaShape, device) -> torch.Tensor:
     return torch.empty(delta_workspace_bytes(op, shape), dtype=torch.uint8, device=device)
 
 
-def _delta_checks(name, s, q, k, v, g, beta, outs, qk_outs, gates, states, workspaces, more_in=()):
-    if type(s) is not LaDeltaShape:
-        raise TypeError("a delta shape is expected, not %s" % type(s).__name__)
-    device, inp, out = _current_device(), _TORCH.get(s.in_dtype), _TORCH.get(s.out_dtype)
-    rows = s.B * s.N
-    _matches(name, device, {"q": q, "k": k}, inp, rows * s.Hk * s.d)
-    _matches(name, device, {"v": v, **dict(more_in)}, inp, rows * s.H * s.e)
-    _matches(name, device, {"g": g, "beta": beta, **gates}, torch.float32, rows * s.H)
-    _matches(name, device, outs, out, rows * s.H * s.e)
-    if qk_outs:
-        _matches(name, device, qk_outs, out, rows * s.Hk * s.d)
-    _matches(name, device, states, torch.float32, s.B * s.H * s.d * s.e)
-    for w in workspaces:
-        if w is not None and w.get_device() != device:
-            raise ValueError("%s: workspaces have to be on the current CUDA device" % name)
-
-
 def la_delta_fwd(shape: LaDeltaShape, q, k, v, g, beta, o, kv_in=None, kv_out=None, workspace=None, stream=None):
     """Gated delta rule over all tokens: q, k have shape.Hk heads, v and o shape.H; g (log decay) and beta are fp32, one per token and
     value head, in the layout of v without its features."""
-    _delta_checks("la_delta_fwd", shape, q, k, v, g, beta, {"o": o}, None, {}, {"kv_in": kv_in, "kv_out": kv_out}, (workspace,))
-    _enter("la_delta_fwd", "dtttttttttir", shape, q, k, v, g, beta, o, kv_in, kv_out, workspace, _bytes(workspace), stream)
+    _enter("la_delta_fwd", "dQQVGGOSSwir", shape, q, k, v, g, beta, o, kv_in, kv_out, workspace, _bytes(workspace), stream)
 
 
 def la_delta_bwd(shape: LaDeltaShape, q, k, v, g, beta, do, dq, dk, dv, dg, dbeta, kv_in=None, grad_kv_out=None, grad_kv_in=None,
                  workspace=None, stream=None, fwd_workspace=None):
     """fwd_workspace: the workspace of the matching la_delta_fwd call, whose contents are otherwise made again."""
-    _delta_checks("la_delta_bwd", shape, q, k, v, g, beta, {"dv": dv}, {"dq": dq, "dk": dk}, {"dg": dg, "dbeta": dbeta},
-                  {"kv_in": kv_in, "grad_kv_out": grad_kv_out, "grad_kv_in": grad_kv_in}, (workspace, fwd_workspace), {"do": do})
+    if type(shape) is not LaDeltaShape:
+        raise TypeError("a delta shape is expected, not %s" % type(shape).__name__)
     if fwd_workspace is not None and _bytes(fwd_workspace) < delta_workspace_bytes(LA_OP_FWD, shape):
         raise LaError(3, "la_delta_bwd (fwd_workspace)")
-    _enter("la_delta_bwd", "dttttttttttttttttir", shape, q, k, v, g, beta, do, dq, dk, dv, dg, dbeta, kv_in, grad_kv_out, grad_kv_in,
+    _enter("la_delta_bwd", "dQQVGGVPPOGGSSSwwir", shape, q, k, v, g, beta, do, dq, dk, dv, dg, dbeta, kv_in, grad_kv_out, grad_kv_in,
            fwd_workspace, workspace, _bytes(workspace), stream)
 
 
 def la_delta_steps(shape: LaDeltaShape, q, k, v, g, beta, kv, o, stream=None):
     """shape.N consecutive tokens on the state kv, updated in place: decoding."""
-    _delta_checks("la_delta_steps", shape, q, k, v, g, beta, {"o": o}, None, {}, {"kv": kv}, ())
-    _enter("la_delta_steps", "dtttttttr", shape, q, k, v, g, beta, kv, o, stream)
+    _enter("la_delta_steps", "dQQVGGSOr", shape, q, k, v, g, beta, kv, o, stream)
 
 
 def make_block_norm_shape(rows, D, dtype, res_dtype, eps=0.0, gate=LA_GATE_PLAIN, post_norm=True) -> LaBlockNormShape:
@@ -492,29 +458,15 @@ def alloc_block_norm_workspace(shape: LaBlockNormShape, device) -> torch.Tensor:
     return torch.empty(block_norm_workspace_bytes(shape), dtype=torch.uint8, device=device)
 
 
-def _norm_checks(name, s, rows, res_rows, weights, workspace=None):
-    if type(s) is not LaBlockNormShape:
-        raise TypeError("a block norm shape is expected, not %s" % type(s).__name__)
-    device = _current_device()
-    _matches(name, device, rows, _TORCH.get(s.dtype), s.rows * s.D)
-    _matches(name, device, res_rows, _TORCH.get(s.res_dtype), s.rows * s.D)
-    _matches(name, device, weights, torch.float32, s.D)
-    if workspace is not None and workspace.get_device() != device:
-        raise ValueError("%s: the workspace has to be on the current CUDA device" % name)
-
-
 def la_block_norm_fwd(shape: LaBlockNormShape, x, y, u=None, w_post=None, s=None, w_pre=None, h=None, n=None, stream=None):
     """h = x + s (.) norm(y) (.) w_post (.) act(u), n = norm(h) (.) w_pre: norm and gate of a block's output y, the residual stream x
     and h, the next block's input n."""
-    _norm_checks("la_block_norm_fwd", shape, {"y": y, "u": u, "n": n}, {"x": x, "h": h}, {"w_post": w_post, "s": s, "w_pre": w_pre})
-    _enter("la_block_norm_fwd", "nttttttttr", shape, x, y, u, w_post, s, w_pre, h, n, stream)
+    _enter("la_block_norm_fwd", "nXYYFFFXYr", shape, x, y, u, w_post, s, w_pre, h, n, stream)
 
 
 def la_block_norm_bwd(shape: LaBlockNormShape, x, y, u, w_post, s, w_pre, dh, dn, dx, dy, du=None, dw_post=None, ds=None, dw_pre=None,
                       workspace=None, stream=None):
-    _norm_checks("la_block_norm_bwd", shape, {"y": y, "u": u, "dn": dn, "dy": dy, "du": du}, {"x": x, "dh": dh, "dx": dx},
-                 {"w_post": w_post, "s": s, "w_pre": w_pre, "dw_post": dw_post, "ds": ds, "dw_pre": dw_pre}, workspace)
-    _enter("la_block_norm_bwd", "ntttttttttttttttir", shape, x, y, u, w_post, s, w_pre, dh, dn, dx, dy, du, dw_post, ds, dw_pre,
+    _enter("la_block_norm_bwd", "nXYYFFFXYXYYFFFwir", shape, x, y, u, w_post, s, w_pre, dh, dn, dx, dy, du, dw_post, ds, dw_pre,
            workspace, _bytes(workspace), stream)
 
 

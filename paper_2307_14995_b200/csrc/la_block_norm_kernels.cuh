@@ -292,8 +292,8 @@ __global__ void __launch_bounds__(LANES > THREADS ? LANES : THREADS) block_norm_
 // The same with the rows of a thread block's next turns on their way while it works on one: every thread copies what it will read
 // itself into a ring of S stages in shared memory (cp.async), so that nobody waits for anybody but in the row sums.  One thread block
 // of 512 threads to an SM, 512 / LANES rows at a time, each row's threads with a barrier of their own; weights in shared memory,
-// sums over tokens in registers to the end.  65536 x 4096 in bf16, forward and backward, us: the kernels above 740 and 4282, this one 452 and
-// 1194 (409 and 654 at the copy bandwidth).
+// sums over tokens in registers to the end.  65536 x 4096 in bf16, forward and backward, us: the kernels above 740 and 4282, this one 430 and
+// 1024 (409 and 654 at the copy bandwidth).
 //
 // Rows whose width is no multiple of eight move in pairs of features, 4 bytes of bf16: where the width is odd a row begins in the middle
 // of a pair, every second one, and a group of threads takes rows of one kind only, so that a thread's features are the same in all.
@@ -377,11 +377,14 @@ struct RingRow {
       if (f + 1 < D) at[f + 1] = from_f32<T>(x[1]);
     }
   }
-  __device__ __forceinline__ void weights(const float* w, int u, float (&x)[F]) const {  // [D] in shared memory, with a margin of 16
+  // [D] in shared memory, with a margin; VEC: the first four of every eight features, then the others, so that neighbours read without
+  // conflicts (weight_at: where feature f is)
+  static __device__ __forceinline__ int weight_at(int f, int D) { return VEC ? (f & 4 ? D / 2 : 0) + (f >> 3) * 4 + (f & 3) : f; }
+  __device__ __forceinline__ void weights(const float* w, int u, float (&x)[F]) const {
     const int f = feature(u);
     if constexpr (VEC) {
-      const int at = f < D ? f : 0;
-      const float4 a = *reinterpret_cast<const float4*>(w + at), b = *reinterpret_cast<const float4*>(w + at + 4);
+      const int at = f < D ? f / 2 : 0;
+      const float4 a = *reinterpret_cast<const float4*>(w + at), b = *reinterpret_cast<const float4*>(w + D / 2 + at);
       x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
     } else {
       x[0] = w[f >= 0 && f < D ? f : 0];
@@ -414,6 +417,16 @@ struct RowSums {
     slot ^= 1;  // (written again behind the next sum's barrier)
   }
 };
+
+template <int F>
+__device__ __forceinline__ uint64_t pair(const float (&x)[F], int i) { return f2_pack(x[i], x[i + 1]); }
+template <int F>
+__device__ __forceinline__ void unpair(uint64_t v, float (&x)[F], int i) { f2_unpack(v, x[i], x[i + 1]); }
+__device__ __forceinline__ float pair_sum(uint64_t v) {
+  float a, b;
+  f2_unpack(v, a, b);
+  return a + b;
+}
 
 // 1 / (1 + exp(-u)), exp and the reciprocal good to an ulp or two (relative 2^-22); where exp is infinite it is 0.
 __device__ __forceinline__ float sigmoid(float u) {
@@ -470,10 +483,11 @@ __global__ void __launch_bounds__(RING, 1) block_norm_ring_kernel(const BlockNor
   const int wd = (a.D + 19) / 4 * 4;
   float *const w_s = w_post + wd, *const w_pre = w_s + wd;
   for (int i = threadIdx.x; i < S * stage_bytes / 16; i += RING) reinterpret_cast<uint4*>(ring)[i] = make_uint4(0u, 0u, 0u, 0u);  // units past the end stay zeros
-  for (int i = threadIdx.x; i < wd; i += RING) {
-    w_post[i] = a.w_post && i < a.D ? a.w_post[i] : 1.f;
-    w_s[i] = a.s && i < a.D ? a.s[i] : 1.f;
-    w_pre[i] = a.w_pre && i < a.D ? a.w_pre[i] : 1.f;
+  for (int i = threadIdx.x; i < a.D; i += RING) {
+    const int at = Row::weight_at(i, a.D);
+    w_post[at] = a.w_post ? a.w_post[i] : 1.f;
+    w_s[at] = a.s ? a.s[i] : 1.f;
+    w_pre[at] = a.w_pre ? a.w_pre[i] : 1.f;
   }
   __syncthreads();
   const int sub = threadIdx.x / LANES;
@@ -532,7 +546,7 @@ __global__ void __launch_bounds__(RING, 1) block_norm_ring_kernel(const BlockNor
         ry = inverse_rms(ss[0], inv_d, a.eps);
       }
     }
-    float both[2] = {0.f, 0.f};  // of h squared, of w_pre dn h
+    uint64_t sum_h = 0, sum_n = 0;  // of h squared, of w_pre dn h, two at a time
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       float x[F], w[F], sc[F];
@@ -541,19 +555,25 @@ __global__ void __launch_bounds__(RING, 1) block_norm_ring_kernel(const BlockNor
       get_gate(u);
       my.weights(w_post, u, w);
       my.weights(w_s, u, sc);
+      const uint64_t ry2 = f2_pack(ry, ry);
 #pragma unroll
-      for (int i = 0; i < F; ++i) {
-        h[u][i] = fmaf(sc[i], y[u][i] * ry * w[i] * g[u][i], x[i]);
-        both[0] = fmaf(h[u][i], h[u][i], both[0]);
+      for (int i = 0; i < F; i += 2) {
+        const uint64_t z = f2_mul(f2_mul(f2_mul(pair(y[u], i), ry2), pair(w, i)), pair(g[u], i));
+        const uint64_t v = f2_fma(pair(sc, i), z, pair(x, i));
+        unpair(v, h[u], i);
+        sum_h = f2_fma(v, v, sum_h);
       }
       if (BWD) {
         my.template get<T>(in + at_dn, u, dn[u]);
         my.weights(w_pre, u, w);
 #pragma unroll
-        for (int i = 0; i < F; ++i) both[1] = fmaf(dn[u][i] * w[i], h[u][i], both[1]);
+        for (int i = 0; i < F; i += 2) sum_n = f2_fma(f2_mul(pair(dn[u], i), pair(w, i)), pair(h[u], i), sum_n);
       }
       if (!BWD && a.h) my.put(static_cast<TR*>(a.h), row, u, h[u]);
     }
+    float both[2];
+    both[0] = pair_sum(sum_h);
+    both[1] = pair_sum(sum_n);
     if (!BWD) {
       fetch(row + S * step, s);
       if (a.n) {
@@ -570,7 +590,8 @@ __global__ void __launch_bounds__(RING, 1) block_norm_ring_kernel(const BlockNor
         }
       }
     } else {
-      float rh = 0.f, along = 0.f, py[1] = {0.f};
+      float rh = 0.f, along = 0.f, py[1];
+      uint64_t sum_p = 0;
       if (a.dn) {
         sums(both, slot);
         rh = inverse_rms(both[0], inv_d, a.eps);
@@ -586,34 +607,38 @@ __global__ void __launch_bounds__(RING, 1) block_norm_ring_kernel(const BlockNor
         }
         my.template get<TR>(in + at_dh, u, dh);
         my.weights(w_pre, u, w);
+        const uint64_t rh2 = f2_pack(rh, rh), along2 = f2_pack(-along, -along), ry2 = f2_pack(ry, ry);
 #pragma unroll
-        for (int i = 0; i < F; ++i) {
-          const float nh = h[u][i] * rh;
-          dh[i] = fmaf(rh, fmaf(-nh, along, dn[u][i] * w[i]), dh[i]);  // H
-          g_pre[u][i] = fmaf(dn[u][i], nh, g_pre[u][i]);
+        for (int i = 0; i < F; i += 2) {
+          const uint64_t nh = f2_mul(pair(h[u], i), rh2), n = pair(dn[u], i);
+          unpair(f2_fma(rh2, f2_fma(nh, along2, f2_mul(n, pair(w, i))), pair(dh, i)), dh, i);  // H
+          unpair(f2_fma(n, nh, pair(g_pre[u], i)), g_pre[u], i);
         }
         my.put(static_cast<TR*>(a.dx), row, u, dh);
         my.weights(w_post, u, w);
         my.weights(w_s, u, sc);
 #pragma unroll
-        for (int i = 0; i < F; ++i) {
-          const float yh = y[u][i] * ry, Hg = dh[i] * g[u][i], Hsg = Hg * sc[i], yw = yh * w[i];
-          g_s[u][i] = fmaf(Hg, yw, g_s[u][i]);
-          g_post[u][i] = fmaf(Hsg, yh, g_post[u][i]);
-          slope[u][i] *= dh[i] * sc[i] * yw;  // du
-          h[u][i] = Hsg * w[i];               // p
-          py[0] = fmaf(h[u][i], yh, py[0]);
+        for (int i = 0; i < F; i += 2) {
+          const uint64_t yh = f2_mul(pair(y[u], i), ry2), H = pair(dh, i), Hg = f2_mul(H, pair(g[u], i)), ws = pair(w, i), yw = f2_mul(yh, ws);
+          const uint64_t Hsg = f2_mul(Hg, pair(sc, i)), p = f2_mul(Hsg, ws);
+          unpair(f2_fma(Hg, yw, pair(g_s[u], i)), g_s[u], i);
+          unpair(f2_fma(Hsg, yh, pair(g_post[u], i)), g_post[u], i);
+          if (a.u) unpair(f2_mul(f2_mul(f2_mul(H, pair(sc, i)), yw), pair(slope[u], i)), slope[u], i);  // du
+          unpair(p, h[u], i);
+          sum_p = f2_fma(p, yh, sum_p);
         }
         if (a.u) my.put(static_cast<T*>(a.du), row, u, slope[u]);
       }
       if (KEEP) fetch(row + S * step, s);
+      py[0] = pair_sum(sum_p);
       if (a.post_norm) sums(py, slot);
       const float along_y = a.post_norm ? py[0] * inv_d * ry : 0.f;
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         if (!KEEP) get_y(u);
+        const uint64_t ry2 = f2_pack(ry, ry), along2 = f2_pack(-along_y, -along_y);
 #pragma unroll
-        for (int i = 0; i < F; ++i) h[u][i] = ry * fmaf(-y[u][i], along_y, h[u][i]);
+        for (int i = 0; i < F; i += 2) unpair(f2_mul(ry2, f2_fma(pair(y[u], i), along2, pair(h[u], i))), h[u], i);
         my.put(static_cast<T*>(a.dy), row, u, h[u]);
       }
       if (!KEEP) fetch(row + S * step, s);

@@ -8,6 +8,13 @@
 //   s  shape         the address of a structure of the type given to bind
 //   d  delta shape   the same of the type for the gated delta rule
 //   n  norm shape    the same of the type for the norms between two blocks
+// Behind a delta shape or a norm shape, tensors of a type and a number of elements that follow from it, on the current device; their gates,
+// weights and shared heads make it easy to hand over another one, which would be read out of bounds:
+//   Q  q, k          P  dq, dk      (B N Hk d, of in_dtype or out_dtype)
+//   V  v, d_o        O  o, dv       (B N H e, likewise)
+//   G  fp32, one for each token and value head      S  fp32, a state for each value head
+//   X  rows of the residual stream   Y  the other rows   F  fp32, one for each feature
+//   w  any tensor on the current device
 //   h  host memory   the address of a ctypes array, or the address itself
 //   r  stream        what the function given to bind makes of it, asked when the arguments before it have been accepted
 // A decode step spends longer in argument conversion than its kernel runs: through ctypes and Python-level checks a call costs
@@ -18,7 +25,18 @@
 
 #define MAX_ARGS 24
 
-static PyObject *s_is_cuda, *s_is_contiguous, *s_data_ptr, *stream_of;
+static PyObject *s_is_cuda, *s_is_contiguous, *s_data_ptr, *s_dtype, *s_numel, *s_get_device, *stream_of, *device_of, *dtypes[2];
+
+// include/la.h
+typedef struct {
+  int B, H, Hk, N, d, e, in_dtype, out_dtype, path, layout;
+  float scale;
+} DeltaShape;
+typedef struct {
+  long long rows;
+  int D, dtype, res_dtype, gate, post_norm;
+  float eps;
+} NormShape;
 static PyTypeObject *shape_type, *delta_type, *norm_type, *ctypes_array;
 
 // 1: *out holds the slot; 0: an exception is set.
@@ -80,6 +98,66 @@ static int slot(char kind, PyObject* a, uint64_t* out) {
   return !(*out == (uint64_t)-1 && PyErr_Occurred());
 }
 
+// The type (0: bf16, 1: fp32; anything else: any) and the number of elements (-1: any) that a letter stands for.
+static void expected(char kind, const void* shape, int is_norm, int* dtype, long long* count) {
+  *dtype = -1;
+  *count = -1;
+  if (kind == 'w' || !shape) return;
+  if (is_norm) {
+    const NormShape* const s = (const NormShape*)shape;
+    *dtype = kind == 'X' ? s->res_dtype : kind == 'Y' ? s->dtype : 1;
+    *count = kind == 'F' ? s->D : s->rows * s->D;
+    return;
+  }
+  const DeltaShape* const s = (const DeltaShape*)shape;
+  const long long rows = (long long)s->B * s->N;
+  *dtype = kind == 'Q' || kind == 'V' ? s->in_dtype : kind == 'P' || kind == 'O' ? s->out_dtype : 1;
+  *count = kind == 'Q' || kind == 'P' ? rows * s->Hk * s->d : kind == 'V' || kind == 'O' ? rows * s->H * s->e
+         : kind == 'G' ? rows * s->H : (long long)s->B * s->H * s->d * s->e;
+}
+
+static int as_long(PyObject* x, long long* out) {  // takes the reference
+  if (!x) return 0;
+  *out = PyLong_AsLongLong(x);
+  Py_DECREF(x);
+  return !(*out == -1 && PyErr_Occurred());
+}
+
+static int checked(char kind, Py_ssize_t index, PyObject* a, const void* shape, int is_norm, long long device, uint64_t* out) {
+  *out = 0;
+  if (a == Py_None) return 1;
+  int dtype;
+  long long count, at, n;
+  expected(kind, shape, is_norm, &dtype, &count);
+  PyObject* x = PyObject_GetAttr(a, s_dtype);
+  if (!x) return 0;
+  const int typed = dtype < 0 || (dtype <= 1 && x == dtypes[dtype]);
+  Py_DECREF(x);
+  if (!as_long(PyObject_CallMethodNoArgs(a, s_numel), &n) || !as_long(PyObject_CallMethodNoArgs(a, s_get_device), &at)) return 0;
+  if (!typed || (count >= 0 && n != count)) {
+    PyErr_Format(PyExc_ValueError, "argument %zd has to be %S with %lld elements", index, dtype == 0 || dtype == 1 ? dtypes[dtype] : Py_None, count);
+    return 0;
+  }
+  if (at != device) {
+    PyErr_Format(PyExc_ValueError, "argument %zd has to be on the current CUDA device", index);
+    return 0;
+  }
+  x = PyObject_CallMethodNoArgs(a, s_is_contiguous);
+  if (!x) return 0;
+  const int ok = PyObject_IsTrue(x);
+  Py_DECREF(x);
+  if (ok < 0) return 0;
+  if (!ok) {
+    PyErr_Format(PyExc_ValueError, "argument %zd has to be contiguous", index);
+    return 0;
+  }
+  x = PyObject_CallMethodNoArgs(a, s_data_ptr);
+  if (!x) return 0;
+  *out = PyLong_AsUnsignedLongLong(x);
+  Py_DECREF(x);
+  return !(*out == (uint64_t)-1 && PyErr_Occurred());
+}
+
 typedef int (*Fn)(uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t,
                   uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t);
 
@@ -94,8 +172,21 @@ static PyObject* call(PyObject* self, PyObject* const* args, Py_ssize_t n) {
   }
   uint64_t a[MAX_ARGS] = {0}, fn;
   if (!slot('i', args[0], &fn)) return NULL;
-  for (Py_ssize_t i = 0; i < kinds_n; ++i)
-    if (!slot(kinds[i], args[2 + i], &a[i])) return NULL;
+  const void* shape = NULL;
+  long long device = -2;
+  for (Py_ssize_t i = 0; i < kinds_n; ++i) {
+    const char kind = kinds[i];
+    if (kind == 'w' || (kind >= 'A' && kind <= 'Z')) {
+      if (device == -2 && (!device_of || !as_long(PyObject_CallNoArgs(device_of), &device))) {
+        if (!PyErr_Occurred()) PyErr_SetString(PyExc_RuntimeError, "bind has not been called");
+        return NULL;
+      }
+      if (!checked(kind, i, args[2 + i], shape, kinds[0] == 'n', device, &a[i])) return NULL;
+      continue;
+    }
+    if (!slot(kind, args[2 + i], &a[i])) return NULL;
+    if (kind == 'd' || kind == 'n') shape = (const void*)(uintptr_t)a[i];
+  }
   int rc;
   Py_BEGIN_ALLOW_THREADS;
   rc = ((Fn)(uintptr_t)fn)(a[0], a[1], a[2], a[3], a[4], a[5], a[6], a[7], a[8], a[9], a[10], a[11], a[12], a[13], a[14], a[15], a[16], a[17],
@@ -106,8 +197,14 @@ static PyObject* call(PyObject* self, PyObject* const* args, Py_ssize_t n) {
 
 static PyObject* bind(PyObject* self, PyObject* args) {
   (void)self;
-  PyObject *type, *f, *delta, *norm;
-  if (!PyArg_ParseTuple(args, "O!OO!O!", &PyType_Type, &type, &f, &PyType_Type, &delta, &PyType_Type, &norm)) return NULL;
+  PyObject *type, *f, *delta, *norm, *device, *bf16, *f32;
+  if (!PyArg_ParseTuple(args, "O!OO!O!OOO", &PyType_Type, &type, &f, &PyType_Type, &delta, &PyType_Type, &norm, &device, &bf16, &f32)) return NULL;
+  Py_INCREF(device);
+  Py_XSETREF(device_of, device);
+  Py_INCREF(bf16);
+  Py_XSETREF(dtypes[0], bf16);
+  Py_INCREF(f32);
+  Py_XSETREF(dtypes[1], f32);
   Py_INCREF(type);
   Py_XSETREF(shape_type, (PyTypeObject*)type);
   Py_INCREF(delta);
@@ -119,7 +216,7 @@ static PyObject* bind(PyObject* self, PyObject* args) {
   Py_RETURN_NONE;
 }
 
-static PyMethodDef methods[] = {{"bind", bind, METH_VARARGS, "bind(type of a shape, function that gives a stream's handle, types of a delta shape and of a norm shape)"},
+static PyMethodDef methods[] = {{"bind", bind, METH_VARARGS, "bind(type of a shape, function that gives a stream's handle, types of a delta shape and of a norm shape, function that gives the current device, torch.bfloat16, torch.float32)"},
                                 {"call", (PyCFunction)(void (*)(void))call, METH_FASTCALL, "call(address, kinds, arg, ...) -> status"},
                                 {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_la_call", NULL, -1, methods, NULL, NULL, NULL, NULL};
@@ -128,7 +225,10 @@ PyMODINIT_FUNC PyInit__la_call(void) {
   s_is_cuda = PyUnicode_InternFromString("is_cuda");
   s_is_contiguous = PyUnicode_InternFromString("is_contiguous");
   s_data_ptr = PyUnicode_InternFromString("data_ptr");
-  if (!s_is_cuda || !s_is_contiguous || !s_data_ptr) return NULL;
+  s_dtype = PyUnicode_InternFromString("dtype");
+  s_numel = PyUnicode_InternFromString("numel");
+  s_get_device = PyUnicode_InternFromString("get_device");
+  if (!s_is_cuda || !s_is_contiguous || !s_data_ptr || !s_dtype || !s_numel || !s_get_device) return NULL;
   PyObject* const ctypes = PyImport_ImportModule("ctypes");
   if (!ctypes) return NULL;
   ctypes_array = (PyTypeObject*)PyObject_GetAttrString(ctypes, "Array");

@@ -24,6 +24,7 @@ struct Record {
 template <int M, int N, typename FA, typename FB>
 __device__ __forceinline__ void product(float (&acc)[M / 16][N / 16], int K, FA a, FB b) {
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+#pragma unroll 4
   for (int k = 0; k < K; ++k) {
     float x[M / 16], y[N / 16];
 #pragma unroll

@@ -20,7 +20,8 @@
 // operands leave out lo x lo.  Sums are fp32, in an order that depends on the shape alone.
 //
 // Operands in shared memory and in the workspace are images: rows of 128 bytes (64 elements) in the 128-byte swizzle, panel after panel of
-// 64 columns, all panels of hi and then those of lo; one image serves K-major and MN-major.  They move by untiled bulk copies.
+// 64 columns, all panels of hi and then those of lo; one image serves K-major and MN-major.  They move by untiled bulk copies.  States are
+// slices of 32 value columns, a panel each: [hi | lo] of the 32 columns, which is the operand of the chain's thread block that made them.
 //
 // Every kernel waits for its predecessor before it does anything (its tensor memory included), and every wait inside is bounded: X_WAIT
 // makes the outcome the same for all threads of the block, which then drain what is in flight, free tensor memory and return.
@@ -759,20 +760,20 @@ x_chain_kernel(const __grid_constant__ XChainArgs a) {
     int par = 0;
     for (int i = 0; i < a.nchunk; ++i) {
       if (owner) {
-        unsigned char* const image = a.image + index(i) * a.image_stride;
 #pragma unroll
         for (int c = 0; c < V / 8; ++c) {
           uint4 h, l;
           split8(&s[8 * c], h, l);
-          const int col = half * (V / 8) + c;  // 16-byte group of the slice
+          const int col = (half * V / 32) * 8 + half * V % 32 / 8 + c;  // 16-byte group, the lo terms four further
           *reinterpret_cast<uint4*>(sm.b + image_at(row, col, D)) = h;
-          *reinterpret_cast<uint4*>(sm.b + image_at(row, NE / 8 + col, D)) = l;
-          const uint32_t at = image_at(row, e0 / 8 + col, D);
-          *reinterpret_cast<uint4*>(image + at) = h;
-          *reinterpret_cast<uint4*>(image + D * D * 2 + at) = l;
+          *reinterpret_cast<uint4*>(sm.b + image_at(row, col + 4, D)) = l;
         }
       }
       X_HAND_OVER();
+      if (tid == 0) {
+        bulk_store(a.image + index(i) * a.image_stride + (size_t)e0 * D * 4, sm.b, NE * D * 4);
+        tma_store_commit();
+      }
       if (warp == 0) {
         const int st = i % XC_STAGES;
         const bool ok = wait_or_abort(&sm.bars[XC_LOAD0 + st], (i / XC_STAGES) & 1, &sm.abort);
@@ -782,7 +783,7 @@ x_chain_kernel(const __grid_constant__ XChainArgs a) {
           const uint32_t b = mnmaj(sm.b, D * 128);
           if (D == 128) {
             umma_group_ss<8, !REV, false>(tmem, REV ? mnmaj(m) : kmaj(m), b, XHI, ID2, 0, go);
-            umma_group_ss<8, !REV, false>(tmem, REV ? mnmaj(m + 32768) : kmaj(m + 32768), b, XHI, ID1, 1, go);
+            umma_group_ss<8, !REV, false>(tmem, REV ? mnmaj(m + 32768) : kmaj(m + 32768), b, XHI, NE == 32 ? ID1 : ID2, 1, go);
           } else {
             umma_group_ss<4, !REV, false>(tmem, REV ? mnmaj(m, 8192) : kmaj(m), b, XHI, ID2, 0, go);
           }
@@ -796,21 +797,24 @@ x_chain_kernel(const __grid_constant__ XChainArgs a) {
       if (owner && i + 1 < a.nchunk) fetch(i + 1, next, next_all);
       X_WAIT(sm.bars[XC_MMA], par, 61);
       par ^= 1;
-      if (tid == 0 && i + XC_STAGES < a.nchunk) load_m(i + XC_STAGES);
+      if (tid == 0) {
+        if (i + XC_STAGES < a.nchunk) load_m(i + XC_STAGES);
+        tma_store_wait_read();  // (before the barrier that lets the next operand be written: D = 64 the one below, else the next turn's)
+      }
       __syncwarp();
       uint32_t d0[V], d1[V];
       if (V == 16) {
         tmem_ld_x16(tmem + mine + half * V, *reinterpret_cast<uint32_t(*)[16]>(d0));
-        tmem_ld_x16(tmem + mine + NE + half * V, *reinterpret_cast<uint32_t(*)[16]>(d1));
+        tmem_ld_x16(tmem + mine + 32 + half * V, *reinterpret_cast<uint32_t(*)[16]>(d1));
       } else {
-        tmem_ld_x32(tmem + mine + half * V, *reinterpret_cast<uint32_t(*)[32]>(d0));
-        tmem_ld_x32(tmem + mine + NE + half * V, *reinterpret_cast<uint32_t(*)[32]>(d1));
+        tmem_ld_x32(tmem + mine + half * 64, *reinterpret_cast<uint32_t(*)[32]>(d0));
+        tmem_ld_x32(tmem + mine + half * 64 + 32, *reinterpret_cast<uint32_t(*)[32]>(d1));
       }
       tmem_ld_wait();
       if constexpr (D == 64) {
         if (!owner)
 #pragma unroll
-          for (int x = 0; x < V; ++x) sm.other[row - 64][half * V + x] = __uint_as_float(d0[x]);
+          for (int x = 0; x < V; ++x) sm.other[row - 64][half * V + x] = __uint_as_float(d0[x]) + __uint_as_float(d1[x]);
         __syncthreads();
       }
       if (owner) {
@@ -902,6 +906,15 @@ __device__ __forceinline__ void load_both(uint32_t taddr, float (&x)[32]) {
   for (int i = 0; i < 32; ++i) x[i] += y[i];
 }
 
+// The same of a product with a state's slices [hi | lo], 32 columns each: the 32 of slice s
+__device__ __forceinline__ void load_slice(uint32_t taddr, int s, float (&x)[32]) {
+  float y[32];
+  load_acc(taddr + 64 * s, x);
+  load_acc(taddr + 64 * s + 32, y);
+#pragma unroll
+  for (int i = 0; i < 32; ++i) x[i] += y[i];
+}
+
 template <int D, typename TO>
 __global__ void __launch_bounds__(256, 2)
 x_output_kernel(const __grid_constant__ XMaps maps, const __grid_constant__ DeltaArgs a) {
@@ -920,8 +933,7 @@ x_output_kernel(const __grid_constant__ XMaps maps, const __grid_constant__ Delt
       bulk_load(&sm.gates, rec + Rec::GATES, 2560, bar);
       for (int x = 0; x < PANELS; ++x) tma_load_4d(sm.qk + x * 16384, &maps.q, bar, x * 64, c * 128, p.hk, p.b);
       for (int x = 0; x < PANELS; ++x) tma_load_4d(sm.qk + 32768 + x * 16384, &maps.k, bar, x * 64, c * 128, p.hk, p.b);
-      bulk_load(sm.s, rec + Rec::S + eh * D * 128, D * 128, bar);
-      bulk_load(sm.s + D * 128, rec + Rec::S + D * D * 2 + eh * D * 128, D * 128, bar);
+      bulk_load(sm.s, rec + Rec::S + eh * 2 * D * 128, 2 * D * 128, bar);
       prefetch(rec + Rec::X, 65536);
       unsigned nx, ny;
       if (later_block(296, nx, ny) && nx % PANELS == 0) {
@@ -950,7 +962,7 @@ x_output_kernel(const __grid_constant__ XMaps maps, const __grid_constant__ Delt
     if (tid == 0) bulk_load(sm.qk, rec + Rec::X, 65536, expect(sm, XO_X, 65536));
     {
       float x[32];
-      load_both(tmem + mine + half * 32, x);
+      load_slice(tmem + mine, half, x);
       each32(raw, [&](int i, float v) { x[i] = fmaf(-since, x[i], v); });
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -969,7 +981,7 @@ x_output_kernel(const __grid_constant__ XMaps maps, const __grid_constant__ Delt
       umma_commit_if(&sm.bars[XO_MMA], go);
     }
     float v[32];
-    load_both(tmem + 128 + mine + half * 32, v);
+    load_slice(tmem + 128 + mine, half, v);
 #pragma unroll
     for (int i = 0; i < 32; ++i) v[i] *= a.scale * since;
     X_WAIT(sm.bars[XO_MMA], 1, 73);
@@ -1145,8 +1157,7 @@ x_values_kernel(const __grid_constant__ XMaps maps, const __grid_constant__ Delt
       bulk_load(&sm.gates, fwd + Rec::GATES, 2560, bar);
       for (int x = 0; x < PANELS; ++x) tma_load_4d(sm.u + x * 16384, &maps.k, bar, x * 64, c * 128, p.hk, p.b);
       const unsigned char* const state = grad ? bwd + Rec::E : fwd + Rec::S;
-      bulk_load(sm.s, state + eh * D * 128, D * 128, bar);
-      bulk_load(sm.s + D * 128, state + D * D * 2 + eh * D * 128, D * 128, bar);
+      bulk_load(sm.s, state + eh * 2 * D * 128, 2 * D * 128, bar);
       unsigned nx, ny;
       if (later_block(296, nx, ny) && nx % (2 * PANELS) == 0) {
         const XPlace o = x_place(a, ny, nx / (2 * PANELS));
@@ -1197,7 +1208,7 @@ x_values_kernel(const __grid_constant__ XMaps maps, const __grid_constant__ Delt
         *reinterpret_cast<uint4*>(sm.s + 16384 + at) = l;
       }
     };
-    load_both(tmem + mine + half * 32, x);
+    load_slice(tmem + mine, half, x);
 #pragma unroll
     for (int i = 0; i < 32; ++i) x[i] = grad ? times * x[i] : fmaf(times, x[i], add[i]);
     put();
@@ -1303,6 +1314,15 @@ __device__ __forceinline__ float prefix_sum_before(float x, int lane) {
   const float y = __shfl_up_sync(0xffffffffu, x, 1);
   return lane == 0 ? 0.f : y;
 }
+// D[tokens, features] (+)= A[tokens, e] S[features, e]^T over the e columns of a state's slices: A K-major panels of 64 columns, terms: 0 for the
+// state's hi terms, 4 (16-byte groups) for the lo terms
+template <int D>
+__device__ __forceinline__ void state_product(uint32_t d, uint32_t a, uint32_t b, uint32_t terms, uint32_t idesc, uint32_t acc, uint32_t go) {
+#pragma unroll
+  for (int k = 0; k < D / 16; ++k)
+    umma_ss(d, a + umma_kstep<true>(k), b + (k >> 1) * (D * 8) + (k & 1) * 2 + terms, XHI, idesc, k > 0 || acc, go);
+}
+
 template <int D, typename TO>
 __global__ void __launch_bounds__(512, 1)
 x_gradient_kernel(const __grid_constant__ XMaps maps, const __grid_constant__ DeltaArgs a) {
@@ -1345,11 +1365,11 @@ x_gradient_kernel(const __grid_constant__ XMaps maps, const __grid_constant__ De
       X_WAIT(sm.bars[XG_LOAD], second, 101);
       // ---- what the states have ----
       if (warp == 0) {
-        umma_group_ss<NK, true, true>(T0, kmaj(sm.o), kmaj(sm.a), XHI, ID_ST, 0, go);
-        umma_group_ss<NK, true, true>(T0, kmaj(sm.o), kmaj(sm.a + D * D * 2), XHI, ID_ST, 1, go);
-        umma_group_ss<NK, true, true>(T1, kmaj(sm.s), kmaj(sm.a), XHI, ID_ST, 0, go);
-        umma_group_ss<NK, true, true>(T1, kmaj(sm.s), kmaj(sm.a + D * D * 2), XHI, ID_ST, 1, go);
-        umma_group_ss<NK, true, true>(T1, kmaj(sm.s + TOK), kmaj(sm.a), XHI, ID_ST, 1, go);
+        state_product<D>(T0, kmaj(sm.o), kmaj(sm.a), 0, ID_ST, 0, go);
+        state_product<D>(T0, kmaj(sm.o), kmaj(sm.a), 4, ID_ST, 1, go);
+        state_product<D>(T1, kmaj(sm.s), kmaj(sm.a), 0, ID_ST, 0, go);
+        state_product<D>(T1, kmaj(sm.s), kmaj(sm.a), 4, ID_ST, 1, go);
+        state_product<D>(T1, kmaj(sm.s + TOK), kmaj(sm.a), 0, ID_ST, 1, go);
         umma_commit_if(&sm.bars[XG_MMA], go);
       }
       if (tid == 0) {
@@ -1370,20 +1390,24 @@ x_gradient_kernel(const __grid_constant__ XMaps maps, const __grid_constant__ De
       const float2 own = sm.sum[row];
       const float since = ex2_approx(own.x + own.y), until = decay2(end, own);
       constexpr int IT = D * D / 8 / 512;
+      auto part_at = [&](int n) {  // eight columns of a row (hi terms; the lo terms are four groups further)
+        const int i = tid + n * 512, r = i / 4 % D;
+        return (uint32_t)(i / (4 * D) * D * 128 + r * 128 + (((i & 3) ^ (r & 7)) << 4));
+      };
       uint4 sh[IT], sl[IT];  // this thread's part of S for <S, E'>
 #pragma unroll
       for (int n = 0; n < IT; ++n) {
-        sh[n] = reinterpret_cast<const uint4*>(sm.a)[tid + n * 512];
-        sl[n] = reinterpret_cast<const uint4*>(sm.a)[tid + n * 512 + D * D / 8];
+        sh[n] = *reinterpret_cast<const uint4*>(sm.a + part_at(n));
+        sl[n] = *reinterpret_cast<const uint4*>(sm.a + (part_at(n) ^ 64));
       }
       X_WAIT(sm.bars[XG_MMA], mma, 102);
       mma ^= 1;
       if (tid == 0) bulk_load(sm.a, bwd + Rec::E, D * D * 4, expect(sm, XG_E, D * D * 4));
       X_WAIT(sm.bars[XG_E], second, 103);
       if (warp == 0) {
-        umma_group_ss<NK, true, true>(T2, kmaj(sm.y), kmaj(sm.a), XHI, ID_ST, 0, go);
-        umma_group_ss<NK, true, true>(T2, kmaj(sm.y), kmaj(sm.a + D * D * 2), XHI, ID_ST, 1, go);
-        umma_group_ss<NK, true, true>(T2, kmaj(sm.y + TOK), kmaj(sm.a), XHI, ID_ST, 1, go);
+        state_product<D>(T2, kmaj(sm.y), kmaj(sm.a), 0, ID_ST, 0, go);
+        state_product<D>(T2, kmaj(sm.y), kmaj(sm.a), 4, ID_ST, 1, go);
+        state_product<D>(T2, kmaj(sm.y + TOK), kmaj(sm.a), 0, ID_ST, 1, go);
         umma_commit_if(&sm.bars[XG_MMA], go);
       }
       float whole = 0.f;
@@ -1391,7 +1415,7 @@ x_gradient_kernel(const __grid_constant__ XMaps maps, const __grid_constant__ De
       for (int n = 0; n < IT; ++n) {
         float x[8], y[8];
         join8(sh[n], sl[n], x);
-        join8(reinterpret_cast<const uint4*>(sm.a)[tid + n * 512], reinterpret_cast<const uint4*>(sm.a)[tid + n * 512 + D * D / 8], y);
+        join8(*reinterpret_cast<const uint4*>(sm.a + part_at(n)), *reinterpret_cast<const uint4*>(sm.a + (part_at(n) ^ 64)), y);
 #pragma unroll
         for (int i = 0; i < 8; ++i) whole = fmaf(x[i], y[i], whole);
       }

@@ -245,6 +245,17 @@ __device__ __forceinline__ uint32_t elect_one() {
   asm volatile("{\n\t.reg .pred q;\n\telect.sync _|q, 0xffffffff;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "=r"(el));
   return el;
 }
+// One instruction of 16 rows of K.
+__device__ __forceinline__ void umma_ss(uint32_t d_tmem, uint32_t a_lo, uint32_t b_lo, uint32_t desc_hi, uint32_t idesc, uint32_t acc,
+                                        uint32_t go) {
+  asm volatile(
+      "{\n\t.reg .pred p, g;\n\t.reg .b64 da, db;\n\t"
+      "setp.ne.b32 g, %6, 0;\n\tsetp.ne.b32 p, %5, 0;\n\t"
+      "mov.b64 da, {%1, %3};\n\tmov.b64 db, {%2, %3};\n\t"
+      "@g tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %4, p;\n\t}" ::"r"(d_tmem),
+      "r"(a_lo), "r"(b_lo), "r"(desc_hi), "r"(idesc), "r"(acc), "r"(go)
+      : "memory");
+}
 // A whole K loop in one instruction sequence: NK tensor-core instructions D[tmem] (+)= A_k * B_k, k = 0..NK-1,
 // all predicated on `go`, the first one accumulating only if `acc0`.  Operand k is operand 0 moved by a
 // compile-time step: for shared-memory operands the low descriptor half advances by step(k) (16-byte units),

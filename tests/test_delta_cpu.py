@@ -142,16 +142,15 @@ def test_argument_kinds_are_those_of_the_header(monkeypatch):
     header = re.sub(r"/\*.*?\*/|//[^\n]*", "", header, flags=re.S)
     got = []
     monkeypatch.setattr(la, "_enter", lambda name, kinds, *args: got.append((name, kinds, len(args))))
-    monkeypatch.setattr(la, "_matches", lambda *args: None)
     for name in ("la_delta_fwd", "la_delta_bwd", "la_delta_steps", "la_block_norm_fwd", "la_block_norm_bwd"):
         args = re.search(r"la_status\s+%s\(([^;]*?)\);" % name, header, re.S).group(1)
         want = ""
         for a in (" ".join(x.split()) for x in args.split(",")):
             want += "d" if "la_delta_shape" in a else "n" if "la_block_norm_shape" in a else "r" if a == "void* stream" else "t" if "*" in a else "i"
         f = getattr(la, name)
-        monkeypatch.setattr(la, "_current_device", lambda: 0)
         f(**{p: (delta() if "delta" in name else norm()) if p == "shape" else None for p in inspect.signature(f).parameters})
-        assert got[-1] == (name, want, len(want))
+        kinds = "".join("t" if c in "QPVOGSXYFw" else c for c in got[-1][1])  # (tensors that are held to the shape)
+        assert (got[-1][0], kinds, got[-1][2]) == (name, want, len(want))
 
 
 @pytest.mark.parametrize("wrong", [la.make_shape(1, 1, 1, 64, 64, BF16, F32), 5, None])
@@ -166,13 +165,24 @@ def test_shapes_of_other_calls_are_refused(monkeypatch, wrong):
 
 
 def test_tensors_that_do_not_match_are_refused(monkeypatch):
-    """(Tensors on the CPU say that they are on device -1.)"""
+    """Types and sizes follow from the shape, argument by argument.  (Tensors on the CPU say that they are on device -1.)"""
+    la.load()
     s = delta(N=3)
     q, v, g = torch.zeros(1, 2, 3, 64), torch.zeros(1, 4, 3, 64), torch.zeros(1, 4, 3)
     kv = torch.zeros(1, 4, 64, 64)
-    for args, word in (((q.bfloat16(), q, v, g, g, kv, v), "q has to be torch.float32"), ((q, v, v, g, g, kv, v), "k has to be"),
-                       ((q, q, q, g, g, kv, v), "v has to be"), ((q, q, v, g.double(), g, kv, v), "g has to be"),
+    for args, word in (((q.bfloat16(), q, v, g, g, kv, v), "argument 1 has to be torch.float32 with 384 elements"), ((q, v, v, g, g, kv, v), "argument 2 has to be torch.float32 with 384"),
+                       ((q, q, q, g, g, kv, v), "argument 3 has to be torch.float32 with 768"), ((q, q, v, g.double(), g, kv, v), "argument 4 has to be torch.float32 with 12 "),
+                       ((q, q, v, g, g, q, v), "argument 6 has to be torch.float32 with 16384"),
+                       ((q, q, v, g, g, kv, q), "argument 7 has to be torch.float32 with 768"),
+                       ((q.transpose(1, 2), q, v, g, g, kv, v), "argument 1 has to be contiguous"),
                        ((q, q, v, g, g, kv, v), "on the current CUDA device")):
         monkeypatch.setattr(la, "_current_device", lambda: 0 if "device" in word else -1)
         with pytest.raises(ValueError, match=word):
             la.la_delta_steps(s, *args)
+    n, x, w = norm(rows=2), torch.zeros(2, 64), torch.zeros(64)
+    y = x.bfloat16()
+    monkeypatch.setattr(la, "_current_device", lambda: -1)
+    for args, word in (((y, y, y, w, w, w, x, y), "argument 1 has to be torch.float32 with 128"), ((x, x, y, w, w, w, x, y), "argument 2 has to be torch.bfloat16"),
+                       ((x, y, y, x, w, w, x, y), "argument 4 has to be torch.float32 with 64"), ((x, y, y, w, w, w, x, x), "argument 8 has to be torch.bfloat16")):
+        with pytest.raises(ValueError, match=word):
+            la.la_block_norm_fwd(n, *args)
