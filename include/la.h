@@ -303,8 +303,10 @@ la_status la_decode_steps(const la_shape* shape, const void* q, const void* k, c
  *   dg, dbeta    the same layout, fp32;
  *   states       [B,H,d,e] fp32, as those of la_fwd; kv_in / kv_out / grad_kv_out / grad_kv_in may be NULL.
  * d == e in {64, 128}; 1 <= Hk <= H, H a multiple of Hk; B * H <= 65535; types as in la_shape.  Accumulation and states are fp32.  bf16
- * inputs run on the tensor cores (path AUTO or TENSOR), where operands formed on chip are carried as two bf16 terms (x to 2^-17);
- * fp32 inputs, and path SIMT, on the CUDA cores.
+ * inputs run on the tensor cores (path AUTO or TENSOR), where operands formed on chip are carried as two bf16 terms (results
+ * in fp32 are then off by 4e-6 to 7e-6 in the relative 2-norm); fp32 inputs, and path SIMT, on the CUDA cores (3e-7).
+ * A NaN or infinity of a token reaches all tokens of its chunk (128 tokens; CUDA cores 64) and those after it, in the heads that read it.
+ * Sequences one after the other in one row of tokens, each from a zero state: g = -inf at the first token of each.
  *
  *   la_delta_fwd     all tokens, from kv_in (NULL: zeros).  workspace: la_delta_workspace_bytes(LA_OP_FWD, shape) bytes, 256-byte
  *                    aligned; calls that share one must be stream-ordered.  Linear in N: a state and the operands that lead from one to

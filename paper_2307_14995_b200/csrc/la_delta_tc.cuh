@@ -16,8 +16,10 @@
 // cores read (records below), and everything else has a thread block per chunk.  A walk that formed V' from What S, then S' from
 // V', would be two dependent products with two conversions between them.
 //
-// As in the walk, operands formed on chip from fp32 values are two bf16 terms hi + lo = x to 2^-17, and products of two such
-// operands leave out lo x lo.  Sums are fp32, in an order that depends on the shape alone.
+// As in the walk, operands formed on chip from fp32 values are two bf16 terms hi + lo, off by 2^-16 of a value at most and by 2.7e-6 of
+// it on the root of the mean square: in a result that passes six of them 6e-6, in a state or gradient 4e-6 to 7e-6 (measured).  Products of two such operands leave
+// out lo x lo, except where it comes with the columns of an operand [hi | lo].  Sums are fp32, in an order that depends on the shape
+// alone: the products of lo terms first, so that fewer additions meet a large sum, whose rounding is towards zero.
 //
 // Operands in shared memory and in the workspace are images: rows of 128 bytes (64 elements) in the 128-byte swizzle, panel after panel of
 // 64 columns, all panels of hi and then those of lo; one image serves K-major and MN-major.  They move by untiled bulk copies.  States are
@@ -200,6 +202,9 @@ __device__ __forceinline__ uint64_t* expect(SM& sm, int i, uint32_t bytes) {
   return &sm.bars[i];
 }
 
+// Products are issued by warp 0, and in the gradient kernel by this one too.
+constexpr int X_ISSUER = 12;
+
 // Start and end that all kernels below share.  body() returns false when a wait gave up.
 template <int COLS, typename SM, typename F>
 __device__ __forceinline__ void x_run(SM& sm, int nbars, F body) {
@@ -223,10 +228,13 @@ __device__ __forceinline__ void x_run(SM& sm, int nbars, F body) {
   grid_dep_launch();
   const uint32_t tmem = sm.tmem_slot;
   const bool ok = body(tmem);
-  if (!ok) {  // products and copies that are still under way end before the block does
-    if (warp == 0) {
-      umma_commit_if(&sm.bars[nbars - 1], elect_one());
-      drain_wait(&sm.bars[nbars - 1], 0);
+  if (!ok) {  // products and copies that are still under way end before the block does; those of a warp are told by its own commit
+    for (int w = 0, par = 0; w < (int)(blockDim.x >> 5); w += X_ISSUER, par ^= 1) {
+      if (warp == w) {
+        umma_commit_if(&sm.bars[nbars - 1], elect_one());
+        drain_wait(&sm.bars[nbars - 1], par);
+      }
+      __syncthreads();
     }
     if (tid == 32)
       for (int i = 0; i < nbars - 1; ++i)
@@ -438,9 +446,9 @@ x_prepare_kernel(const __grid_constant__ XMaps maps, const __grid_constant__ Del
       if (warp == 0) {
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
-          umma_group_tsd2(R + 32 * b, P + 48, mnmaj(pair + b * 4096), XHI, ID_KN32, 0, go);
+          umma_group_tsd2(R + 32 * b, P + 112, mnmaj(pair + b * 4096), XHI, ID_KN32, 0, go);
           umma_group_tsd2(R + 32 * b, P + 48, mnmaj(pair + 8192 + b * 4096), XHI, ID_KN32, 1, go);
-          umma_group_tsd2(R + 32 * b, P + 112, mnmaj(pair + b * 4096), XHI, ID_KN32, 1, go);
+          umma_group_tsd2(R + 32 * b, P + 48, mnmaj(pair + b * 4096), XHI, ID_KN32, 1, go);
         }
         umma_commit_if(&sm.bars[XP_MMA], go);
       }
@@ -491,9 +499,9 @@ x_prepare_kernel(const __grid_constant__ XMaps maps, const __grid_constant__ Del
     };
     auto square_product = [&](uint32_t hi, uint32_t lo) {  // to columns 0 .. 63 of R
       if (warp == 0) {
-        umma_group_tsd4<false>(R, hi, mnmaj(sm.x), XHI, ID_KN64, 0, go);
+        umma_group_tsd4<false>(R, lo, mnmaj(sm.x), XHI, ID_KN64, 0, go);
         umma_group_tsd4<false>(R, hi, mnmaj(sm.x + 8192), XHI, ID_KN64, 1, go);
-        umma_group_tsd4<false>(R, lo, mnmaj(sm.x), XHI, ID_KN64, 1, go);
+        umma_group_tsd4<false>(R, hi, mnmaj(sm.x), XHI, ID_KN64, 1, go);
         umma_commit_if(&sm.bars[XP_MMA], go);
       }
     };
@@ -577,9 +585,9 @@ x_prepare_kernel(const __grid_constant__ XMaps maps, const __grid_constant__ Del
       tma_store_commit();
     }
     if (warp == 0) {  // X = P That: That [m][j] is U [j][m]
-      umma_group_tsd<true>(R, P, kmaj(sm.x), XHI, ID_KK, 0, go);
+      umma_group_tsd<true>(R, P + 64, kmaj(sm.x), XHI, ID_KK, 0, go);
       umma_group_tsd<true>(R, P, kmaj(sm.x + 32768), XHI, ID_KK, 1, go);
-      umma_group_tsd<true>(R, P + 64, kmaj(sm.x), XHI, ID_KK, 1, go);
+      umma_group_tsd<true>(R, P, kmaj(sm.x), XHI, ID_KK, 1, go);
       umma_commit_if(&sm.bars[XP_MMA], go);
       if (tid == 0) tma_store_wait_read();
       __syncwarp();
@@ -599,8 +607,8 @@ x_prepare_kernel(const __grid_constant__ XMaps maps, const __grid_constant__ Del
     put_image(h, l, row, w4 * 4, 128, 32768);
     X_HAND_OVER();
     if (warp == 0) {  // J^T [d, j] = K^T U'^T
-      umma_group_ss<8, false, true>(P, mnmaj(sm.k), kmaj(sm.x), XHI, ID_NK, 0, go);
-      umma_group_ss<8, false, true>(P, mnmaj(sm.k), kmaj(sm.x + 32768), XHI, ID_NK, 1, go);
+      umma_group_ss<8, false, true>(P, mnmaj(sm.k), kmaj(sm.x + 32768), XHI, ID_NK, 0, go);
+      umma_group_ss<8, false, true>(P, mnmaj(sm.k), kmaj(sm.x), XHI, ID_NK, 1, go);
       umma_commit_if(&sm.bars[XP_MMA], go);
     }
     {  // X leaves as an image
@@ -635,8 +643,8 @@ x_prepare_kernel(const __grid_constant__ XMaps maps, const __grid_constant__ Del
     X_HAND_OVER();
     X_WAIT(sm.bars[XP_V], 0, 56);
     if (warp == 0) {  // N = J^T V
-      umma_group_tsd<false>(P, R, mnmaj(sm.x), XHI, ID_KN, 0, go);
-      umma_group_tsd<false>(P, R + 64, mnmaj(sm.x), XHI, ID_KN, 1, go);
+      umma_group_tsd<false>(P, R + 64, mnmaj(sm.x), XHI, ID_KN, 0, go);
+      umma_group_tsd<false>(P, R, mnmaj(sm.x), XHI, ID_KN, 1, go);
       umma_commit_if(&sm.bars[XP_MMA], go);
     }
     X_WAIT(sm.bars[XP_MMA], par, 57);
@@ -661,8 +669,8 @@ x_prepare_kernel(const __grid_constant__ XMaps maps, const __grid_constant__ Del
       }
       X_HAND_OVER();
       if (warp == 0) {
-        umma_group_tsd<false>(P, R, mnmaj(sm.k), XHI, ID_KN, 0, go);
-        umma_group_tsd<false>(P, R + 64, mnmaj(sm.k), XHI, ID_KN, 1, go);
+        umma_group_tsd<false>(P, R + 64, mnmaj(sm.k), XHI, ID_KN, 0, go);
+        umma_group_tsd<false>(P, R, mnmaj(sm.k), XHI, ID_KN, 1, go);
         umma_commit_if(&sm.bars[XP_MMA], go);
       }
 #pragma unroll
@@ -740,7 +748,7 @@ x_chain_kernel(const __grid_constant__ XChainArgs a) {
       for (int i = 0; i < XC_STAGES && i < a.nchunk; ++i) load_m(i);
     __syncwarp();
     const uint32_t go = warp == 0 ? elect_one() : 0;
-    constexpr uint32_t ID2 = umma_idesc_bf16(128, 2 * NE, REV, true), ID1 = umma_idesc_bf16(128, NE, REV, true);
+    constexpr uint32_t ID2 = umma_idesc_bf16(128, 2 * NE, REV, true);
     float s[V], add[V], all = 0.f;
     if (owner) {
       const size_t at = ((size_t)bh * D + row) * D + e0 + half * V;
@@ -782,8 +790,8 @@ x_chain_kernel(const __grid_constant__ XChainArgs a) {
           const unsigned char* const m = sm.m[st];
           const uint32_t b = mnmaj(sm.b, D * 128);
           if (D == 128) {
-            umma_group_ss<8, !REV, false>(tmem, REV ? mnmaj(m) : kmaj(m), b, XHI, ID2, 0, go);
-            umma_group_ss<8, !REV, false>(tmem, REV ? mnmaj(m + 32768) : kmaj(m + 32768), b, XHI, NE == 32 ? ID1 : ID2, 1, go);
+            umma_group_ss<8, !REV, false>(tmem, REV ? mnmaj(m + 32768) : kmaj(m + 32768), b, XHI, ID2, 0, go);
+            umma_group_ss<8, !REV, false>(tmem, REV ? mnmaj(m) : kmaj(m), b, XHI, ID2, 1, go);
           } else {
             umma_group_ss<4, !REV, false>(tmem, REV ? mnmaj(m, 8192) : kmaj(m), b, XHI, ID2, 0, go);
           }
@@ -950,7 +958,7 @@ x_output_kernel(const __grid_constant__ XMaps maps, const __grid_constant__ Delt
     load_raw32(static_cast<const __nv_bfloat16*>(a.v) + p.row + row * a.sT + eh * 64 + half * 32, row < p.n, raw);
     __syncwarp();
     const uint32_t go = warp == 0 ? elect_one() : 0;
-    constexpr uint32_t ID2 = umma_idesc_bf16(128, 128, false, true), ID1 = umma_idesc_bf16(128, 64, false, true);
+    constexpr uint32_t ID2 = umma_idesc_bf16(128, 128, false, true);
     X_WAIT(sm.bars[XO_LOAD], 0, 70);
     const float since = ex2_approx(sm.gates.sum[row].x + sm.gates.sum[row].y);
     if (warp == 0) {
@@ -976,8 +984,8 @@ x_output_kernel(const __grid_constant__ XMaps maps, const __grid_constant__ Delt
     X_HAND_OVER();
     X_WAIT(sm.bars[XO_X], 0, 72);
     if (warp == 0) {
-      umma_group_ss<8, true, false>(tmem, kmaj(sm.qk), mnmaj(sm.s), XHI, ID2, 0, go);
-      umma_group_ss<8, true, false>(tmem, kmaj(sm.qk + 32768), mnmaj(sm.s), XHI, ID1, 1, go);
+      umma_group_ss<8, true, false>(tmem, kmaj(sm.qk + 32768), mnmaj(sm.s), XHI, ID2, 0, go);
+      umma_group_ss<8, true, false>(tmem, kmaj(sm.qk), mnmaj(sm.s), XHI, ID2, 1, go);
       umma_commit_if(&sm.bars[XO_MMA], go);
     }
     float v[32];
@@ -1040,8 +1048,8 @@ x_adjoint_kernel(const __grid_constant__ XMaps maps, const __grid_constant__ Del
     X_WAIT(sm.bars[XA_LOAD], 0, 80);
     const float since = ex2_approx(sm.gates.sum[row].x + sm.gates.sum[row].y);
     if (warp == 0) {
-      umma_group_ss<8, false, false>(tmem, mnmaj(sm.x), mnmaj(sm.t + 16384), XHI, ID1, 0, go);
-      umma_group_ss<8, false, false>(tmem, mnmaj(sm.x + 32768), mnmaj(sm.t + 16384), XHI, ID1, 1, go);
+      umma_group_ss<8, false, false>(tmem, mnmaj(sm.x + 32768), mnmaj(sm.t + 16384), XHI, ID1, 0, go);
+      umma_group_ss<8, false, false>(tmem, mnmaj(sm.x), mnmaj(sm.t + 16384), XHI, ID1, 1, go);
       umma_commit_if(&sm.bars[XA_MMA], go);
     }
     uint4 raw[4];
@@ -1186,8 +1194,7 @@ x_values_kernel(const __grid_constant__ XMaps maps, const __grid_constant__ Delt
     }
     __syncwarp();
     const uint32_t go = warp == 0 ? elect_one() : 0;
-    constexpr uint32_t ID2 = umma_idesc_bf16(128, 128, false, true), ID1 = umma_idesc_bf16(128, 64, false, true);
-    constexpr uint32_t ID2T = umma_idesc_bf16(128, 128, true, true), ID1T = umma_idesc_bf16(128, 64, true, true);
+    constexpr uint32_t ID2 = umma_idesc_bf16(128, 128, false, true), ID2T = umma_idesc_bf16(128, 128, true, true);
     X_WAIT(sm.bars[XV_LOAD], 0, 90);
     const float2 own = sm.gates.sum[row];
     const float times = grad ? sm.gates.beta[row] * decay2(end, own) : -ex2_approx(own.x + own.y);
@@ -1216,11 +1223,11 @@ x_values_kernel(const __grid_constant__ XMaps maps, const __grid_constant__ Delt
     X_WAIT(sm.bars[XV_U], 0, 92);
     if (warp == 0) {
       if (grad) {
-        umma_group_ss<8, true, false>(tmem, kmaj(sm.u), mnmaj(sm.s), XHI, ID2, 0, go);
-        umma_group_ss<8, true, false>(tmem, kmaj(sm.u + 32768), mnmaj(sm.s), XHI, ID1, 1, go);
+        umma_group_ss<8, true, false>(tmem, kmaj(sm.u + 32768), mnmaj(sm.s), XHI, ID2, 0, go);
+        umma_group_ss<8, true, false>(tmem, kmaj(sm.u), mnmaj(sm.s), XHI, ID2, 1, go);
       } else {
-        umma_group_ss<8, false, false>(tmem, mnmaj(sm.u), mnmaj(sm.s), XHI, ID2T, 0, go);
-        umma_group_ss<8, false, false>(tmem, mnmaj(sm.u + 32768), mnmaj(sm.s), XHI, ID1T, 1, go);
+        umma_group_ss<8, false, false>(tmem, mnmaj(sm.u + 32768), mnmaj(sm.s), XHI, ID2T, 0, go);
+        umma_group_ss<8, false, false>(tmem, mnmaj(sm.u), mnmaj(sm.s), XHI, ID2T, 1, go);
       }
       umma_commit_if(&sm.bars[XV_MMA], go);
     }
@@ -1365,11 +1372,11 @@ x_gradient_kernel(const __grid_constant__ XMaps maps, const __grid_constant__ De
       X_WAIT(sm.bars[XG_LOAD], second, 101);
       // ---- what the states have ----
       if (warp == 0) {
-        state_product<D>(T0, kmaj(sm.o), kmaj(sm.a), 0, ID_ST, 0, go);
-        state_product<D>(T0, kmaj(sm.o), kmaj(sm.a), 4, ID_ST, 1, go);
-        state_product<D>(T1, kmaj(sm.s), kmaj(sm.a), 0, ID_ST, 0, go);
+        state_product<D>(T0, kmaj(sm.o), kmaj(sm.a), 4, ID_ST, 0, go);
+        state_product<D>(T0, kmaj(sm.o), kmaj(sm.a), 0, ID_ST, 1, go);
+        state_product<D>(T1, kmaj(sm.s + TOK), kmaj(sm.a), 0, ID_ST, 0, go);
         state_product<D>(T1, kmaj(sm.s), kmaj(sm.a), 4, ID_ST, 1, go);
-        state_product<D>(T1, kmaj(sm.s + TOK), kmaj(sm.a), 0, ID_ST, 1, go);
+        state_product<D>(T1, kmaj(sm.s), kmaj(sm.a), 0, ID_ST, 1, go);
         umma_commit_if(&sm.bars[XG_MMA], go);
       }
       if (tid == 0) {
@@ -1405,9 +1412,9 @@ x_gradient_kernel(const __grid_constant__ XMaps maps, const __grid_constant__ De
       if (tid == 0) bulk_load(sm.a, bwd + Rec::E, D * D * 4, expect(sm, XG_E, D * D * 4));
       X_WAIT(sm.bars[XG_E], second, 103);
       if (warp == 0) {
-        state_product<D>(T2, kmaj(sm.y), kmaj(sm.a), 0, ID_ST, 0, go);
+        state_product<D>(T2, kmaj(sm.y + TOK), kmaj(sm.a), 0, ID_ST, 0, go);
         state_product<D>(T2, kmaj(sm.y), kmaj(sm.a), 4, ID_ST, 1, go);
-        state_product<D>(T2, kmaj(sm.y + TOK), kmaj(sm.a), 0, ID_ST, 1, go);
+        state_product<D>(T2, kmaj(sm.y), kmaj(sm.a), 0, ID_ST, 1, go);
         umma_commit_if(&sm.bars[XG_MMA], go);
       }
       float whole = 0.f;
@@ -1465,8 +1472,8 @@ x_gradient_kernel(const __grid_constant__ XMaps maps, const __grid_constant__ De
       // ---- scores ----
       if (warp == 0) {
         umma_group_ss<NK, true, true>(T2, kmaj(sm.a), kmaj(sm.a + TOK), XHI, ID_SC, 0, go);
-        umma_group_ss<NK, true, true>(T3, kmaj(sm.o), kmaj(sm.y), XHI, ID_SC, 0, go);
-        umma_group_ss<NK, true, true>(T3, kmaj(sm.o), kmaj(sm.y + TOK), XHI, ID_SC, 1, go);
+        umma_group_ss<NK, true, true>(T3, kmaj(sm.o), kmaj(sm.y + TOK), XHI, ID_SC, 0, go);
+        umma_group_ss<NK, true, true>(T3, kmaj(sm.o), kmaj(sm.y), XHI, ID_SC, 1, go);
         umma_commit_if(&sm.bars[XG_MMA], go);
       }
       X_WAIT(sm.bars[XG_MMA], mma, 106);
@@ -1528,9 +1535,9 @@ x_gradient_kernel(const __grid_constant__ XMaps maps, const __grid_constant__ De
       tc_fence_after_sync();
       if (warp == 0) {
         umma_group_ss<NK, true, true>(T2, kmaj(sm.a + TOK), kmaj(sm.a + TOK), XHI, ID_SC, 0, go);
-        umma_group_ss<NK, true, true>(T3, kmaj(sm.s), kmaj(sm.y), XHI, ID_SC, 0, go);
+        umma_group_ss<NK, true, true>(T3, kmaj(sm.s + TOK), kmaj(sm.y), XHI, ID_SC, 0, go);
         umma_group_ss<NK, true, true>(T3, kmaj(sm.s), kmaj(sm.y + TOK), XHI, ID_SC, 1, go);
-        umma_group_ss<NK, true, true>(T3, kmaj(sm.s + TOK), kmaj(sm.y), XHI, ID_SC, 1, go);
+        umma_group_ss<NK, true, true>(T3, kmaj(sm.s), kmaj(sm.y), XHI, ID_SC, 1, go);
         umma_commit_if(&sm.bars[XG_MMA], go);
       }
       X_WAIT(sm.bars[XG_MMA], mma, 107);
@@ -1548,21 +1555,20 @@ x_gradient_kernel(const __grid_constant__ XMaps maps, const __grid_constant__ De
       }
       // The last products are issued by a warp whose scores are above the diagonal, so that it has no part in Z: an issuing warp waits as long
       // as its products run, here 4100 clocks, and the others sum up Z meanwhile, at a barrier of their own.
-      constexpr int ISSUER = 12;
       sums.a[w4][row] = dot_a;
       sums.b[w4][row] = dot_b;
       if (lane == 0) sums.part[warp] = whole;
-      if (warp == ISSUER) {
+      if (warp == X_ISSUER) {
         sums.rows[w4][row] = 0.f;
         sums.col[q][c0 + lane] = 0.f;
         if (lane == 0) sums.total[w4][q] = 0.f;
       }
       X_HAND_OVER();
-      if (warp == ISSUER) {
+      if (warp == X_ISSUER) {
         const uint32_t go = elect_one();
         const unsigned char *const qt = sm.a, *const kt = sm.a + TOK;
 #pragma unroll
-        for (int term = 0; term < 2; ++term) {
+        for (int term = 1; term >= 0; --term) {
           umma_group_ss<8, true, false>(T0, kmaj(sm.y + term * 32768), mnmaj(kt), XHI, ID_N, 1, go);
           umma_group_ss<8, false, false>(T1, mnmaj(sm.y + term * 32768), mnmaj(qt), XHI, ID_T, 1, go);
           umma_group_ss<8, false, false>(T1, mnmaj(sm.s + term * 32768), mnmaj(kt), XHI, ID_T, 1, go);

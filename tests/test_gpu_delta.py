@@ -1,10 +1,10 @@
 """The gated delta rule through the C ABI against the fp64 oracle: la_delta_fwd, la_delta_bwd, la_delta_steps.
 
 Tolerances, in units of the RMS of each (batch, head) slice of the result.  CUDA cores: fp32 throughout, the library's 1e-4 for its fp32
-workload.  Tensor cores: operands that are formed on chip are rounded to two bf16 terms, at most 2^-17 of each value (a relative 2-norm
-of 2^-17 / sqrt(3) = 4.4e-6 for rounding errors spread evenly); a result passes six such products forward and twelve backward, 1.5e-5,
-its largest error is five times that, and the inverse of a unit triangle with entries below 1 enlarges it by 4 at most on these
-inputs: 3e-4.  A result in bf16 is off by half a step of its own besides, 2^-8 of its value."""
+workload.  Tensor cores: operands that are formed on chip are rounded to two bf16 terms, at most 2^-16 of each value (each term leaves
+2^-8 / sqrt(3) of the rest on the root of the mean square, times 0.72 for values spread over a binade: 2.7e-6 for both); a result passes
+six such operands forward and twelve backward, 9e-6, its largest error is five times that, and the inverse of a unit triangle with
+entries below 1 enlarges it by 4 at most on these inputs: 2e-4, and half as much again for the products of lo terms that are left out.  A result in bf16 is off by half a step of its own besides, 2^-8 of its value."""
 import numpy as np
 import pytest
 import torch
@@ -182,6 +182,24 @@ def test_gates_at_their_ends(d, dtype, path):
     call.bwd()
     call.done()
     check(call, reference(data, kv_in=kv_in, grad_kv_out=grad), tol(path, dtype))
+
+
+@pytest.mark.parametrize("dtype,path", KINDS)
+def test_packed_sequences(dtype, path):
+    """Sequences one after the other, g = -inf at the first token of each: every one as on its own, forward and backward."""
+    lengths = [1, 130, 64, 5, 200]
+    data = list(draw(1, 4, 2, sum(lengths), 128, 61, dtype))
+    first = np.cumsum([0] + lengths)
+    data[3][:, :, first[:-1]] = -np.inf
+    call = Call(data, path=path)
+    call.fwd()
+    call.bwd()
+    call.done()
+    got = call.results()
+    for a, b in zip(first[:-1], first[1:]):
+        ref = reference([x[:, :, a:b].contiguous() for x in data])
+        for name in ("o", "dq", "dk", "dv", "dbeta"):
+            near(got[name][:, :, a:b], ref[name], tol(path, dtype) * (1 if b - a > 5 else 4), name)  # (an RMS of few values)
 
 
 @pytest.mark.parametrize("dtype,path", KINDS)
