@@ -76,6 +76,7 @@ __device__ __forceinline__ Place place(const DeltaArgs& a, int bh, int c) {
 // rows [n of C][D] of a token tensor to shared memory, zero behind the last one
 template <int D, typename T>
 __device__ __forceinline__ void load_rows(float (*dst)[D + 1], const T* src, long long stride, int n) {
+#pragma unroll 8
   for (int i = threadIdx.x; i < C * D; i += THREADS) {
     const int t = i / D, x = i % D;
     dst[t][x] = t < n ? to_f32(src[t * stride + x]) : 0.f;
@@ -144,6 +145,7 @@ __global__ void __launch_bounds__(THREADS) delta_prepare_kernel(const DeltaArgs 
     __syncwarp();
   }
   __syncthreads();
+#pragma unroll 8
   for (int i = threadIdx.x; i < C * C; i += THREADS) rec[Record<D>::T + i] = t[i / C][i % C];
   float acc[4][D / 16];
   clear(acc);
@@ -169,6 +171,7 @@ __global__ void __launch_bounds__(THREADS) delta_walk_kernel(const DeltaArgs a) 
   grid_dep_wait();
   grid_dep_launch();
   const int bh = blockIdx.y, e0 = blockIdx.x * SLICE;
+#pragma unroll 8
   for (int i = threadIdx.x; i < D * SLICE; i += THREADS)
     s[i / SLICE][i % SLICE] = a.kv_in ? a.kv_in[((size_t)bh * D + i / SLICE) * D + e0 + i % SLICE] : 0.f;
   for (int c = 0; c < a.nchunk; ++c) {
@@ -178,6 +181,7 @@ __global__ void __launch_bounds__(THREADS) delta_walk_kernel(const DeltaArgs a) 
     load_rows<D>(k, static_cast<const TI*>(a.k) + p.krow, a.sTk, p.n);
     load_rows<D>(w, rec + Record<D>::W, D, C);
     load_gates(gates, a, p);
+#pragma unroll 8
     for (int i = threadIdx.x; i < D * SLICE; i += THREADS) rec[Record<D>::S + (i / SLICE) * D + e0 + i % SLICE] = s[i / SLICE][i % SLICE];
     float acc[4][2];
     clear(acc);
@@ -196,6 +200,7 @@ __global__ void __launch_bounds__(THREADS) delta_walk_kernel(const DeltaArgs a) 
   }
   __syncthreads();
   if (a.kv_out)
+#pragma unroll 8
     for (int i = threadIdx.x; i < D * SLICE; i += THREADS)
       a.kv_out[((size_t)bh * D + i / SLICE) * D + e0 + i % SLICE] = s[i / SLICE][i % SLICE];
 }
@@ -280,6 +285,7 @@ __global__ void __launch_bounds__(THREADS) delta_walk_back_kernel(const DeltaArg
   grid_dep_wait();
   grid_dep_launch();
   const int bh = blockIdx.y, e0 = blockIdx.x * SLICE;
+#pragma unroll 8
   for (int i = threadIdx.x; i < D * SLICE; i += THREADS)
     s[i / SLICE][i % SLICE] = a.grad_kv_out ? a.grad_kv_out[((size_t)bh * D + i / SLICE) * D + e0 + i % SLICE] : 0.f;
   for (int c = a.nchunk - 1; c >= 0; --c) {
@@ -292,10 +298,12 @@ __global__ void __launch_bounds__(THREADS) delta_walk_back_kernel(const DeltaArg
     load_rows<D>(w, fwd + Record<D>::W, D, C);
     load_gates(gates, a, p);
     const TI* const in = static_cast<const TI*>(a.d_o) + p.row + e0;
+#pragma unroll 8
     for (int i = threadIdx.x; i < C * SLICE; i += THREADS) {
       const int t = i / SLICE;
       d_o[t][i % SLICE] = t < p.n ? to_f32(in[t * a.sT + i % SLICE]) * (a.scale * gates.since[t]) : 0.f;
     }
+#pragma unroll 8
     for (int i = threadIdx.x; i < D * SLICE; i += THREADS) rec[Record<D>::E + (i / SLICE) * D + e0 + i % SLICE] = s[i / SLICE][i % SLICE];
     float acc[4][2];
     clear(acc);
@@ -315,6 +323,7 @@ __global__ void __launch_bounds__(THREADS) delta_walk_back_kernel(const DeltaArg
   }
   __syncthreads();
   if (a.grad_kv_in)
+#pragma unroll 8
     for (int i = threadIdx.x; i < D * SLICE; i += THREADS)
       a.grad_kv_in[((size_t)bh * D + i / SLICE) * D + e0 + i % SLICE] = s[i / SLICE][i % SLICE];
 }
@@ -353,6 +362,7 @@ __global__ void __launch_bounds__(THREADS) delta_grad_kernel(const DeltaArgs a) 
     load_gates(gates, a, p);
     load_rows<D>(y, fwd + Record<D>::Y, D, C);
     load_rows<D>(d_o, rec + Record<D>::L, D, C);
+#pragma unroll 8
     for (int i = tid; i < C * C; i += THREADS) h[i / C][i % C] = fwd[Record<D>::T + i];
     __syncthreads();
     // dR = That^T diag(beta) dV', and dV' . Y
@@ -373,6 +383,7 @@ __global__ void __launch_bounds__(THREADS) delta_grad_kernel(const DeltaArgs a) 
     }
     __syncthreads();
     load_rows<D>(d_o, static_cast<const TI*>(a.d_o) + p.row, a.sT, p.n);
+#pragma unroll 8
     for (int i = tid; i < D * D; i += THREADS) st[(i / D) * (D + 1) + i % D] = fwd[Record<D>::S + i];
     __syncthreads();
     // Hh, with the products of the keys for dbeta; F
@@ -456,9 +467,11 @@ __global__ void __launch_bounds__(THREADS) delta_grad_kernel(const DeltaArgs a) 
 #pragma unroll
       for (int j = 0; j < D / 16; ++j) sum_k[i][j] -= acc[i][j];
     float whole = 0.f;
+#pragma unroll 8
     for (int i = tid; i < D * D; i += THREADS) whole = fmaf(st[(i / D) * (D + 1) + i % D], rec[Record<D>::E + i], whole);
     whole *= gates.all;
     __syncthreads();
+#pragma unroll 8
     for (int i = tid; i < D * D; i += THREADS) st[(i / D) * (D + 1) + i % D] = rec[Record<D>::E + i];
     if (tid < C) {  // Z's sums along its rows: of the columns before s
       float x = 0.f;

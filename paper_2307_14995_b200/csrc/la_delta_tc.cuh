@@ -57,6 +57,39 @@ __device__ __forceinline__ void prefetch(const void* src, uint32_t bytes) {  // 
 }
 __device__ __forceinline__ void bulk_store_done() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
 
+// The images of U (upper triangular) and X (lower) have 64 x 64 zeros: the half of a panel, of both terms, which neither moves nor is
+// kept; whoever loads one clears it in shared memory.
+constexpr uint32_t TRIANGLE = 49152;  // bytes that move
+template <bool UPPER>
+__device__ __forceinline__ void load_triangle(unsigned char* dst, const unsigned char* src, uint64_t* bar) {
+#pragma unroll
+  for (uint32_t term = 0; term < 65536; term += 32768) {
+    bulk_load(dst + term + (UPPER ? 0 : 24576), src + term + (UPPER ? 0 : 24576), 8192, bar);
+    bulk_load(dst + term + (UPPER ? 16384 : 0), src + term + (UPPER ? 16384 : 0), 16384, bar);
+  }
+}
+template <bool UPPER>
+__device__ __forceinline__ void store_triangle(unsigned char* dst, const unsigned char* src) {
+#pragma unroll
+  for (uint32_t term = 0; term < 65536; term += 32768) {
+    bulk_store(dst + term + (UPPER ? 0 : 24576), src + term + (UPPER ? 0 : 24576), 8192);
+    bulk_store(dst + term + (UPPER ? 16384 : 0), src + term + (UPPER ? 16384 : 0), 16384);
+  }
+}
+template <bool UPPER>
+__device__ __forceinline__ void prefetch_triangle(const unsigned char* src) {
+#pragma unroll
+  for (uint32_t term = 0; term < 65536; term += 32768) {
+    prefetch(src + term + (UPPER ? 0 : 24576), 8192);
+    prefetch(src + term + (UPPER ? 16384 : 0), 16384);
+  }
+}
+template <bool UPPER>
+__device__ __forceinline__ void clear_triangle(unsigned char* image, int tid, int threads) {
+  for (int i = tid; i < 1024; i += threads)
+    reinterpret_cast<uint4*>(image + (i >> 9) * 32768 + (UPPER ? 8192 : 16384))[i & 511] = make_uint4(0u, 0u, 0u, 0u);
+}
+
 // Byte offset of columns 8 c .. 8 c + 7 of row r in an image whose panels have `rows` rows.
 __device__ __forceinline__ uint32_t image_at(int r, int c, int rows) { return (uint32_t)((c >> 3) * rows * 128 + r * 128 + (((c & 7) ^ (r & 7)) << 4)); }
 
@@ -581,7 +614,7 @@ x_prepare_kernel(const __grid_constant__ XMaps maps, const __grid_constant__ Del
     put_image(h, l, row, w4 * 4, 128, 32768);
     X_HAND_OVER();
     if (tid == 0) {
-      bulk_store(rec + Rec::U, sm.x, 65536);
+      store_triangle<true>(rec + Rec::U, sm.x);
       tma_store_commit();
     }
     if (warp == 0) {  // X = P That: That [m][j] is U [j][m]
@@ -621,7 +654,7 @@ x_prepare_kernel(const __grid_constant__ XMaps maps, const __grid_constant__ Del
     put_image(h, l, row, w4 * 4, 128, 32768);
     X_HAND_OVER();
     if (tid == 0) {
-      bulk_store(rec + Rec::X, sm.x, 65536);
+      store_triangle<false>(rec + Rec::X, sm.x);
       tma_store_commit();
     }
     {  // J^T as an A operand in X's place; D = 64: lanes 64 .. 127 have J^T once more, for M, times e^G
@@ -942,7 +975,7 @@ x_output_kernel(const __grid_constant__ XMaps maps, const __grid_constant__ Delt
       for (int x = 0; x < PANELS; ++x) tma_load_4d(sm.qk + x * 16384, &maps.q, bar, x * 64, c * 128, p.hk, p.b);
       for (int x = 0; x < PANELS; ++x) tma_load_4d(sm.qk + 32768 + x * 16384, &maps.k, bar, x * 64, c * 128, p.hk, p.b);
       bulk_load(sm.s, rec + Rec::S + eh * 2 * D * 128, 2 * D * 128, bar);
-      prefetch(rec + Rec::X, 65536);
+      prefetch_triangle<false>(rec + Rec::X);
       unsigned nx, ny;
       if (later_block(296, nx, ny) && nx % PANELS == 0) {
         const XPlace o = x_place(a, ny, nx / PANELS);
@@ -967,7 +1000,8 @@ x_output_kernel(const __grid_constant__ XMaps maps, const __grid_constant__ Delt
       umma_commit_if(&sm.bars[XO_MMA], go);
     }
     X_WAIT(sm.bars[XO_MMA], 0, 71);
-    if (tid == 0) bulk_load(sm.qk, rec + Rec::X, 65536, expect(sm, XO_X, 65536));
+    if (tid == 0) load_triangle<false>(sm.qk, rec + Rec::X, expect(sm, XO_X, TRIANGLE));
+    clear_triangle<false>(sm.qk, tid, 256);
     {
       float x[32];
       load_slice(tmem + mine, half, x);
@@ -1037,14 +1071,16 @@ x_adjoint_kernel(const __grid_constant__ XMaps maps, const __grid_constant__ Del
     unsigned char* const bwd = static_cast<unsigned char*>(a.ws_bwd) + p.rec * Rec::BWD;
     const uint32_t mine = (uint32_t)(q * 32) << 16, R = tmem + 128;
     if (tid == 0) {
-      uint64_t* const bar = expect(sm, XA_LOAD, 65536 + 16384 + 2560);
+      uint64_t* const bar = expect(sm, XA_LOAD, TRIANGLE + 16384 + 2560);
       bulk_load(&sm.gates, fwd + Rec::GATES, 2560, bar);
-      bulk_load(sm.x, fwd + Rec::X, 65536, bar);
+      load_triangle<false>(sm.x, fwd + Rec::X, bar);
       tma_load_4d(sm.t + 16384, &maps.d_o, bar, eh * 64, c * 128, p.h, p.b);
     }
     __syncwarp();
     const uint32_t go = warp == 0 ? elect_one() : 0;
     constexpr uint32_t ID1 = umma_idesc_bf16(128, 64, true, true), ID2 = umma_idesc_bf16(128, 128, true, true);
+    clear_triangle<false>(sm.x, tid, 256);
+    fence_proxy_async_smem();
     X_WAIT(sm.bars[XA_LOAD], 0, 80);
     const float since = ex2_approx(sm.gates.sum[row].x + sm.gates.sum[row].y);
     if (warp == 0) {
@@ -1176,7 +1212,7 @@ x_values_kernel(const __grid_constant__ XMaps maps, const __grid_constant__ Delt
         const unsigned char* const of = static_cast<const unsigned char*>(a.ws) + o.rec * Rec::FWD;
         const unsigned char* const ob = static_cast<const unsigned char*>(a.ws_bwd) + o.rec * Rec::BWD;
         prefetch(of + Rec::S, Rec::STATE);
-        prefetch(of + Rec::U, 65536);
+        prefetch_triangle<true>(of + Rec::U);
         prefetch(ob + Rec::E, Rec::STATE);
         prefetch(ob + Rec::Z, Rec::TOK);
       }
@@ -1203,7 +1239,8 @@ x_values_kernel(const __grid_constant__ XMaps maps, const __grid_constant__ Delt
       umma_commit_if(&sm.bars[XV_MMA], go);
     }
     X_WAIT(sm.bars[XV_MMA], 0, 91);
-    if (tid == 0) bulk_load(sm.u, fwd + Rec::U, 65536, expect(sm, XV_U, 65536));
+    if (tid == 0) load_triangle<true>(sm.u, fwd + Rec::U, expect(sm, XV_U, TRIANGLE));
+    clear_triangle<true>(sm.u, tid, 256);
     float x[32];
     auto put = [&]() {
 #pragma unroll
