@@ -12,7 +12,7 @@
 namespace la {
 namespace {
 
-constexpr int C = DELTA_SIMT_CHUNK, THREADS = 256, SLICE = 32;
+constexpr int C = DELTA_SIMT_CHUNK, THREADS = 256, SLICE = 32, PC = C + 4;  // PC, PD: pitch of rows of C and of D values
 
 template <int D>
 struct Record {
@@ -20,21 +20,67 @@ struct Record {
   static constexpr size_t L = 0, E = L + C * D, BWD = E + D * D;
 };
 
-// acc[i][j] += sum_k a(row, k) b(k, col) for row = ty + 16 i, col = tx + 16 j
-template <int M, int N, typename FA, typename FB>
-__device__ __forceinline__ void product(float (&acc)[M / 16][N / 16], int K, FA a, FB b) {
+// Operands of a product, four values of consecutive k at a time: rows along which k runs (one access, so their pitch is a multiple of
+// 16 bytes; that of four more than a multiple of 32 values keeps the rows of a warp in different banks), rows of one k each, and values
+// of a function; all of them times a value per row or per k.
+struct Along {
+  const float* p;
+  int pitch;
+  __device__ __forceinline__ void four(int r, int k, float (&x)[4]) const {
+    const float4 v = *reinterpret_cast<const float4*>(p + r * pitch + k);
+    x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w;
+  }
+};
+struct Across {
+  const float* p;
+  int pitch;
+  __device__ __forceinline__ void four(int r, int k, float (&x)[4]) const {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = p[(k + i) * pitch + r];
+  }
+};
+template <typename F>
+struct Of {
+  F f;  // f(k, row)
+  __device__ __forceinline__ void four(int r, int k, float (&x)[4]) const {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = f(k + i, r);
+  }
+};
+template <typename F>
+__device__ __forceinline__ Of<F> of(F f) { return {f}; }
+template <typename A, bool ROW>
+struct Times {
+  A a;
+  const float* by;
+  __device__ __forceinline__ void four(int r, int k, float (&x)[4]) const {
+    a.four(r, k, x);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] *= by[ROW ? r : k + i];
+  }
+};
+template <typename A>
+__device__ __forceinline__ Times<A, false> times_k(A a, const float* by) { return {a, by}; }
+template <typename A>
+__device__ __forceinline__ Times<A, true> times_row(A a, const float* by) { return {a, by}; }
+
+// acc[i][j] += sum_k a(row, k) b(col, k) for row = ty + 16 i, col = tx + 16 j
+template <int M, int N, typename A, typename B>
+__device__ __forceinline__ void product(float (&acc)[M / 16][N / 16], int K, A a, B b) {
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-#pragma unroll 4
-  for (int k = 0; k < K; ++k) {
-    float x[M / 16], y[N / 16];
+#pragma unroll 2
+  for (int k = 0; k < K; k += 4) {
+    float x[M / 16][4], y[N / 16][4];
 #pragma unroll
-    for (int i = 0; i < M / 16; ++i) x[i] = a(ty + 16 * i, k);
+    for (int i = 0; i < M / 16; ++i) a.four(ty + 16 * i, k, x[i]);
 #pragma unroll
-    for (int j = 0; j < N / 16; ++j) y[j] = b(k, tx + 16 * j);
+    for (int j = 0; j < N / 16; ++j) b.four(tx + 16 * j, k, y[j]);
 #pragma unroll
-    for (int i = 0; i < M / 16; ++i)
+    for (int kk = 0; kk < 4; ++kk)
 #pragma unroll
-      for (int j = 0; j < N / 16; ++j) acc[i][j] = fmaf(x[i], y[j], acc[i][j]);
+      for (int i = 0; i < M / 16; ++i)
+#pragma unroll
+        for (int j = 0; j < N / 16; ++j) acc[i][j] = fmaf(x[i][kk], y[j][kk], acc[i][j]);
   }
 }
 template <int M, int N>
@@ -73,14 +119,31 @@ __device__ __forceinline__ Place place(const DeltaArgs& a, int bh, int c) {
   return p;
 }
 
-// rows [n of C][D] of a token tensor to shared memory, zero behind the last one
-template <int D, typename T>
-__device__ __forceinline__ void load_rows(float (*dst)[D + 1], const T* src, long long stride, int n) {
-#pragma unroll 8
-  for (int i = threadIdx.x; i < C * D; i += THREADS) {
-    const int t = i / D, x = i % D;
-    dst[t][x] = t < n ? to_f32(src[t * stride + x]) : 0.f;
+// Rows [n of C][D] of a token tensor, zero behind the last one, on their way to shared memory; in registers while a product runs.
+template <int D, int PITCH = D + 4>
+struct Rows {
+  float x[C * D / THREADS];
+  template <typename T>
+  __device__ __forceinline__ void fetch(const T* src, long long stride, int n) {
+#pragma unroll
+    for (int i = 0; i < C * D / THREADS; ++i) {
+      const int at = i * THREADS + threadIdx.x, t = at / D;
+      x[i] = t < n ? to_f32(src[t * stride + at % D]) : 0.f;
+    }
   }
+  __device__ __forceinline__ void put(float* dst) const {
+#pragma unroll
+    for (int i = 0; i < C * D / THREADS; ++i) {
+      const int at = i * THREADS + threadIdx.x;
+      dst[at / D * PITCH + at % D] = x[i];
+    }
+  }
+};
+template <int D, typename T>
+__device__ __forceinline__ void load_rows(float* dst, const T* src, long long stride, int n) {
+  Rows<D> rows;
+  rows.fetch(src, stride, n);
+  rows.put(dst);
 }
 
 // sums of the log decays up to each token, and beta; tokens behind the last one forget nothing and write nothing
@@ -89,21 +152,31 @@ struct Gates {
   float beta[C], since[C], until[C];  // since: decay from the state entering to the token; until: from the token to the chunk's end
   float all;
 };
-__device__ __forceinline__ void load_gates(Gates& s, const DeltaArgs& a, const Place& p) {
+struct Gate {
+  float g, beta;
+};
+__device__ __forceinline__ Gate fetch_gate(const DeltaArgs& a, const Place& p) {
   const int t = threadIdx.x;
+  if (t >= p.n) return {0.f, 0.f};
+  return {a.g[p.gate + t * a.gT], a.beta[p.gate + t * a.gT]};
+}
+__device__ __forceinline__ void make_gates(Gates& s, const Gate& own) {
+  const int t = threadIdx.x;
+  double x = clamped_log_decay(own.g);
   if (t < C) {
-    s.sum[t] = t < p.n ? clamped_log_decay(a.g[p.gate + t * a.gT]) : 0.0;
-    s.beta[t] = t < p.n ? a.beta[p.gate + t * a.gT] : 0.f;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const double y = __shfl_up_sync(0xffffffffu, x, o);
+      if ((t & 31) >= o) x += y;
+    }
+    s.sum[t] = x;
+    s.beta[t] = own.beta;
   }
   __syncthreads();
-  double x = 0.0, end = 0.0;
-  if (t < C)
-    for (int i = 0; i < C; ++i) {
-      end += s.sum[i];
-      if (i == t) x = end;
-    }
+  const double half = s.sum[C / 2 - 1], end = half + s.sum[C - 1];
   __syncthreads();
   if (t < C) {
+    if (t >= C / 2) x += half;
     s.sum[t] = x;
     s.since[t] = expf((float)x);
     s.until[t] = expf((float)(end - x));
@@ -111,107 +184,164 @@ __device__ __forceinline__ void load_gates(Gates& s, const DeltaArgs& a, const P
   }
   __syncthreads();
 }
+__device__ __forceinline__ void load_gates(Gates& s, const DeltaArgs& a, const Place& p) { make_gates(s, fetch_gate(a, p)); }
 __device__ __forceinline__ float decay(const Gates& s, int i, int j) { return expf((float)(s.sum[i] - s.sum[j])); }
 
 // ---- That, Uhat, What -----------------------------------------------------------------------------------------------------------
 template <typename TI, int D>
 __global__ void __launch_bounds__(THREADS) delta_prepare_kernel(const DeltaArgs a) {
   extern __shared__ float smem[];
-  auto x = reinterpret_cast<float(*)[D + 1]>(smem);              // k, then v
-  auto n = reinterpret_cast<float(*)[C + 1]>(smem + C * (D + 1));  // n diag(beta)
-  auto t = n + C;
+  constexpr int PD = D + 4;
+  float* const x = smem;           // k, then v
+  float* const n = x + C * PD;     // n diag(beta)
+  float* const t = n + C * PC;
   __shared__ Gates gates;
   grid_dep_wait();
   grid_dep_launch();
   const Place p = place(a, blockIdx.y, blockIdx.x);
   float* rec = static_cast<float*>(a.ws) + p.rec * Record<D>::FWD;
+  const int tid = threadIdx.x, lane = tid & 31;
+  const Gate own = fetch_gate(a, p);
   load_rows<D>(x, static_cast<const TI*>(a.k) + p.krow, a.sTk, p.n);
-  load_gates(gates, a, p);
+  make_gates(gates, own);
   {
     float acc[4][4];
     clear(acc);
-    product<C, C>(acc, D, [&](int i, int k) { return x[i][k]; }, [&](int k, int j) { return x[j][k]; });
-    each(acc, [&](int i, int j, float v) { n[i][j] = i > j ? v * decay(gates, i, j) * gates.beta[j] : 0.f; });
+    product<C, C>(acc, D, Along{x, PD}, Along{x, PD});
+    each(acc, [&](int i, int j, float v) { n[i * PC + j] = i > j ? v * decay(gates, i, j) * gates.beta[j] : 0.f; });
+  }
+  Rows<D> v;  // on their way until the keys are no longer needed
+  v.fetch(static_cast<const TI*>(a.v) + p.row, a.sT, p.n);
+  __syncthreads();
+  // the inverse: blocks of 32 on the diagonal by forward substitution, a warp each, a column to a lane; the one below is -T22 (n21 T11),
+  // made by way of the one above, which is zero
+  if (tid < 64) {
+    const int at = tid >> 5 << 5;
+    float y[32];
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+      float s[4] = {i == lane ? 1.f : 0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int m = 0; m < i; m += 4) {
+        const float4 w = *reinterpret_cast<const float4*>(n + (at + i) * PC + at + m);
+        s[0] = fmaf(-w.x, y[m], s[0]);
+        if (m + 1 < i) s[1] = fmaf(-w.y, y[m + 1], s[1]);
+        if (m + 2 < i) s[2] = fmaf(-w.z, y[m + 2], s[2]);
+        if (m + 3 < i) s[3] = fmaf(-w.w, y[m + 3], s[3]);
+      }
+      y[i] = (s[0] + s[1]) + (s[2] + s[3]);
+      t[(at + i) * PC + at + lane] = y[i];
+    }
   }
   __syncthreads();
-  // column j of the inverse by forward substitution, four threads to a column
-  const int j = threadIdx.x >> 2, part = threadIdx.x & 3;
-  for (int i = 0; i < C; ++i) {
-    float v = 0.f;
-    for (int m = j + part; m < i; m += 4) v = fmaf(n[i][m], t[m][j], v);
-    v += __shfl_xor_sync(0xffffffffu, v, 1);
-    v += __shfl_xor_sync(0xffffffffu, v, 2);
-    if (part == 0) t[i][j] = i < j ? 0.f : (i == j ? 1.f : 0.f) - v;
-    __syncwarp();
+  {
+    const int r = tid >> 3, c = (tid & 7) * 4;
+    auto block = [&](const float* left, const float* right, float sign, float* to) {  // [32, 32], four columns of a row to a thread
+      float s[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+      for (int m = 0; m < 32; ++m) {
+        const float l = left[r * PC + m];
+        const float4 w = *reinterpret_cast<const float4*>(right + m * PC + c);
+        s[0] = fmaf(l, w.x, s[0]);
+        s[1] = fmaf(l, w.y, s[1]);
+        s[2] = fmaf(l, w.z, s[2]);
+        s[3] = fmaf(l, w.w, s[3]);
+      }
+      *reinterpret_cast<float4*>(to + r * PC + c) = make_float4(sign * s[0], sign * s[1], sign * s[2], sign * s[3]);
+    };
+    block(n + 32 * PC, t, 1.f, t + 32);
+    __syncthreads();
+    block(t + 32 * PC + 32, t + 32, -1.f, t + 32 * PC);
+    __syncthreads();
+    *reinterpret_cast<float4*>(t + r * PC + 32 + c) = make_float4(0.f, 0.f, 0.f, 0.f);
   }
   __syncthreads();
 #pragma unroll 8
-  for (int i = threadIdx.x; i < C * C; i += THREADS) rec[Record<D>::T + i] = t[i / C][i % C];
+  for (int i = tid; i < C * C; i += THREADS) rec[Record<D>::T + i] = t[i / C * PC + i % C];
   float acc[4][D / 16];
   clear(acc);
-  product<C, D>(acc, C, [&](int i, int k) { return t[i][k] * gates.since[k]; }, [&](int k, int c) { return x[k][c]; });
-  each(acc, [&](int i, int c, float v) { rec[Record<D>::W + i * D + c] = v; });
+  product<C, D>(acc, C, times_k(Along{t, PC}, gates.since), Across{x, PD});
+  each(acc, [&](int i, int c, float w) { rec[Record<D>::W + i * D + c] = w; });
   __syncthreads();
-  load_rows<D>(x, static_cast<const TI*>(a.v) + p.row, a.sT, p.n);
+  v.put(x);
   __syncthreads();
   clear(acc);
-  product<C, D>(acc, C, [&](int i, int k) { return t[i][k]; }, [&](int k, int c) { return x[k][c]; });
-  each(acc, [&](int i, int c, float v) { rec[Record<D>::Y + i * D + c] = v; });
+  product<C, D>(acc, C, Along{t, PC}, Across{x, PD});
+  each(acc, [&](int i, int c, float u) { rec[Record<D>::Y + i * D + c] = u; });
 }
 
 // ---- the walk: S entering every chunk, Y -------------------------------------------------------------------------------------------
 template <typename TI, int D>
 __global__ void __launch_bounds__(THREADS) delta_walk_kernel(const DeltaArgs a) {
   extern __shared__ float smem[];
-  auto k = reinterpret_cast<float(*)[D + 1]>(smem);
-  auto w = k + C;
-  auto s = reinterpret_cast<float(*)[SLICE + 1]>(smem + 2 * C * (D + 1));
-  auto y = s + D;
+  constexpr int PD = D + 4, PS = SLICE + 1;
+  float* const k = smem;
+  float* const w = k + C * PD;
+  float* const s = w + C * PD;
+  float* const y = s + D * PS;
   __shared__ Gates gates;
   grid_dep_wait();
   grid_dep_launch();
-  const int bh = blockIdx.y, e0 = blockIdx.x * SLICE;
+  const int bh = blockIdx.y, e0 = blockIdx.x * SLICE, tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
 #pragma unroll 8
   for (int i = threadIdx.x; i < D * SLICE; i += THREADS)
-    s[i / SLICE][i % SLICE] = a.kv_in ? a.kv_in[((size_t)bh * D + i / SLICE) * D + e0 + i % SLICE] : 0.f;
-  for (int c = 0; c < a.nchunk; ++c) {
+    s[i / SLICE * PS + i % SLICE] = a.kv_in ? a.kv_in[((size_t)bh * D + i / SLICE) * D + e0 + i % SLICE] : 0.f;
+  // a chunk's inputs come while the one before is worked on
+  Rows<D> keys, whats;
+  float uhat[4][2];
+  Gate gate;
+  auto record = [&](int c) { return static_cast<float*>(a.ws) + ((size_t)bh * a.nchunk + c) * Record<D>::FWD; };
+  auto fetch = [&](int c) {
     const Place p = place(a, bh, c);
-    float* rec = static_cast<float*>(a.ws) + p.rec * Record<D>::FWD;
-    __syncthreads();
-    load_rows<D>(k, static_cast<const TI*>(a.k) + p.krow, a.sTk, p.n);
-    load_rows<D>(w, rec + Record<D>::W, D, C);
-    load_gates(gates, a, p);
-#pragma unroll 8
-    for (int i = threadIdx.x; i < D * SLICE; i += THREADS) rec[Record<D>::S + (i / SLICE) * D + e0 + i % SLICE] = s[i / SLICE][i % SLICE];
+    gate = fetch_gate(a, p);
+    keys.fetch(static_cast<const TI*>(a.k) + p.krow, a.sTk, p.n);
+    whats.fetch(record(c) + Record<D>::W, D, C);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) uhat[i][j] = record(c)[Record<D>::Y + (ty + 16 * i) * D + e0 + tx + 16 * j];
+  };
+  fetch(0);
+  for (int c = 0; c < a.nchunk; ++c) {
+    float* const rec = record(c);
     float acc[4][2];
-    clear(acc);
-    product<C, SLICE>(acc, D, [&](int i, int x) { return w[i][x]; }, [&](int x, int e) { return s[x][e]; });
+    __syncthreads();
+    keys.put(k);
+    whats.put(w);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) acc[i][j] = -uhat[i][j];
+    make_gates(gates, gate);
+    if (c + 1 < a.nchunk) fetch(c + 1);
+#pragma unroll 8
+    for (int i = threadIdx.x; i < D * SLICE; i += THREADS) rec[Record<D>::S + (i / SLICE) * D + e0 + i % SLICE] = s[i / SLICE * PS + i % SLICE];
+    product<C, SLICE>(acc, D, Along{w, PD}, Across{s, PS});
     each(acc, [&](int i, int e, float v) {
-      float* at = rec + Record<D>::Y + i * D + e0 + e;
-      const float got = *at - v;
-      *at = got;
-      y[i][e] = got * (gates.beta[i] * gates.until[i]);
+      rec[Record<D>::Y + i * D + e0 + e] = -v;
+      y[i * PS + e] = -v * (gates.beta[i] * gates.until[i]);
     });
     __syncthreads();
     float next[D / 16][2];
     clear(next);
-    product<D, SLICE>(next, C, [&](int x, int i) { return k[i][x]; }, [&](int i, int e) { return y[i][e]; });
-    each(next, [&](int x, int e, float v) { s[x][e] = fmaf(gates.all, s[x][e], v); });
+    product<D, SLICE>(next, C, Across{k, PD}, Across{y, PS});
+    each(next, [&](int x, int e, float v) { s[x * PS + e] = fmaf(gates.all, s[x * PS + e], v); });
   }
   __syncthreads();
   if (a.kv_out)
 #pragma unroll 8
     for (int i = threadIdx.x; i < D * SLICE; i += THREADS)
-      a.kv_out[((size_t)bh * D + i / SLICE) * D + e0 + i % SLICE] = s[i / SLICE][i % SLICE];
+      a.kv_out[((size_t)bh * D + i / SLICE) * D + e0 + i % SLICE] = s[i / SLICE * PS + i % SLICE];
 }
 
 // ---- O ------------------------------------------------------------------------------------------------------------------------------
 template <typename TI, typename TO, int D>
 __global__ void __launch_bounds__(THREADS) delta_output_kernel(const DeltaArgs a) {
   extern __shared__ float smem[];
-  auto q = reinterpret_cast<float(*)[D + 1]>(smem);
-  auto k = q + C;
-  auto f = reinterpret_cast<float(*)[C + 1]>(smem + 2 * C * (D + 1));
+  constexpr int PD = D + 4;
+  float* const q = smem;
+  float* const k = q + C * PD;
+  float* const f = k + C * PD;
   __shared__ Gates gates;
   grid_dep_wait();
   grid_dep_launch();
@@ -223,18 +353,18 @@ __global__ void __launch_bounds__(THREADS) delta_output_kernel(const DeltaArgs a
   {
     float acc[4][4];
     clear(acc);
-    product<C, C>(acc, D, [&](int i, int x) { return q[i][x]; }, [&](int x, int j) { return k[j][x]; });
-    each(acc, [&](int i, int j, float v) { f[i][j] = i >= j ? v * decay(gates, i, j) * gates.beta[j] : 0.f; });
+    product<C, C>(acc, D, Along{q, PD}, Along{k, PD});
+    each(acc, [&](int i, int j, float v) { f[i * PC + j] = i >= j ? v * decay(gates, i, j) * gates.beta[j] : 0.f; });
   }
   __syncthreads();
   float acc[4][D / 16];
   clear(acc);
-  product<C, D>(acc, D, [&](int i, int x) { return q[i][x]; }, [&](int x, int e) { return rec[Record<D>::S + x * D + e]; });
+  product<C, D>(acc, D, Along{q, PD}, Across{rec + Record<D>::S, D});
 #pragma unroll
   for (int i = 0; i < 4; ++i)
 #pragma unroll
     for (int j = 0; j < D / 16; ++j) acc[i][j] *= gates.since[(threadIdx.x >> 4) + 16 * i];
-  product<C, D>(acc, C, [&](int i, int x) { return f[i][x]; }, [&](int x, int e) { return rec[Record<D>::Y + x * D + e]; });
+  product<C, D>(acc, C, Along{f, PC}, Across{rec + Record<D>::Y, D});
   TO* o = static_cast<TO*>(a.o) + p.row;
   each(acc, [&](int i, int e, float v) {
     if (i < p.n) o[i * a.sT + e] = from_f32<TO>(a.scale * v);
@@ -245,9 +375,10 @@ __global__ void __launch_bounds__(THREADS) delta_output_kernel(const DeltaArgs a
 template <typename TI, int D>
 __global__ void __launch_bounds__(THREADS) delta_scores_kernel(const DeltaArgs a) {
   extern __shared__ float smem[];
-  auto q = reinterpret_cast<float(*)[D + 1]>(smem);
-  auto k = q + C;
-  auto f = reinterpret_cast<float(*)[C + 1]>(smem + 2 * C * (D + 1));
+  constexpr int PD = D + 4;
+  float* const q = smem;
+  float* const k = q + C * PD;
+  float* const f = k + C * PD;
   __shared__ Gates gates;
   grid_dep_wait();
   grid_dep_launch();
@@ -259,15 +390,15 @@ __global__ void __launch_bounds__(THREADS) delta_scores_kernel(const DeltaArgs a
   {
     float acc[4][4];
     clear(acc);
-    product<C, C>(acc, D, [&](int i, int x) { return q[i][x]; }, [&](int x, int j) { return k[j][x]; });
-    each(acc, [&](int i, int j, float v) { f[i][j] = i >= j ? v * decay(gates, i, j) : 0.f; });
+    product<C, C>(acc, D, Along{q, PD}, Along{k, PD});
+    each(acc, [&](int i, int j, float v) { f[i * PC + j] = i >= j ? v * decay(gates, i, j) : 0.f; });
   }
   __syncthreads();
   load_rows<D>(q, static_cast<const TI*>(a.d_o) + p.row, a.sT, p.n);
   __syncthreads();
   float acc[4][D / 16];
   clear(acc);
-  product<C, D>(acc, C, [&](int j, int t) { return f[t][j]; }, [&](int t, int e) { return q[t][e]; });
+  product<C, D>(acc, C, Across{f, PC}, Across{q, PD});
   each(acc, [&](int j, int e, float v) { rec[Record<D>::L + j * D + e] = a.scale * v; });
 }
 
@@ -275,70 +406,96 @@ __global__ void __launch_bounds__(THREADS) delta_scores_kernel(const DeltaArgs a
 template <typename TI, int D>
 __global__ void __launch_bounds__(THREADS) delta_walk_back_kernel(const DeltaArgs a) {
   extern __shared__ float smem[];
-  auto k = reinterpret_cast<float(*)[D + 1]>(smem);
-  auto w = k + C;
-  auto q = w + C;
-  auto s = reinterpret_cast<float(*)[SLICE + 1]>(smem + 3 * C * (D + 1));
-  auto y = s + D;
-  auto d_o = y + C;
+  constexpr int PD = D + 4, PS = SLICE + 1;
+  float* const k = smem;
+  float* const w = k + C * PD;
+  float* const q = w + C * PD;
+  float* const s = q + C * PD;
+  float* const y = s + D * PS;
+  float* const d_o = y + C * PS;
   __shared__ Gates gates;
   grid_dep_wait();
   grid_dep_launch();
-  const int bh = blockIdx.y, e0 = blockIdx.x * SLICE;
+  const int bh = blockIdx.y, e0 = blockIdx.x * SLICE, tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
 #pragma unroll 8
   for (int i = threadIdx.x; i < D * SLICE; i += THREADS)
-    s[i / SLICE][i % SLICE] = a.grad_kv_out ? a.grad_kv_out[((size_t)bh * D + i / SLICE) * D + e0 + i % SLICE] : 0.f;
-  for (int c = a.nchunk - 1; c >= 0; --c) {
+    s[i / SLICE * PS + i % SLICE] = a.grad_kv_out ? a.grad_kv_out[((size_t)bh * D + i / SLICE) * D + e0 + i % SLICE] : 0.f;
+  Rows<D> keys, queries, whats;
+  Rows<SLICE, PS> outs;
+  float scores[4][2];
+  Gate gate;
+  auto record = [&](int c) { return static_cast<float*>(a.ws_bwd) + ((size_t)bh * a.nchunk + c) * Record<D>::BWD; };
+  auto fetch = [&](int c) {
     const Place p = place(a, bh, c);
-    const float* fwd = static_cast<const float*>(a.ws) + p.rec * Record<D>::FWD;
-    float* rec = static_cast<float*>(a.ws_bwd) + p.rec * Record<D>::BWD;
+    gate = fetch_gate(a, p);
+    keys.fetch(static_cast<const TI*>(a.k) + p.krow, a.sTk, p.n);
+    queries.fetch(static_cast<const TI*>(a.q) + p.krow, a.sTk, p.n);
+    whats.fetch(static_cast<const float*>(a.ws) + p.rec * Record<D>::FWD + Record<D>::W, D, C);
+    outs.fetch(static_cast<const TI*>(a.d_o) + p.row + e0, a.sT, p.n);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) scores[i][j] = record(c)[Record<D>::L + (ty + 16 * i) * D + e0 + tx + 16 * j];
+  };
+  fetch(a.nchunk - 1);
+  for (int c = a.nchunk - 1; c >= 0; --c) {
+    float* const rec = record(c);
+    float from_scores[4][2];
     __syncthreads();
-    load_rows<D>(k, static_cast<const TI*>(a.k) + p.krow, a.sTk, p.n);
-    load_rows<D>(q, static_cast<const TI*>(a.q) + p.krow, a.sTk, p.n);
-    load_rows<D>(w, fwd + Record<D>::W, D, C);
-    load_gates(gates, a, p);
-    const TI* const in = static_cast<const TI*>(a.d_o) + p.row + e0;
+    keys.put(k);
+    queries.put(q);
+    whats.put(w);
+    outs.put(d_o);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) from_scores[i][j] = scores[i][j];
+    make_gates(gates, gate);
+    if (c) fetch(c - 1);
 #pragma unroll 8
-    for (int i = threadIdx.x; i < C * SLICE; i += THREADS) {
-      const int t = i / SLICE;
-      d_o[t][i % SLICE] = t < p.n ? to_f32(in[t * a.sT + i % SLICE]) * (a.scale * gates.since[t]) : 0.f;
-    }
-#pragma unroll 8
-    for (int i = threadIdx.x; i < D * SLICE; i += THREADS) rec[Record<D>::E + (i / SLICE) * D + e0 + i % SLICE] = s[i / SLICE][i % SLICE];
+    for (int i = threadIdx.x; i < D * SLICE; i += THREADS) rec[Record<D>::E + (i / SLICE) * D + e0 + i % SLICE] = s[i / SLICE * PS + i % SLICE];
     float acc[4][2];
     clear(acc);
-    product<C, SLICE>(acc, D, [&](int i, int x) { return k[i][x]; }, [&](int x, int e) { return s[x][e]; });
-    each(acc, [&](int i, int e, float v) {
-      float* at = rec + Record<D>::L + i * D + e0 + e;
-      const float got = fmaf(gates.until[i], v, *at);
-      *at = got;
-      y[i][e] = -got * gates.beta[i];
-    });
+    product<C, SLICE>(acc, D, Along{k, PD}, Across{s, PS});
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const int r = ty + 16 * i, e = tx + 16 * j;
+        const float got = fmaf(gates.until[r], acc[i][j], from_scores[i][j]);
+        rec[Record<D>::L + r * D + e0 + e] = got;
+        y[r * PS + e] = -got * gates.beta[r];
+        d_o[r * PS + e] *= a.scale * gates.since[r];
+      }
     __syncthreads();
     float next[D / 16][2];
     clear(next);
-    product<D, SLICE>(next, C, [&](int x, int i) { return q[i][x]; }, [&](int i, int e) { return d_o[i][e]; });
-    product<D, SLICE>(next, C, [&](int x, int i) { return w[i][x]; }, [&](int i, int e) { return y[i][e]; });
-    each(next, [&](int x, int e, float v) { s[x][e] = fmaf(gates.all, s[x][e], v); });
+    product<D, SLICE>(next, C, Across{q, PD}, Across{d_o, PS});
+    product<D, SLICE>(next, C, Across{w, PD}, Across{y, PS});
+    each(next, [&](int x, int e, float v) { s[x * PS + e] = fmaf(gates.all, s[x * PS + e], v); });
   }
   __syncthreads();
   if (a.grad_kv_in)
 #pragma unroll 8
     for (int i = threadIdx.x; i < D * SLICE; i += THREADS)
-      a.grad_kv_in[((size_t)bh * D + i / SLICE) * D + e0 + i % SLICE] = s[i / SLICE][i % SLICE];
+      a.grad_kv_in[((size_t)bh * D + i / SLICE) * D + e0 + i % SLICE] = s[i / SLICE * PS + i % SLICE];
 }
 
 // ---- backward: gradients.  A thread block per key head and chunk takes the value heads of the group in order. --------------------------
 template <typename TI, typename TO, int D>
 __global__ void __launch_bounds__(THREADS) delta_grad_kernel(const DeltaArgs a) {
   extern __shared__ float smem[];
-  auto y = reinterpret_cast<float(*)[D + 1]>(smem);
-  auto d_o = y + C;  // that of dV' before
-  auto dr = d_o + C;
-  auto f = reinterpret_cast<float(*)[C + 1]>(smem + 3 * C * (D + 1));
-  auto h = f + C;
-  auto z = h + C;
-  float* const st = smem + 3 * C * (D + 1) + 3 * C * (C + 1);  // [D][D + 1]: S, then E'
+  constexpr int PD = D + 4;
+  constexpr bool KEPT = D == 64;  // keys and queries stay in shared memory (D = 128: in the state's place, until it comes)
+  float* const y = smem;
+  float* const d_o = y + C * PD;  // that of dV' before
+  float* const dr = d_o + C * PD;
+  float* const f = dr + C * PD;
+  float* const h = f + C * PC;  // That, then -H
+  float* const z = h + C * PC;
+  float* const st = z + C * PC;  // [D][PD]: S, then E'
+  float* const ks = KEPT ? st + D * PD : st;
+  float* const qs = ks + C * PD;
   __shared__ Gates gates;
   __shared__ float row_a[C], row_b[C];
   __shared__ float part[THREADS / 32];
@@ -356,57 +513,72 @@ __global__ void __launch_bounds__(THREADS) delta_grad_kernel(const DeltaArgs a) 
     const float* rec = static_cast<const float*>(a.ws_bwd) + p.rec * Record<D>::BWD;
     const TI* const kk = static_cast<const TI*>(a.k) + p.krow;
     const TI* const qq = static_cast<const TI*>(a.q) + p.krow;
-    auto key = [&](int t, int x) { return t < p.n ? to_f32(kk[t * a.sTk + x]) : 0.f; };
-    auto query = [&](int t, int x) { return t < p.n ? to_f32(qq[t * a.sTk + x]) : 0.f; };
+    auto key = [&](int t, int x) { return KEPT ? ks[t * PD + x] : t < p.n ? to_f32(kk[t * a.sTk + x]) : 0.f; };
+    auto query = [&](int t, int x) { return KEPT ? qs[t * PD + x] : t < p.n ? to_f32(qq[t * a.sTk + x]) : 0.f; };
+    auto load_state = [&](const float* from) {
+#pragma unroll 16
+      for (int i = tid; i < D * D; i += THREADS) st[i / D * PD + i % D] = from[i];
+    };
     __syncthreads();
-    load_gates(gates, a, p);
-    load_rows<D>(y, fwd + Record<D>::Y, D, C);
-    load_rows<D>(d_o, rec + Record<D>::L, D, C);
-#pragma unroll 8
-    for (int i = tid; i < C * C; i += THREADS) h[i / C][i % C] = fwd[Record<D>::T + i];
-    __syncthreads();
+    {
+      const Gate own = fetch_gate(a, p);
+      Rows<D> r0, r1;
+      r0.fetch(fwd + Record<D>::Y, D, C);
+      r1.fetch(rec + Record<D>::L, D, C);
+      r0.put(y);
+      r1.put(d_o);
+#pragma unroll
+      for (int i = tid; i < C * C; i += THREADS) h[i / C * PC + i % C] = fwd[Record<D>::T + i];
+      if (!KEPT || gh == 0) {
+        r0.fetch(kk, a.sTk, p.n);
+        r1.fetch(qq, a.sTk, p.n);
+        r0.put(ks);
+        r1.put(qs);
+      }
+      make_gates(gates, own);
+    }
+    Rows<D> outs;
+    outs.fetch(static_cast<const TI*>(a.d_o) + p.row, a.sT, p.n);
     // dR = That^T diag(beta) dV', and dV' . Y
     {
       float acc[4][D / 16];
       clear(acc);
-      product<C, D>(acc, C, [&](int j, int i) { return h[i][j] * gates.beta[i]; }, [&](int i, int e) { return d_o[i][e]; });
+      product<C, D>(acc, C, times_k(Across{h, PC}, gates.beta), Across{d_o, PD});
       TO* dv = static_cast<TO*>(a.dv) + p.row;
       each(acc, [&](int j, int e, float v) {
-        dr[j][e] = v;
+        dr[j * PD + e] = v;
         if (j < p.n) dv[j * a.sT + e] = from_f32<TO>(v);
       });
     }
     float dbeta = 0.f;
     {
       const int t = tid >> 2;
-      for (int e = tid & 3; e < D; e += 4) dbeta = fmaf(d_o[t][e], y[t][e], dbeta);
+      for (int e = tid & 3; e < D; e += 4) dbeta = fmaf(d_o[t * PD + e], y[t * PD + e], dbeta);
     }
     __syncthreads();
-    load_rows<D>(d_o, static_cast<const TI*>(a.d_o) + p.row, a.sT, p.n);
-#pragma unroll 8
-    for (int i = tid; i < D * D; i += THREADS) st[(i / D) * (D + 1) + i % D] = fwd[Record<D>::S + i];
-    __syncthreads();
+    outs.put(d_o);
+    if (KEPT) load_state(fwd + Record<D>::S);
     // Hh, with the products of the keys for dbeta; F
     {
       float hh[4][4], n[4][4];
       clear(hh);
       clear(n);
-      product<C, C>(hh, D, [&](int i, int e) { return dr[i][e]; }, [&](int e, int j) { return y[j][e]; });
-      product<C, C>(n, D, [&](int i, int x) { return key(i, x); }, [&](int x, int j) { return key(j, x); });
+      product<C, C>(hh, D, Along{dr, PD}, Along{y, PD});
+      product<C, C>(n, D, Along{ks, PD}, Along{ks, PD});
 #pragma unroll
       for (int i = 0; i < 4; ++i)
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           const int r = ty + 16 * i, c = tx + 16 * j;
           const float v = r > c ? hh[i][j] * decay(gates, r, c) : 0.f;
-          h[r][c] = v;
-          f[r][c] = z[r][c] = r > c ? n[i][j] * v : 0.f;
+          h[r * PC + c] = -v;
+          f[r * PC + c] = z[r * PC + c] = r > c ? n[i][j] * v : 0.f;
         }
     }
     __syncthreads();
     {
       const int j = tid >> 2;
-      for (int i = tid & 3; i < C; i += 4) dbeta -= f[i][j];
+      for (int i = tid & 3; i < C; i += 4) dbeta -= f[i * PC + j];
       dbeta += __shfl_xor_sync(0xffffffffu, dbeta, 1);
       dbeta += __shfl_xor_sync(0xffffffffu, dbeta, 2);
       if ((tid & 3) == 0 && j < p.n) a.dbeta[p.gate + j * a.gT] = dbeta;
@@ -416,20 +588,37 @@ __global__ void __launch_bounds__(THREADS) delta_grad_kernel(const DeltaArgs a) 
       float acc[4][4], qk[4][4];
       clear(acc);
       clear(qk);
-      product<C, C>(acc, D, [&](int i, int e) { return d_o[i][e]; }, [&](int e, int j) { return y[j][e]; });
-      product<C, C>(qk, D, [&](int i, int x) { return query(i, x); }, [&](int x, int j) { return key(j, x); });
+      product<C, C>(acc, D, Along{d_o, PD}, Along{y, PD});
+      product<C, C>(qk, D, Along{qs, PD}, Along{ks, PD});
 #pragma unroll
       for (int i = 0; i < 4; ++i)
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           const int r = ty + 16 * i, c = tx + 16 * j;
           const float v = r >= c ? a.scale * acc[i][j] * decay(gates, r, c) * gates.beta[c] : 0.f;
-          f[r][c] = v;
-          h[r][c] *= gates.beta[c];
-          z[r][c] = fmaf(v, qk[i][j], -gates.beta[c] * z[r][c]);
+          f[r * PC + c] = v;
+          h[r * PC + c] *= gates.beta[c];
+          z[r * PC + c] = fmaf(v, qk[i][j], -gates.beta[c] * z[r * PC + c]);
         }
     }
     __syncthreads();
+    if (!KEPT) {
+      load_state(fwd + Record<D>::S);
+      __syncthreads();
+    }
+    for (int r = tid >> 5; r < C; r += THREADS / 32) {  // Z's sums along its rows: of the columns before s
+      const int lane = tid & 31;
+      const float2 v = *reinterpret_cast<const float2*>(z + r * PC + 2 * lane);
+      float x = v.x + v.y;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const float before = __shfl_up_sync(0xffffffffu, x, o);
+        if (lane >= o) x += before;
+      }
+      x = __shfl_up_sync(0xffffffffu, x, 1);
+      if (lane == 0) x = 0.f;
+      *reinterpret_cast<float2*>(z + r * PC + 2 * lane) = make_float2(x, x + v.x);
+    }
     // scales the rows of acc, and sums up the products of each with the same row of x over the sixteen threads that share it
     auto scaled_dots = [&](float(&acc)[4][D / 16], const float* with, float times, auto x, float(&dot)[4]) {
 #pragma unroll
@@ -447,50 +636,45 @@ __global__ void __launch_bounds__(THREADS) delta_grad_kernel(const DeltaArgs a) 
     float acc[4][D / 16], dot_q[4], dot[4];
     // dQ
     clear(acc);
-    product<C, D>(acc, D, [&](int i, int e) { return d_o[i][e]; }, [&](int e, int x) { return st[x * (D + 1) + e]; });
+    product<C, D>(acc, D, Along{d_o, PD}, Along{st, PD});
     scaled_dots(acc, gates.since, a.scale, query, dot_q);
-    product<C, D>(acc, C, [&](int i, int j) { return f[i][j]; }, [&](int j, int x) { return key(j, x); });
+    product<C, D>(acc, C, Along{f, PC}, of(key));
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
       for (int j = 0; j < D / 16; ++j) sum_q[i][j] += acc[i][j];
     // dK: what the keys read
     clear(acc);
-    product<C, D>(acc, D, [&](int i, int e) { return dr[i][e]; }, [&](int e, int x) { return st[x * (D + 1) + e]; });
-    scaled_dots(acc, gates.since, 1.f, key, dot);
+    product<C, D>(acc, D, Along{dr, PD}, Along{st, PD});
+    scaled_dots(acc, gates.since, -1.f, key, dot);
     if (tx == 0)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) row_a[ty + 16 * i] = dot_q[i] - dot[i];
-    product<C, D>(acc, C, [&](int i, int j) { return h[i][j]; }, [&](int j, int x) { return key(j, x); });
+      for (int i = 0; i < 4; ++i) row_a[ty + 16 * i] = dot_q[i] + dot[i];
+    product<C, D>(acc, C, Along{h, PC}, of(key));
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
-      for (int j = 0; j < D / 16; ++j) sum_k[i][j] -= acc[i][j];
+      for (int j = 0; j < D / 16; ++j) sum_k[i][j] += acc[i][j];
     float whole = 0.f;
-#pragma unroll 8
-    for (int i = tid; i < D * D; i += THREADS) whole = fmaf(st[(i / D) * (D + 1) + i % D], rec[Record<D>::E + i], whole);
-    whole *= gates.all;
     __syncthreads();
-#pragma unroll 8
-    for (int i = tid; i < D * D; i += THREADS) st[(i / D) * (D + 1) + i % D] = rec[Record<D>::E + i];
-    if (tid < C) {  // Z's sums along its rows: of the columns before s
-      float x = 0.f;
-      for (int s = 0; s < C; ++s) {
-        const float next = x + z[tid][s];
-        z[tid][s] = x;
-        x = next;
-      }
+#pragma unroll 16
+    for (int i = tid; i < D * D; i += THREADS) {  // each thread the elements that it put there: <S, E'>, and E' in S's place
+      float* const at = st + i / D * PD + i % D;
+      const float e = rec[Record<D>::E + i];
+      whole = fmaf(*at, e, whole);
+      *at = e;
     }
+    whole *= gates.all;
     __syncthreads();
     // dK: what the keys write
     clear(acc);
-    product<C, D>(acc, D, [&](int i, int e) { return y[i][e] * gates.beta[i]; }, [&](int e, int x) { return st[x * (D + 1) + e]; });
+    product<C, D>(acc, D, times_row(Along{y, PD}, gates.beta), Along{st, PD});
     scaled_dots(acc, gates.until, 1.f, key, dot);
     if (tx == 0)
 #pragma unroll
       for (int i = 0; i < 4; ++i) row_b[ty + 16 * i] = dot[i];
-    product<C, D>(acc, C, [&](int j, int t) { return f[t][j]; }, [&](int t, int x) { return query(t, x); });
-    product<C, D>(acc, C, [&](int j, int t) { return -h[t][j]; }, [&](int t, int x) { return key(t, x); });
+    product<C, D>(acc, C, Across{f, PC}, of(query));
+    product<C, D>(acc, C, Across{h, PC}, of(key));
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -499,12 +683,15 @@ __global__ void __launch_bounds__(THREADS) delta_grad_kernel(const DeltaArgs a) 
     for (int o = 16; o > 0; o >>= 1) whole += __shfl_xor_sync(0xffffffffu, whole, o);
     if ((tid & 31) == 0) part[tid >> 5] = whole;
     __syncthreads();
-    if (tid < p.n) {
+    {  // four threads to a token
+      const int t = tid >> 2;
       float x = 0.f;
+      for (int j = tid & 3; j < t; j += 4) x += row_b[j];
+      for (int i = t + (tid & 3); i < p.n; i += 4) x += z[i * PC + t] + row_a[i];
+      x += __shfl_xor_sync(0xffffffffu, x, 1);
+      x += __shfl_xor_sync(0xffffffffu, x, 2);
       for (int i = 0; i < THREADS / 32; ++i) x += part[i];
-      for (int j = 0; j < tid; ++j) x += row_b[j];
-      for (int i = p.n - 1; i >= tid; --i) x += z[i][tid] + row_a[i];
-      a.dg[p.gate + tid * a.gT] = x;
+      if ((tid & 3) == 0 && t < p.n) a.dg[p.gate + t * a.gT] = x;
     }
   }
   TO* const dq = static_cast<TO*>(a.dq) + p.krow;
@@ -531,26 +718,27 @@ cudaError_t start(K kern, int kind, dim3 grid, size_t floats, const DeltaArgs& a
 template <typename TI, int D>
 cudaError_t states(const DeltaArgs& a, cudaStream_t stream) {
   const dim3 chunks(a.nchunk, a.B * a.H), slices(D / SLICE, a.B * a.H);
-  const cudaError_t err = start(delta_prepare_kernel<TI, D>, K_PREPASS, chunks, C * (D + 1) + 2 * C * (C + 1), a, stream);
+  const cudaError_t err = start(delta_prepare_kernel<TI, D>, K_PREPASS, chunks, C * (D + 4) + 2 * C * PC, a, stream);
   if (err != cudaSuccess) return err;
-  return start(delta_walk_kernel<TI, D>, K_SCAN, slices, 2 * C * (D + 1) + (D + C) * (SLICE + 1), a, stream);
+  return start(delta_walk_kernel<TI, D>, K_SCAN, slices, 2 * C * (D + 4) + (D + C) * (SLICE + 1), a, stream);
 }
 template <typename TI, typename TO, int D>
 cudaError_t fwd_t(const DeltaArgs& a, cudaStream_t stream) {
   const cudaError_t err = states<TI, D>(a, stream);
   if (err != cudaSuccess) return err;
-  return start(delta_output_kernel<TI, TO, D>, K_WALK, dim3(a.nchunk, a.B * a.H), 2 * C * (D + 1) + C * (C + 1), a, stream);
+  return start(delta_output_kernel<TI, TO, D>, K_WALK, dim3(a.nchunk, a.B * a.H), 2 * C * (D + 4) + C * PC, a, stream);
 }
 template <typename TI, typename TO, int D>
 cudaError_t bwd_t(const DeltaArgs& a, bool have_fwd, cudaStream_t stream) {
   cudaError_t err = have_fwd ? cudaSuccess : states<TI, D>(a, stream);
   if (err != cudaSuccess) return err;
   const dim3 chunks(a.nchunk, a.B * a.H), slices(D / SLICE, a.B * a.H);
-  err = start(delta_scores_kernel<TI, D>, K_PREPASS, chunks, 2 * C * (D + 1) + C * (C + 1), a, stream);
+  err = start(delta_scores_kernel<TI, D>, K_PREPASS, chunks, 2 * C * (D + 4) + C * PC, a, stream);
   if (err != cudaSuccess) return err;
-  err = start(delta_walk_back_kernel<TI, D>, K_SCAN, slices, 3 * C * (D + 1) + (D + 2 * C) * (SLICE + 1), a, stream);
+  err = start(delta_walk_back_kernel<TI, D>, K_SCAN, slices, 3 * C * (D + 4) + (D + 2 * C) * (SLICE + 1), a, stream);
   if (err != cudaSuccess) return err;
-  return start(delta_grad_kernel<TI, TO, D>, K_WALK_PAIR, dim3(a.nchunk, a.B * a.Hk), 3 * C * (D + 1) + 3 * C * (C + 1) + D * (D + 1), a, stream);
+  return start(delta_grad_kernel<TI, TO, D>, K_WALK_PAIR, dim3(a.nchunk, a.B * a.Hk),
+               3 * C * (D + 4) + 3 * C * PC + D * (D + 4) + (D == 64 ? 2 * C * (D + 4) : 0), a, stream);
 }
 
 }  // namespace
