@@ -174,9 +174,13 @@ __global__ void __launch_bounds__(LANES > THREADS ? LANES : THREADS) block_norm_
   }
 }
 
+// From 512 threads to a row on, its values and the sums over tokens do not fit in the registers together: the sums are in shared memory
+// [3][D], and what a row has is read again (from L2) where it is used.
 template <typename T, typename TR, int LANES, int NV, bool VEC>
 __global__ void __launch_bounds__(LANES > THREADS ? LANES : THREADS) block_norm_bwd_kernel(const BlockNormArgs a) {
   constexpr int ROWS = (LANES > THREADS ? LANES : THREADS) / LANES;
+  constexpr bool WIDE = LANES >= 512;
+  extern __shared__ float wide_sums[];
   __shared__ RowSum<LANES, ROWS> sum;
   grid_dep_wait();
   grid_dep_launch();
@@ -184,23 +188,35 @@ __global__ void __launch_bounds__(LANES > THREADS ? LANES : THREADS) block_norm_
   const Cols<LANES, VEC> cols{(int)threadIdx.x % LANES, a.D};
   const float inv_d = 1.f / (float)a.D;
   const long long groups = (a.rows + ROWS - 1) / ROWS;
-  float g_post[NV][8], g_s[NV][8], g_pre[NV][8];
+  constexpr int NG = WIDE ? 1 : NV;
+  float g_post[NG][8], g_s[NG][8], g_pre[NG][8];
 #pragma unroll
-  for (int v = 0; v < NV; ++v)
+  for (int v = 0; v < NG; ++v)
 #pragma unroll
     for (int i = 0; i < 8; ++i) g_post[v][i] = g_s[v][i] = g_pre[v][i] = 0.f;
+  if (WIDE) {
+#pragma unroll
+    for (int v = 0; v < NV; ++v)
+#pragma unroll
+      for (int k = 0; k < 3; ++k) cols.store(wide_sums + k * a.D, v, g_post[0]);  // (zeros; everyone's own)
+  }
   for (long long group = blockIdx.x; group < groups; group += gridDim.x) {
     const long long row = group * ROWS + sub;
     const bool mine = row < a.rows;
     const long long at = mine ? row * a.D : 0;
     float y[NV][8], h[NV][8], u[NV][8], dn[NV][8];
+    auto get_y = [&](int v) { cols.load(static_cast<const T*>(a.y) + at, v, y[v]); };
+    auto get_u = [&](int v) { cols.load(a.u ? static_cast<const T*>(a.u) + at : nullptr, v, u[v]); };
+    auto get_dn = [&](int v) { cols.load(a.dn && mine ? static_cast<const T*>(a.dn) + at : nullptr, v, dn[v]); };
     float ss = 0.f;
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-      cols.load(static_cast<const T*>(a.y) + at, v, y[v]);
-      cols.load(static_cast<const TR*>(a.x) + at, v, h[v]);
-      cols.load(a.u ? static_cast<const T*>(a.u) + at : nullptr, v, u[v]);
-      cols.load(a.dn && mine ? static_cast<const T*>(a.dn) + at : nullptr, v, dn[v]);
+      get_y(v);
+      if (!WIDE) {
+        cols.load(static_cast<const TR*>(a.x) + at, v, h[v]);
+        get_u(v);
+        get_dn(v);
+      }
 #pragma unroll
       for (int i = 0; i < 8; ++i) ss = fmaf(y[v][i], y[v][i], ss);
     }
@@ -211,6 +227,12 @@ __global__ void __launch_bounds__(LANES > THREADS ? LANES : THREADS) block_norm_
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
       float w[8], s[8], wp[8];
+      if (WIDE) {
+        get_y(v);
+        cols.load(static_cast<const TR*>(a.x) + at, v, h[v]);
+        get_u(v);
+        get_dn(v);
+      }
       cols.load(a.w_post, v, w, 1.f);
       cols.load(a.s, v, s, 1.f);
       cols.load(a.w_pre, v, wp, 1.f);
@@ -231,7 +253,18 @@ __global__ void __launch_bounds__(LANES > THREADS ? LANES : THREADS) block_norm_
     float py = 0.f;
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-      float w[8], s[8], wp[8], dh[8], du[8];
+      float w[8], s[8], wp[8], dh[8], du[8], sum_post[8], sum_s[8], sum_pre[8];
+      if (WIDE) {
+        get_y(v);
+        get_u(v);
+        get_dn(v);
+        cols.load(wide_sums, v, sum_post);
+        cols.load(wide_sums + a.D, v, sum_s);
+        cols.load(wide_sums + 2 * a.D, v, sum_pre);
+      }
+      float* const to_post = WIDE ? sum_post : g_post[v % NG];
+      float* const to_s = WIDE ? sum_s : g_s[v % NG];
+      float* const to_pre = WIDE ? sum_pre : g_pre[v % NG];
       cols.load(a.w_post, v, w, 1.f);
       cols.load(a.s, v, s, 1.f);
       cols.load(a.w_pre, v, wp, 1.f);
@@ -242,18 +275,23 @@ __global__ void __launch_bounds__(LANES > THREADS ? LANES : THREADS) block_norm_
         float H = dh[i];
         if (a.dn) {
           H = fmaf(rh, dn[v][i] * wp[i] - nh * along, H);
-          g_pre[v][i] = fmaf(dn[v][i], nh, g_pre[v][i]);
+          to_pre[i] = fmaf(dn[v][i], nh, to_pre[i]);
         }
         dh[i] = H;
         float gate = 1.f, slope = 0.f;
         if (a.u) gate = act(a.gate, u[v][i], slope);
         if (mine) {
-          g_s[v][i] = fmaf(H, yh * w[i] * gate, g_s[v][i]);
-          g_post[v][i] = fmaf(H * s[i], yh * gate, g_post[v][i]);
+          to_s[i] = fmaf(H, yh * w[i] * gate, to_s[i]);
+          to_post[i] = fmaf(H * s[i], yh * gate, to_post[i]);
         }
         du[i] = H * s[i] * yh * w[i] * slope;
         h[v][i] = H * s[i] * gate * w[i];  // p
         py = fmaf(h[v][i], yh, py);
+      }
+      if (WIDE) {
+        cols.store(wide_sums, v, sum_post);
+        cols.store(wide_sums + a.D, v, sum_s);
+        cols.store(wide_sums + 2 * a.D, v, sum_pre);
       }
       if (mine) cols.store(static_cast<TR*>(a.dx) + at, v, dh);
       if (mine && a.u) cols.store(static_cast<T*>(a.du) + at, v, du);
@@ -262,6 +300,7 @@ __global__ void __launch_bounds__(LANES > THREADS ? LANES : THREADS) block_norm_
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
       if (a.post_norm) {
+        if (WIDE) get_y(v);
 #pragma unroll
         for (int i = 0; i < 8; ++i) h[v][i] = ry * (h[v][i] - y[v][i] * ry * py);
       }
@@ -271,6 +310,16 @@ __global__ void __launch_bounds__(LANES > THREADS ? LANES : THREADS) block_norm_
   }
   // the thread block's part; where it has several rows at a time, their threads add up in order
   float* const part = a.parts + (size_t)blockIdx.x * 3 * a.D;
+  if (WIDE) {
+#pragma unroll
+    for (int v = 0; v < NV; ++v)
+#pragma unroll
+      for (int k = 0; k < 3; ++k) {
+        cols.load(wide_sums + k * a.D, v, g_post[0]);
+        cols.store(part + k * a.D, v, g_post[0]);
+      }
+    return;
+  }
   for (int r = 0; r < ROWS; ++r) {
     if (sub == r) {
 #pragma unroll
@@ -279,9 +328,9 @@ __global__ void __launch_bounds__(LANES > THREADS ? LANES : THREADS) block_norm_
         for (int i = 0; i < 8; ++i) {
           const int c = VEC ? (v * LANES + cols.lane) * 8 + i : (8 * v + i) * LANES + cols.lane;
           if (c >= a.D) continue;
-          part[c] = g_post[v][i] + (r > 0 ? part[c] : 0.f);
-          part[a.D + c] = g_s[v][i] + (r > 0 ? part[a.D + c] : 0.f);
-          part[2 * a.D + c] = g_pre[v][i] + (r > 0 ? part[2 * a.D + c] : 0.f);
+          part[c] = g_post[v % NG][i] + (r > 0 ? part[c] : 0.f);
+          part[a.D + c] = g_s[v % NG][i] + (r > 0 ? part[a.D + c] : 0.f);
+          part[2 * a.D + c] = g_pre[v % NG][i] + (r > 0 ? part[2 * a.D + c] : 0.f);
         }
     }
     __syncthreads();
@@ -372,6 +421,9 @@ struct RingRow {
     const int f = feature(u);
     if constexpr (VEC) {
       if (f < D) store8(at + f, x);
+    } else if (f >= 0 && f + 1 < D) {  // (the pair begins at an even element of the tensor)
+      if constexpr (sizeof(T) == 2) *reinterpret_cast<__nv_bfloat162*>(at + f) = __floats2bfloat162_rn(x[0], x[1]);
+      else *reinterpret_cast<float2*>(at + f) = make_float2(x[0], x[1]);
     } else {
       if (f >= 0 && f < D) at[f] = from_f32<T>(x[0]);
       if (f + 1 < D) at[f + 1] = from_f32<T>(x[1]);
@@ -483,12 +535,6 @@ __global__ void __launch_bounds__(RING, 1) block_norm_ring_kernel(const BlockNor
   const int wd = (a.D + 19) / 4 * 4;
   float *const w_s = w_post + wd, *const w_pre = w_s + wd;
   for (int i = threadIdx.x; i < S * stage_bytes / 16; i += RING) reinterpret_cast<uint4*>(ring)[i] = make_uint4(0u, 0u, 0u, 0u);  // units past the end stay zeros
-  for (int i = threadIdx.x; i < a.D; i += RING) {
-    const int at = Row::weight_at(i, a.D);
-    w_post[at] = a.w_post ? a.w_post[i] : 1.f;
-    w_s[at] = a.s ? a.s[i] : 1.f;
-    w_pre[at] = a.w_pre ? a.w_pre[i] : 1.f;
-  }
   __syncthreads();
   const int sub = threadIdx.x / LANES;
   const long long first = (long long)blockIdx.x * ROWS + sub, step = (long long)gridDim.x * ROWS;
@@ -506,20 +552,49 @@ __global__ void __launch_bounds__(RING, 1) block_norm_ring_kernel(const BlockNor
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
   };
+  // With eight features to a thread what is read, and the weights, stay in registers; with sixteen they are read again where they are used.
+  constexpr bool KEEP = NV == 1;
   float g_post[BWD ? U : 1][F], g_s[BWD ? U : 1][F], g_pre[BWD ? U : 1][F];
 #pragma unroll
   for (int u = 0; u < (BWD ? U : 1); ++u)
 #pragma unroll
     for (int i = 0; i < F; ++i) g_post[u][i] = g_s[u][i] = g_pre[u][i] = 0.f;
   for (int s = 0; s < S; ++s) fetch(first + s * step, s);
+  float k_post[KEEP ? U : 1][F], k_s[KEEP ? U : 1][F], k_pre[KEEP ? U : 1][F];
+  if constexpr (KEEP) {
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int i = 0; i < F; ++i) {
+        const int f = my.feature(u) + i;
+        const bool in = f >= 0 && f < a.D;
+        k_post[u][i] = in && a.w_post ? a.w_post[f] : 1.f;
+        k_s[u][i] = in && a.s ? a.s[f] : 1.f;
+        k_pre[u][i] = in && a.w_pre ? a.w_pre[f] : 1.f;
+      }
+  } else {
+    for (int i = threadIdx.x; i < a.D; i += RING) {
+      const int at = Row::weight_at(i, a.D);
+      w_post[at] = a.w_post ? a.w_post[i] : 1.f;
+      w_s[at] = a.s ? a.s[i] : 1.f;
+      w_pre[at] = a.w_pre ? a.w_pre[i] : 1.f;
+    }
+    __syncthreads();
+  }
+  auto weights = [&](const float(&kept)[KEEP ? U : 1][F], const float* at, int u, float (&x)[F]) {
+    if constexpr (KEEP) {
+#pragma unroll
+      for (int i = 0; i < F; ++i) x[i] = kept[u][i];
+    } else {
+      my.weights(at, u, x);
+    }
+  };
   int s = 0, slot = 0;
   for (long long row = first; row < a.rows; row += step) {
     if (S == 3) copies_wait<2>();
     else if (S == 2) copies_wait<1>();
     else copies_wait<0>();
     const unsigned char* const in = ring + s * stage_bytes;
-    // With eight features to a thread what is read stays in registers; with sixteen it is read again where it is used.
-    constexpr bool KEEP = NV == 1;
     float y[U][F], g[U][F], slope[U][F], dn[U][F], h[U][F];
     auto get_y = [&](int u) { my.template get<T>(in, u, y[u]); };
     auto get_gate = [&](int u) {
@@ -553,8 +628,8 @@ __global__ void __launch_bounds__(RING, 1) block_norm_ring_kernel(const BlockNor
       if (!KEEP) get_y(u);
       my.template get<TR>(in + at_x, u, x);
       get_gate(u);
-      my.weights(w_post, u, w);
-      my.weights(w_s, u, sc);
+      weights(k_post, w_post, u, w);
+      weights(k_s, w_s, u, sc);
       const uint64_t ry2 = f2_pack(ry, ry);
 #pragma unroll
       for (int i = 0; i < F; i += 2) {
@@ -565,7 +640,7 @@ __global__ void __launch_bounds__(RING, 1) block_norm_ring_kernel(const BlockNor
       }
       if (BWD) {
         my.template get<T>(in + at_dn, u, dn[u]);
-        my.weights(w_pre, u, w);
+        weights(k_pre, w_pre, u, w);
 #pragma unroll
         for (int i = 0; i < F; i += 2) sum_n = f2_fma(f2_mul(pair(dn[u], i), pair(w, i)), pair(h[u], i), sum_n);
       }
@@ -583,7 +658,7 @@ __global__ void __launch_bounds__(RING, 1) block_norm_ring_kernel(const BlockNor
 #pragma unroll
         for (int u = 0; u < U; ++u) {
           float w[F];
-          my.weights(w_pre, u, w);
+          weights(k_pre, w_pre, u, w);
 #pragma unroll
           for (int i = 0; i < F; ++i) w[i] *= h[u][i] * rh;
           my.put(static_cast<T*>(a.n), row, u, w);
@@ -606,7 +681,7 @@ __global__ void __launch_bounds__(RING, 1) block_norm_ring_kernel(const BlockNor
           my.template get<T>(in + at_dn, u, dn[u]);
         }
         my.template get<TR>(in + at_dh, u, dh);
-        my.weights(w_pre, u, w);
+        weights(k_pre, w_pre, u, w);
         const uint64_t rh2 = f2_pack(rh, rh), along2 = f2_pack(-along, -along), ry2 = f2_pack(ry, ry);
 #pragma unroll
         for (int i = 0; i < F; i += 2) {
@@ -615,8 +690,8 @@ __global__ void __launch_bounds__(RING, 1) block_norm_ring_kernel(const BlockNor
           unpair(f2_fma(n, nh, pair(g_pre[u], i)), g_pre[u], i);
         }
         my.put(static_cast<TR*>(a.dx), row, u, dh);
-        my.weights(w_post, u, w);
-        my.weights(w_s, u, sc);
+        weights(k_post, w_post, u, w);
+        weights(k_s, w_s, u, sc);
 #pragma unroll
         for (int i = 0; i < F; i += 2) {
           const uint64_t yh = f2_mul(pair(y[u], i), ry2), H = pair(dh, i), Hg = f2_mul(H, pair(g[u], i)), ws = pair(w, i), yw = f2_mul(yh, ws);
@@ -699,7 +774,10 @@ cudaError_t run(const BlockNormArgs& a, bool backward, cudaStream_t stream) {
   KernelTimer timer(K_GATE, stream);
   cudaError_t err;
   if (backward) {
-    err = launch_early(block_norm_bwd_kernel<T, TR, LANES, NV, VEC>, dim3((unsigned)(groups < a.nparts ? groups : a.nparts)), dim3(BLOCK), 0, stream, 1, a);
+    const int smem = LANES >= 512 ? 3 * a.D * 4 : 0;
+    err = cudaFuncSetAttribute(block_norm_bwd_kernel<T, TR, LANES, NV, VEC>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (err != cudaSuccess) return err;
+    err = launch_early(block_norm_bwd_kernel<T, TR, LANES, NV, VEC>, dim3((unsigned)(groups < a.nparts ? groups : a.nparts)), dim3(BLOCK), smem, stream, 1, a);
   } else {
     const long long cap = 148LL * 64;  // a few waves, then each thread block takes further rows
     err = launch_early(block_norm_fwd_kernel<T, TR, LANES, NV, VEC>, dim3((unsigned)(groups < cap ? groups : cap)), dim3(BLOCK), 0, stream, 1, a);
@@ -722,7 +800,7 @@ template <typename T, typename TR, int LANES, int NV, bool VEC, bool BWD>
 cudaError_t run_ring(const BlockNormArgs& a, cudaStream_t stream) {
   using Row = RingRow<LANES, NV, VEC>;
   constexpr int ROWS = RING / LANES, BT = Row::template bytes<T>(), BR = Row::template bytes<TR>();
-  const int stage = BT + BR + (a.u ? BT : 0) + (BWD ? BT + BR : 0), weights = 3 * ((a.D + 19) / 4 * 4) * 4;
+  const int stage = BT + BR + (a.u ? BT : 0) + (BWD ? BT + BR : 0), weights = NV == 1 ? 0 : 3 * ((a.D + 19) / 4 * 4) * 4;
   const int most = 227 * 1024 - 512;
   const int stages = 3 * stage + weights <= most ? 3 : 2 * stage + weights <= most ? 2 : 1;
   int smem = stages * stage + weights;
