@@ -347,8 +347,10 @@ __global__ void __launch_bounds__(LANES > THREADS ? LANES : THREADS) block_norm_
 // Rows whose width is no multiple of eight move in pairs of features, 4 bytes of bf16: where the width is odd a row begins in the middle
 // of a pair, every second one, and a group of threads takes rows of one kind only, so that a thread's features are the same in all.
 constexpr int RING = 512;
-__device__ __forceinline__ void copy16(uint32_t to, const void* from) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+template <int BYTES>
+__device__ __forceinline__ void copy(uint32_t to, const void* from) {
+  if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+  else asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(to), "l"(from) : "memory");
 }
 __device__ __forceinline__ void copy4(uint32_t to, const void* from, int bytes) {  // the rest of the four are zeros
   asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to), "l"(from), "r"(bytes) : "memory");
@@ -358,19 +360,24 @@ __device__ __forceinline__ void copies_wait() {
   asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
 
-// One tensor's place in a stage, and this thread's features of a row: unit u has features (u LANES + lane) F - shift .. + F - 1.
-template <int LANES, int NV, bool VEC>
+// One tensor's place in a stage, and this thread's features of a row: unit u has features (u LANES + lane) F - shift .. + F - 1.  F is
+// eight where all tensors are bf16 and four where one is fp32, 16 bytes of the wider type: neighbours' pieces touch, so that every
+// sector is asked for once.  (With eight of fp32, two pieces of a thread side by side: SIDEBYSIDE.)
+template <int LANES, int NV, int FEATURES>
 struct RingRow {
-  static constexpr int F = VEC ? 8 : 2, U = 8 * NV / F;
+  static constexpr int F = FEATURES, U = 8 * NV / F;
+  static constexpr bool VEC = F > 2;
+  template <bool BWD>
+  static constexpr bool kept() { return NV == 1 && (!BWD || F == 8); }  // the weights' place
   int lane, D, shift;
   long long total;  // features of the tensor
   __device__ __forceinline__ int feature(int u) const { return (u * LANES + lane) * F - shift; }
   template <typename T>
   static constexpr int bytes() { return RING * 8 * NV * (int)sizeof(T); }
-  // stage memory: unit u of thread t in 16- (4-) byte pieces at piece (k U + u) RING + t, k the piece of the unit
+  // stage memory: unit u of thread t in pieces of 16, 8 or 4 bytes at piece (k U + u) RING + t, k the piece of the unit
   template <typename T>
   __device__ __forceinline__ void fetch(uint32_t to, const T* base, long long row) const {
-    constexpr int PIECE = VEC ? 16 : 4, K = F * (int)sizeof(T) / PIECE, PER = F / K;  // pieces of a unit, features of a piece
+    constexpr int PIECE = F == 4 ? 4 * (int)sizeof(T) : VEC ? 16 : 4, K = F * (int)sizeof(T) / PIECE, PER = F / K;  // pieces of a unit, features of a piece
     const T* const at = base + row * D;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -380,7 +387,7 @@ struct RingRow {
         const uint32_t dst = to + (uint32_t)((k * U + u) * RING + threadIdx.x) * PIECE;
         const int g = f + k * PER;
         if (VEC) {
-          if (g < D) copy16(dst, at + g);
+          if (g < D) copy<PIECE>(dst, at + g);
         } else if (sizeof(T) == 4) {
           if (g >= 0 && g < D) copy4(dst, at + g, 4);
         } else if (g + 1 >= 0 && g < D) {
@@ -391,11 +398,15 @@ struct RingRow {
   }
   template <typename T>
   __device__ __forceinline__ void get(const unsigned char* from, int u, float (&x)[F]) const {
-    constexpr int PIECE = VEC ? 16 : 4, K = F * (int)sizeof(T) / PIECE;
+    constexpr int PIECE = F == 4 ? 4 * (int)sizeof(T) : VEC ? 16 : 4, K = F * (int)sizeof(T) / PIECE;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
       const unsigned char* const src = from + ((k * U + u) * RING + threadIdx.x) * PIECE;
-      if constexpr (VEC && sizeof(T) == 2) {
+      if constexpr (F == 4 && sizeof(T) == 2) {
+        const uint2 v = *reinterpret_cast<const uint2*>(src);
+        x[0] = __uint_as_float(v.x << 16), x[1] = __uint_as_float(v.x & 0xffff0000u);
+        x[2] = __uint_as_float(v.y << 16), x[3] = __uint_as_float(v.y & 0xffff0000u);
+      } else if constexpr (VEC && sizeof(T) == 2) {
         const uint4 v = *reinterpret_cast<const uint4*>(src);
         const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
@@ -419,7 +430,9 @@ struct RingRow {
   __device__ __forceinline__ void put(T* base, long long row, int u, const float (&x)[F]) const {
     T* const at = base + row * D;
     const int f = feature(u);
-    if constexpr (VEC) {
+    if constexpr (F == 4) {
+      if (f < D) Vec4<T>::store(at + f, x);
+    } else if constexpr (VEC) {
       if (f < D) store8(at + f, x);
     } else if (f >= 0 && f + 1 < D) {  // (the pair begins at an even element of the tensor)
       if constexpr (sizeof(T) == 2) *reinterpret_cast<__nv_bfloat162*>(at + f) = __floats2bfloat162_rn(x[0], x[1]);
@@ -429,12 +442,15 @@ struct RingRow {
       if (f + 1 < D) at[f + 1] = from_f32<T>(x[1]);
     }
   }
-  // [D] in shared memory, with a margin; VEC: the first four of every eight features, then the others, so that neighbours read without
+  // [D] in shared memory, with a margin; units of eight: the first four of every eight features, then the others, so that neighbours read without
   // conflicts (weight_at: where feature f is)
-  static __device__ __forceinline__ int weight_at(int f, int D) { return VEC ? (f & 4 ? D / 2 : 0) + (f >> 3) * 4 + (f & 3) : f; }
+  static __device__ __forceinline__ int weight_at(int f, int D) { return F == 8 ? (f & 4 ? D / 2 : 0) + (f >> 3) * 4 + (f & 3) : f; }
   __device__ __forceinline__ void weights(const float* w, int u, float (&x)[F]) const {
     const int f = feature(u);
-    if constexpr (VEC) {
+    if constexpr (F == 4) {
+      const float4 a = *reinterpret_cast<const float4*>(w + (f < D ? f : 0));
+      x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
+    } else if constexpr (VEC) {
       const int at = f < D ? f / 2 : 0;
       const float4 a = *reinterpret_cast<const float4*>(w + at), b = *reinterpret_cast<const float4*>(w + D / 2 + at);
       x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
@@ -521,7 +537,7 @@ __device__ __forceinline__ void gate_values(int kind, float (&g)[F], float (&slo
 
 template <typename T, typename TR, int LANES, int NV, bool VEC, bool BWD>
 __global__ void __launch_bounds__(RING, 1) block_norm_ring_kernel(const BlockNormArgs a, const int S) {
-  using Row = RingRow<LANES, NV, VEC>;
+  using Row = RingRow<LANES, NV, !VEC ? 2 : sizeof(TR) == 4 ? 4 : 8>;
   constexpr int F = Row::F, U = Row::U, ROWS = RING / LANES;
   constexpr int BT = Row::template bytes<T>(), BR = Row::template bytes<TR>();
   extern __shared__ __align__(16) unsigned char ring[];
@@ -552,16 +568,17 @@ __global__ void __launch_bounds__(RING, 1) block_norm_ring_kernel(const BlockNor
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
   };
-  // With eight features to a thread what is read, and the weights, stay in registers; with sixteen they are read again where they are used.
-  constexpr bool KEEP = NV == 1;
+  // With eight features to a thread what is read stays in registers, with sixteen it is read again where it is used.  The weights stay
+  // there too where they leave enough: forward, and backward where units are of eight.
+  constexpr bool KEEP = NV == 1, KEPT = Row::template kept<BWD>();
   float g_post[BWD ? U : 1][F], g_s[BWD ? U : 1][F], g_pre[BWD ? U : 1][F];
 #pragma unroll
   for (int u = 0; u < (BWD ? U : 1); ++u)
 #pragma unroll
     for (int i = 0; i < F; ++i) g_post[u][i] = g_s[u][i] = g_pre[u][i] = 0.f;
   for (int s = 0; s < S; ++s) fetch(first + s * step, s);
-  float k_post[KEEP ? U : 1][F], k_s[KEEP ? U : 1][F], k_pre[KEEP ? U : 1][F];
-  if constexpr (KEEP) {
+  float k_post[KEPT ? U : 1][F], k_s[KEPT ? U : 1][F], k_pre[KEPT ? U : 1][F];
+  if constexpr (KEPT) {
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll
@@ -581,8 +598,8 @@ __global__ void __launch_bounds__(RING, 1) block_norm_ring_kernel(const BlockNor
     }
     __syncthreads();
   }
-  auto weights = [&](const float(&kept)[KEEP ? U : 1][F], const float* at, int u, float (&x)[F]) {
-    if constexpr (KEEP) {
+  auto weights = [&](const float(&kept)[KEPT ? U : 1][F], const float* at, int u, float (&x)[F]) {
+    if constexpr (KEPT) {
 #pragma unroll
       for (int i = 0; i < F; ++i) x[i] = kept[u][i];
     } else {
@@ -798,9 +815,9 @@ cudaError_t sum_parts(const BlockNormArgs& a, int n, cudaStream_t stream) {
 
 template <typename T, typename TR, int LANES, int NV, bool VEC, bool BWD>
 cudaError_t run_ring(const BlockNormArgs& a, cudaStream_t stream) {
-  using Row = RingRow<LANES, NV, VEC>;
+  using Row = RingRow<LANES, NV, !VEC ? 2 : sizeof(TR) == 4 ? 4 : 8>;
   constexpr int ROWS = RING / LANES, BT = Row::template bytes<T>(), BR = Row::template bytes<TR>();
-  const int stage = BT + BR + (a.u ? BT : 0) + (BWD ? BT + BR : 0), weights = NV == 1 ? 0 : 3 * ((a.D + 19) / 4 * 4) * 4;
+  const int stage = BT + BR + (a.u ? BT : 0) + (BWD ? BT + BR : 0), weights = Row::template kept<BWD>() ? 0 : 3 * ((a.D + 19) / 4 * 4) * 4;
   const int most = 227 * 1024 - 512;
   const int stages = 3 * stage + weights <= most ? 3 : 2 * stage + weights <= most ? 2 : 1;
   int smem = stages * stage + weights;
