@@ -359,6 +359,16 @@ template <int N>
 __device__ __forceinline__ void copies_wait() {
   asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
+constexpr int STAGES = 5;  // at most
+__device__ __forceinline__ void copies_wait(int n) {  // all but the last n stages
+  switch (n) {
+    case 0: copies_wait<0>(); break;
+    case 1: copies_wait<1>(); break;
+    case 2: copies_wait<2>(); break;
+    case 3: copies_wait<3>(); break;
+    default: copies_wait<4>();
+  }
+}
 
 // One tensor's place in a stage, and this thread's features of a row: unit u has features (u LANES + lane) F - shift .. + F - 1.  F is
 // eight where all tensors are bf16 and four where one is fp32, 16 bytes of the wider type: neighbours' pieces touch, so that every
@@ -461,28 +471,51 @@ struct RingRow {
   }
 };
 
-// Sums of one or two values over a row's threads: over each warp's lanes, then every warp adds up the warps' sums the same way.
+// Sums of values over a row's threads: over each warp's lanes, then every warp adds up the warps' sums the same way.
 template <int LANES>
 struct RowSums {
-  float part[2][2][RING / 32];
-  template <int N>
-  __device__ __forceinline__ void operator()(float (&x)[N], int& slot) {
-    constexpr int W = LANES / 32;
+  static constexpr int W = LANES / 32;
+  float part[2][8][20];  // slot, value, warp; the pitch keeps the lanes of several() apart
+  __device__ __forceinline__ void meet() const { asm volatile("bar.sync %0, %1;" ::"r"(1 + (int)threadIdx.x / LANES), "n"(LANES) : "memory"); }
+  __device__ __forceinline__ float one(float x, int& slot) {
 #pragma unroll
-    for (int n = 0; n < N; ++n)
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) x[n] += __shfl_xor_sync(0xffffffffu, x[n], o);
-    if (W <= 1) return;
+    for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+    if (W <= 1) return x;
     const int warp = threadIdx.x / 32, lane = threadIdx.x & 31, first = warp / W * W;
-    if (lane < N) part[slot][lane][warp] = lane == 0 ? x[0] : x[N - 1];
-    asm volatile("bar.sync %0, %1;" ::"r"(1 + first / W), "n"(LANES) : "memory");
+    if (lane == 0) part[slot][0][warp] = x;
+    meet();
+    x = part[slot][0][first + lane % W];
 #pragma unroll
-    for (int n = 0; n < N; ++n) {
-      x[n] = part[slot][n][first + lane % W];
-#pragma unroll
-      for (int o = W / 2; o > 0; o >>= 1) x[n] += __shfl_xor_sync(0xffffffffu, x[n], o);
-    }
+    for (int o = W / 2; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
     slot ^= 1;  // (written again behind the next sum's barrier)
+    return x;
+  }
+  // eight at once, by halves: four lanes end up with one value's sum
+  __device__ __forceinline__ void several(float (&x)[8], int& slot) {
+    const int warp = threadIdx.x / 32, lane = threadIdx.x & 31, first = warp / W * W;
+#pragma unroll
+    for (int o = 16, n = 4; o >= 4; o >>= 1, n >>= 1)
+#pragma unroll
+      for (int i = 0; i < n; ++i) {
+        const float keep = lane & o ? x[n + i] : x[i], give = lane & o ? x[i] : x[n + i];
+        x[i] = keep + __shfl_xor_sync(0xffffffffu, give, o);
+      }
+    float v = x[0];
+    v += __shfl_xor_sync(0xffffffffu, v, 2);
+    v += __shfl_xor_sync(0xffffffffu, v, 1);
+    if (W > 1) {
+      if ((lane & 3) == 0) part[slot][lane >> 2][warp] = v;
+      meet();
+      v = 0.f;
+#pragma unroll
+      for (int w = 0; w < W; w += 4)
+        if (w + (lane & 3) < W) v += part[slot][lane >> 2][first + w + (lane & 3)];
+      v += __shfl_xor_sync(0xffffffffu, v, 2);
+      v += __shfl_xor_sync(0xffffffffu, v, 1);
+      slot ^= 1;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = __shfl_sync(0xffffffffu, v, 4 * i);
   }
 };
 
@@ -607,71 +640,59 @@ __global__ void __launch_bounds__(RING, 1) block_norm_ring_kernel(const BlockNor
     }
   };
   int s = 0, slot = 0;
-  for (long long row = first; row < a.rows; row += step) {
-    if (S == 3) copies_wait<2>();
-    else if (S == 2) copies_wait<1>();
-    else copies_wait<0>();
-    const unsigned char* const in = ring + s * stage_bytes;
-    float y[U][F], g[U][F], slope[U][F], dn[U][F], h[U][F];
-    auto get_y = [&](int u) { my.template get<T>(in, u, y[u]); };
-    auto get_gate = [&](int u) {
-      if (a.u) {
-        my.template get<T>(in + at_u, u, g[u]);
-        if (BWD) gate_values(a.gate, g[u], slope[u]);
-        else gate_values(a.gate, g[u]);
-      } else {
+  float y[U][F], g[U][F], slope[U][F], h[U][F];
+  auto get_y = [&](const unsigned char* in, int u) { my.template get<T>(in, u, y[u]); };
+  auto get_gate = [&](const unsigned char* in, int u) {
+    if (a.u) {
+      my.template get<T>(in + at_u, u, g[u]);
+      if (BWD) gate_values(a.gate, g[u], slope[u]);
+      else gate_values(a.gate, g[u]);
+    } else {
 #pragma unroll
-        for (int i = 0; i < F; ++i) g[u][i] = 1.f, slope[u][i] = 0.f;
-      }
-    };
-    float ry = 1.f;
-    if (KEEP || a.post_norm) {
-      float ss[1] = {0.f};
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        get_y(u);
-#pragma unroll
-        for (int i = 0; i < F; ++i) ss[0] = fmaf(y[u][i], y[u][i], ss[0]);
-      }
-      if (a.post_norm) {
-        sums(ss, slot);
-        ry = inverse_rms(ss[0], inv_d, a.eps);
-      }
+      for (int i = 0; i < F; ++i) g[u][i] = 1.f, slope[u][i] = 0.f;
     }
-    uint64_t sum_h = 0, sum_n = 0;  // of h squared, of w_pre dn h, two at a time
+  };
+  auto square_of_y = [&](const unsigned char* in) {
+    uint64_t sum = 0;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      float x[F], w[F], sc[F];
-      if (!KEEP) get_y(u);
-      my.template get<TR>(in + at_x, u, x);
-      get_gate(u);
-      weights(k_post, w_post, u, w);
-      weights(k_s, w_s, u, sc);
-      const uint64_t ry2 = f2_pack(ry, ry);
+      float v[F];
+      my.template get<T>(in, u, v);
 #pragma unroll
-      for (int i = 0; i < F; i += 2) {
-        const uint64_t z = f2_mul(f2_mul(f2_mul(pair(y[u], i), ry2), pair(w, i)), pair(g[u], i));
-        const uint64_t v = f2_fma(pair(sc, i), z, pair(x, i));
-        unpair(v, h[u], i);
-        sum_h = f2_fma(v, v, sum_h);
-      }
-      if (BWD) {
-        my.template get<T>(in + at_dn, u, dn[u]);
-        weights(k_pre, w_pre, u, w);
-#pragma unroll
-        for (int i = 0; i < F; i += 2) sum_n = f2_fma(f2_mul(pair(dn[u], i), pair(w, i)), pair(h[u], i), sum_n);
-      }
-      if (!BWD && a.h) my.put(static_cast<TR*>(a.h), row, u, h[u]);
+      for (int i = 0; i < F; i += 2) sum = f2_fma(pair(v, i), pair(v, i), sum);
     }
-    float both[2];
-    both[0] = pair_sum(sum_h);
-    both[1] = pair_sum(sum_n);
-    if (!BWD) {
+    return pair_sum(sum);
+  };
+  float ry = 1.f;
+  const bool ahead = S > 2;  // two rows may be waited for
+  for (long long row = first; row < a.rows; row += step) {
+    const unsigned char* const in = ring + s * stage_bytes;
+    const int after = s + 1 == S ? 0 : s + 1;
+    if constexpr (!BWD) {
+      copies_wait(S - 1);
+      if (a.post_norm) ry = inverse_rms(sums.one(square_of_y(in), slot), inv_d, a.eps);
+      uint64_t sum_h = 0;
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        float x[F], w[F], sc[F];
+        get_y(in, u);
+        my.template get<TR>(in + at_x, u, x);
+        get_gate(in, u);
+        weights(k_post, w_post, u, w);
+        weights(k_s, w_s, u, sc);
+        const uint64_t ry2 = f2_pack(ry, ry);
+#pragma unroll
+        for (int i = 0; i < F; i += 2) {
+          const uint64_t z = f2_mul(f2_mul(f2_mul(pair(y[u], i), ry2), pair(w, i)), pair(g[u], i));
+          const uint64_t v = f2_fma(pair(sc, i), z, pair(x, i));
+          unpair(v, h[u], i);
+          sum_h = f2_fma(v, v, sum_h);
+        }
+        if (a.h) my.put(static_cast<TR*>(a.h), row, u, h[u]);
+      }
       fetch(row + S * step, s);
       if (a.n) {
-        float ss[1] = {both[0]};
-        sums(ss, slot);
-        const float rh = inverse_rms(ss[0], inv_d, a.eps);
+        const float rh = inverse_rms(sums.one(pair_sum(sum_h), slot), inv_d, a.eps);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
           float w[F];
@@ -682,27 +703,66 @@ __global__ void __launch_bounds__(RING, 1) block_norm_ring_kernel(const BlockNor
         }
       }
     } else {
-      float rh = 0.f, along = 0.f, py[1];
-      uint64_t sum_p = 0;
-      if (a.dn) {
-        sums(both, slot);
-        rh = inverse_rms(both[0], inv_d, a.eps);
-        along = both[1] * rh * inv_d;  // mean(w_pre dn n^)
+      // One meeting of a row's threads: c = s z (so h = x + c), and sum p y^ = sum H c is taken apart,
+      //   sum H c = sum dh c + r_h (sum w_pre dn c - mean(w_pre dn n^) r_h sum h c),
+      // whose terms are no larger than those of H itself; the square of the next row's y is summed up with them.  (With a
+      // meeting for each sum that depends on another, three a row: 1005 us for 65536 x 4096 in bf16.)
+      if (a.post_norm && (row == first || !ahead)) {
+        copies_wait(S - 1);
+        ry = inverse_rms(sums.one(square_of_y(in), slot), inv_d, a.eps);
       }
+      copies_wait(ahead ? S - 2 : S - 1);
+      uint64_t sum[5] = {0, 0, 0, 0, 0};  // h h, w_pre dn h, dh c, w_pre dn c, h c: two at a time
+      const uint64_t ry2 = f2_pack(ry, ry);
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        float w[F], sc[F], dh[F];
-        if (!KEEP) {
-          get_y(u);
-          get_gate(u);
-          my.template get<T>(in + at_dn, u, dn[u]);
-        }
+        float x[F], w[F], sc[F], wp[F], dn[F], dh[F];
+        get_y(in, u);
+        my.template get<TR>(in + at_x, u, x);
+        get_gate(in, u);
+        my.template get<T>(in + at_dn, u, dn);
         my.template get<TR>(in + at_dh, u, dh);
-        weights(k_pre, w_pre, u, w);
-        const uint64_t rh2 = f2_pack(rh, rh), along2 = f2_pack(-along, -along), ry2 = f2_pack(ry, ry);
+        weights(k_post, w_post, u, w);
+        weights(k_s, w_s, u, sc);
+        weights(k_pre, w_pre, u, wp);
 #pragma unroll
         for (int i = 0; i < F; i += 2) {
-          const uint64_t nh = f2_mul(pair(h[u], i), rh2), n = pair(dn[u], i);
+          const uint64_t c = f2_mul(pair(sc, i), f2_mul(f2_mul(f2_mul(pair(y[u], i), ry2), pair(w, i)), pair(g[u], i)));
+          const uint64_t v = f2_add(c, pair(x, i)), n = f2_mul(pair(dn, i), pair(wp, i));
+          unpair(v, h[u], i);
+          sum[0] = f2_fma(v, v, sum[0]);
+          sum[1] = f2_fma(n, v, sum[1]);
+          sum[2] = f2_fma(pair(dh, i), c, sum[2]);
+          sum[3] = f2_fma(n, c, sum[3]);
+          sum[4] = f2_fma(v, c, sum[4]);
+        }
+      }
+      float all[8];
+#pragma unroll
+      for (int i = 0; i < 5; ++i) all[i] = pair_sum(sum[i]);
+      all[5] = a.post_norm && ahead ? square_of_y(ring + after * stage_bytes) : 0.f;  // (behind the last row: whatever, not used)
+      all[6] = all[7] = 0.f;
+      sums.several(all, slot);
+      float rh = 0.f, along = 0.f;
+      if (a.dn) {
+        rh = inverse_rms(all[0], inv_d, a.eps);
+        along = all[1] * rh * inv_d;  // mean(w_pre dn n^)
+      }
+      const float py = fmaf(rh, all[3] - along * rh * all[4], all[2]), along_y = a.post_norm ? py * inv_d * ry : 0.f;
+      const uint64_t rh2 = f2_pack(rh, rh), along2 = f2_pack(-along, -along), along_y2 = f2_pack(-along_y, -along_y);
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        float w[F], sc[F], dn[F], dh[F], dy[F];
+        if (!KEEP) {
+          get_y(in, u);
+          get_gate(in, u);
+        }
+        my.template get<T>(in + at_dn, u, dn);
+        my.template get<TR>(in + at_dh, u, dh);
+        weights(k_pre, w_pre, u, w);
+#pragma unroll
+        for (int i = 0; i < F; i += 2) {
+          const uint64_t nh = f2_mul(pair(h[u], i), rh2), n = pair(dn, i);
           unpair(f2_fma(rh2, f2_fma(nh, along2, f2_mul(n, pair(w, i))), pair(dh, i)), dh, i);  // H
           unpair(f2_fma(n, nh, pair(g_pre[u], i)), g_pre[u], i);
         }
@@ -716,26 +776,15 @@ __global__ void __launch_bounds__(RING, 1) block_norm_ring_kernel(const BlockNor
           unpair(f2_fma(Hg, yw, pair(g_s[u], i)), g_s[u], i);
           unpair(f2_fma(Hsg, yh, pair(g_post[u], i)), g_post[u], i);
           if (a.u) unpair(f2_mul(f2_mul(f2_mul(H, pair(sc, i)), yw), pair(slope[u], i)), slope[u], i);  // du
-          unpair(p, h[u], i);
-          sum_p = f2_fma(p, yh, sum_p);
+          unpair(f2_mul(ry2, f2_fma(pair(y[u], i), along_y2, p)), dy, i);
         }
         if (a.u) my.put(static_cast<T*>(a.du), row, u, slope[u]);
+        my.put(static_cast<T*>(a.dy), row, u, dy);
       }
-      if (KEEP) fetch(row + S * step, s);
-      py[0] = pair_sum(sum_p);
-      if (a.post_norm) sums(py, slot);
-      const float along_y = a.post_norm ? py[0] * inv_d * ry : 0.f;
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        if (!KEEP) get_y(u);
-        const uint64_t ry2 = f2_pack(ry, ry), along2 = f2_pack(-along_y, -along_y);
-#pragma unroll
-        for (int i = 0; i < F; i += 2) unpair(f2_mul(ry2, f2_fma(pair(y[u], i), along2, pair(h[u], i))), h[u], i);
-        my.put(static_cast<T*>(a.dy), row, u, h[u]);
-      }
-      if (!KEEP) fetch(row + S * step, s);
+      fetch(row + S * step, s);
+      ry = a.post_norm ? inverse_rms(all[5], inv_d, a.eps) : 1.f;
     }
-    if (++s == S) s = 0;
+    s = after;
   }
   if (!BWD) return;
   // the thread block's part: its rows' threads add up in order
@@ -819,7 +868,8 @@ cudaError_t run_ring(const BlockNormArgs& a, cudaStream_t stream) {
   constexpr int ROWS = RING / LANES, BT = Row::template bytes<T>(), BR = Row::template bytes<TR>();
   const int stage = BT + BR + (a.u ? BT : 0) + (BWD ? BT + BR : 0), weights = Row::template kept<BWD>() ? 0 : 3 * ((a.D + 19) / 4 * 4) * 4;
   const int most = 227 * 1024 - 512;
-  const int stages = 3 * stage + weights <= most ? 3 : 2 * stage + weights <= most ? 2 : 1;
+  int stages = STAGES;
+  while (stages > 1 && stages * stage + weights > most) --stages;
   int smem = stages * stage + weights;
   if (BWD && smem < ROWS * 3 * a.D * 4) smem = ROWS * 3 * a.D * 4;
   if (smem > most) return cudaErrorNotSupported;
