@@ -841,7 +841,7 @@ cudaError_t run(const BlockNormArgs& a, bool backward, cudaStream_t stream) {
   cudaError_t err;
   if (backward) {
     const int smem = LANES >= 512 ? 3 * a.D * 4 : 0;
-    err = cudaFuncSetAttribute(block_norm_bwd_kernel<T, TR, LANES, NV, VEC>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    err = smem ? cudaFuncSetAttribute(block_norm_bwd_kernel<T, TR, LANES, NV, VEC>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) : cudaSuccess;
     if (err != cudaSuccess) return err;
     err = launch_early(block_norm_bwd_kernel<T, TR, LANES, NV, VEC>, dim3((unsigned)(groups < a.nparts ? groups : a.nparts)), dim3(BLOCK), smem, stream, 1, a);
   } else {

@@ -202,8 +202,9 @@ __device__ __forceinline__ bool later_block(unsigned ahead, unsigned& x, unsigne
   return y < gridDim.y;
 }
 
-// One warp looks, the others stand at the block's barrier: sixteen that look take the instruction slots of the thread block beside them
-// (half of the prepare kernel's instructions were such looks).  Then each sees the completed phase for itself.
+// One warp looks, the others stand at the block's barrier: sixteen that look take issue slots of the thread block beside them (half
+// of the prepare kernel's instructions were such looks; its time did not change, since the slots were not what it waited for).  Then each
+// sees the completed phase for itself.
 #define X_WAIT(bar, par, code)                                                \
   do {                                                                        \
     bool ok_ = true;                                                          \
@@ -293,9 +294,10 @@ __device__ __forceinline__ uint32_t mnmaj(const void* p, uint32_t panel = 16384)
 // step from 16 to 64 took 11000 clocks with two thread blocks to an SM.)  Powers of the triangle would need no order of rows, but grow far beyond the inverse where keys are
 // alike.
 //
-// What it costs is the latency of its dependent steps, of which nine wait for a product, and the instructions between them: with
-// 256 threads to a block and all loops unrolled it was 100 KB of instructions, each executed once and fetched for it, and took 68 us
-// a chunk and SM; with decays as products of factors and most loops left as loops 18; with 512 threads see the table of measurements.
+// What it costs is the latency of its dependent steps, of which nine wait for a product, and the instructions between them, most of
+// which are executed once and fetched for it.  2048 chunks, D = 128, us: decays made by every kernel for itself and all of them
+// exponentials, 256 threads, 525; factors made once, 255; with 512 threads 228, of which the tensor cores work for a fifth
+// and an instruction is issued in two clocks of five; 217 since U and X move without their zeros (0.6 GB in 0.2 ms: HBM is not it).
 enum { XP_LOAD = 0, XP_V, XP_MMA, XP_DRAIN, XP_BARS };
 template <int D>
 struct alignas(1024) XPrepSmem {
@@ -836,12 +838,11 @@ x_chain_kernel(const __grid_constant__ XChainArgs a) {
       }
       float next[V], next_all = 0.f;
       if (owner && i + 1 < a.nchunk) fetch(i + 1, next, next_all);
+      if (tid == 0) tma_store_wait_read();  // (the barrier of X_WAIT lets the next operand be written)
+      __syncwarp();
       X_WAIT(sm.bars[XC_MMA], par, 61);
       par ^= 1;
-      if (tid == 0) {
-        if (i + XC_STAGES < a.nchunk) load_m(i + XC_STAGES);
-        tma_store_wait_read();  // (before the barrier that lets the next operand be written: D = 64 the one below, else the next turn's)
-      }
+      if (tid == 0 && i + XC_STAGES < a.nchunk) load_m(i + XC_STAGES);
       __syncwarp();
       uint32_t d0[V], d1[V];
       if (V == 16) {
