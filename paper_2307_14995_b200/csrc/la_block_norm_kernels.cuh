@@ -529,42 +529,38 @@ __device__ __forceinline__ float pair_sum(uint64_t v) {
   return a + b;
 }
 
-// 1 / (1 + exp(-u)), exp and the reciprocal good to an ulp or two (relative 2^-22); where exp is infinite it is 0.
-__device__ __forceinline__ float sigmoid(float u) {
-  float r;
-  asm("{\n\t.reg .f32 e;\n\tmul.f32 e, %1, 0fBFB8AA3B;\n\tex2.approx.f32 e, e;\n\tadd.f32 e, e, 0f3F800000;\n\trcp.approx.f32 %0, e;\n\t}" : "=f"(r) : "f"(u));
-  return r;
+// 1 / (1 + exp(-u)) of two values, exp and the reciprocal good to an ulp or two (relative 2^-22); where exp is infinite it is 0.
+__device__ __forceinline__ uint64_t sigmoid2(uint64_t u) {
+  float a, b;
+  f2_unpack(f2_mul(u, f2_pack(-1.44269504f, -1.44269504f)), a, b);
+  asm("ex2.approx.f32 %0, %0;" : "+f"(a));
+  asm("ex2.approx.f32 %0, %0;" : "+f"(b));
+  f2_unpack(f2_add(f2_pack(a, b), f2_pack(1.f, 1.f)), a, b);
+  asm("rcp.approx.f32 %0, %0;" : "+f"(a));
+  asm("rcp.approx.f32 %0, %0;" : "+f"(b));
+  return f2_pack(a, b);
 }
 // g becomes act(g), slope act'(g); one branch for all of a unit's features
-template <int F>
-__device__ __forceinline__ void gate_values(int kind, float (&g)[F]) {
-  if (kind == GATE_PLAIN) return;
-  if (kind == GATE_SIGMOID) {
-#pragma unroll
-    for (int i = 0; i < F; ++i) g[i] = sigmoid(g[i]);
-  } else {
-#pragma unroll
-    for (int i = 0; i < F; ++i) g[i] *= sigmoid(g[i]);
-  }
-}
-template <int F>
+template <bool SLOPE, int F>
 __device__ __forceinline__ void gate_values(int kind, float (&g)[F], float (&slope)[F]) {
+  const uint64_t one = f2_pack(1.f, 1.f), minus = f2_pack(-1.f, -1.f);
   if (kind == GATE_SILU) {
 #pragma unroll
-    for (int i = 0; i < F; ++i) {
-      const float s = sigmoid(g[i]);
-      g[i] *= s;
-      slope[i] = fmaf(g[i], 1.f - s, s);
+    for (int i = 0; i < F; i += 2) {
+      const uint64_t s = sigmoid2(pair(g, i)), v = f2_mul(pair(g, i), s);
+      unpair(v, g, i);
+      if (SLOPE) unpair(f2_fma(v, f2_fma(s, minus, one), s), slope, i);
     }
-  } else {
+  } else if (kind == GATE_SIGMOID) {
 #pragma unroll
-    for (int i = 0; i < F; ++i) {
-      slope[i] = 1.f;
-      if (kind == GATE_SIGMOID) {
-        g[i] = sigmoid(g[i]);
-        slope[i] = g[i] * (1.f - g[i]);
-      }
+    for (int i = 0; i < F; i += 2) {
+      const uint64_t s = sigmoid2(pair(g, i));
+      unpair(s, g, i);
+      if (SLOPE) unpair(f2_mul(s, f2_fma(s, minus, one)), slope, i);
     }
+  } else if (SLOPE) {
+#pragma unroll
+    for (int i = 0; i < F; ++i) slope[i] = 1.f;
   }
 }
 
@@ -645,8 +641,7 @@ __global__ void __launch_bounds__(RING, 1) block_norm_ring_kernel(const BlockNor
   auto get_gate = [&](const unsigned char* in, int u) {
     if (a.u) {
       my.template get<T>(in + at_u, u, g[u]);
-      if (BWD) gate_values(a.gate, g[u], slope[u]);
-      else gate_values(a.gate, g[u]);
+      gate_values<BWD>(a.gate, g[u], slope[u]);
     } else {
 #pragma unroll
       for (int i = 0; i < F; ++i) g[u][i] = 1.f, slope[u][i] = 0.f;
