@@ -4,11 +4,15 @@
 //   H = dh + r_h (w_pre dn - n^ mean(w_pre dn n^)),  n^ = h r_h;     dx = H,   ds = sum H z,   dw_pre = sum dn n^,
 //   du = s H y^ w_post act'(u),  y^ = y r_y;     p = s H act(u) w_post,   dw_post = sum s H act(u) y^,   dy = r_y (p - y^ mean(p y^)).
 //
-// HBM bounds both: every input is read once and every output written once, a row stays in registers from the one to the other.  LANES
-// threads share a row (a warp up to 512 features, else a part of a thread block or all of it), each with NV groups of eight
-// features, 16 bytes of bf16 at a time; rows whose width is no multiple of eight are not aligned and take the same features one by
-// one.  The sums over tokens (ds, dw) stay in registers over the rows that a thread block takes, leave it as one part [3][D] in the
-// workspace, and a second kernel adds the parts up in order: no atomics, the same bits every time.
+// HBM bounds both: every input is read once and every output written once.  LANES threads share a row (a warp up to 512 features,
+// else a part of a thread block or all of it), each with NV groups of eight features.  Two forms: the kernels right below, a row's loads
+// when its turn comes, and a ring of rows on their way (further down, "many rows").  The sums over tokens (ds, dw) stay on chip over the rows
+// that a thread block takes, leave it as one part [3][D] in the workspace, and a second kernel adds the parts up in order: no
+// atomics, the same bits every time.
+//
+// Forward, the ring takes rows from 4 MB of residual stream on, us without / with it (bf16, gate): 4096 features 148 rows 4.5 / 5.3, 296
+// 5.7 / 5.4, 2400 30.5 / 22.6; 1024 features 296 rows 3.0 / 4.7, 2400 8.8 / 9.2, 4800 16.1 / 14.3.  Backward always, where it fits into
+// shared memory (up to 8192 features; fp32 with a gate up to 5600): 4096 features one row 16 / 10, 296 rows 39 / 15, 4800 rows 343 / 83.
 #pragma once
 #include "la_block_norm.cuh"
 
@@ -174,175 +178,130 @@ __global__ void __launch_bounds__(LANES > THREADS ? LANES : THREADS) block_norm_
   }
 }
 
-// From 512 threads to a row on, its values and the sums over tokens do not fit in the registers together: the sums are in shared memory
-// [3][D], and what a row has is read again (from L2) where it is used.
+// For rows that the ring does not take.  A row's values and the sums over tokens do not fit in the registers together: the sums are in
+// shared memory [3][D], and what a row has is read again (from L2) where it is used.  4096 x 16384 in bf16: 824 us, all in registers 1775.
 template <typename T, typename TR, int LANES, int NV, bool VEC>
-__global__ void __launch_bounds__(LANES > THREADS ? LANES : THREADS) block_norm_bwd_kernel(const BlockNormArgs a) {
-  constexpr int ROWS = (LANES > THREADS ? LANES : THREADS) / LANES;
-  constexpr bool WIDE = LANES >= 512;
-  extern __shared__ float wide_sums[];
-  __shared__ RowSum<LANES, ROWS> sum;
+__global__ void __launch_bounds__(LANES) block_norm_bwd_kernel(const BlockNormArgs a) {
+  extern __shared__ float sums[];
+  __shared__ RowSum<LANES, 1> sum;
   grid_dep_wait();
   grid_dep_launch();
-  const int sub = threadIdx.x / LANES;
-  const Cols<LANES, VEC> cols{(int)threadIdx.x % LANES, a.D};
+  const Cols<LANES, VEC> cols{(int)threadIdx.x, a.D};
   const float inv_d = 1.f / (float)a.D;
-  const long long groups = (a.rows + ROWS - 1) / ROWS;
-  constexpr int NG = WIDE ? 1 : NV;
-  float g_post[NG][8], g_s[NG][8], g_pre[NG][8];
+  float zero[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-  for (int v = 0; v < NG; ++v)
+  for (int v = 0; v < NV; ++v)
 #pragma unroll
-    for (int i = 0; i < 8; ++i) g_post[v][i] = g_s[v][i] = g_pre[v][i] = 0.f;
-  if (WIDE) {
-#pragma unroll
-    for (int v = 0; v < NV; ++v)
-#pragma unroll
-      for (int k = 0; k < 3; ++k) cols.store(wide_sums + k * a.D, v, g_post[0]);  // (zeros; everyone's own)
-  }
-  for (long long group = blockIdx.x; group < groups; group += gridDim.x) {
-    const long long row = group * ROWS + sub;
-    const bool mine = row < a.rows;
-    const long long at = mine ? row * a.D : 0;
-    float y[NV][8], h[NV][8], u[NV][8], dn[NV][8];
+    for (int k = 0; k < 3; ++k) cols.store(sums + k * a.D, v, zero);  // (everyone's own)
+  for (long long row = blockIdx.x; row < a.rows; row += gridDim.x) {
+    const long long at = row * a.D;
+    float y[NV][8], h[NV][8], u[8], dn[8];
     auto get_y = [&](int v) { cols.load(static_cast<const T*>(a.y) + at, v, y[v]); };
-    auto get_u = [&](int v) { cols.load(a.u ? static_cast<const T*>(a.u) + at : nullptr, v, u[v]); };
-    auto get_dn = [&](int v) { cols.load(a.dn && mine ? static_cast<const T*>(a.dn) + at : nullptr, v, dn[v]); };
-    float ss = 0.f;
-#pragma unroll
-    for (int v = 0; v < NV; ++v) {
-      get_y(v);
-      if (!WIDE) {
-        cols.load(static_cast<const TR*>(a.x) + at, v, h[v]);
-        get_u(v);
-        get_dn(v);
-      }
-#pragma unroll
-      for (int i = 0; i < 8; ++i) ss = fmaf(y[v][i], y[v][i], ss);
-    }
+    auto get_u = [&](int v) { cols.load(a.u ? static_cast<const T*>(a.u) + at : nullptr, v, u); };
+    auto get_dn = [&](int v) { cols.load(a.dn ? static_cast<const T*>(a.dn) + at : nullptr, v, dn); };
     float ry = 1.f;
-    if (a.post_norm) ry = inverse_rms(sum(ss, 0, sub), inv_d, a.eps);
-    ss = 0.f;
-    float dot = 0.f;
+    if (a.post_norm) {
+      float ss = 0.f;
+#pragma unroll
+      for (int v = 0; v < NV; ++v) {
+        get_y(v);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) ss = fmaf(y[v][i], y[v][i], ss);
+      }
+      ry = inverse_rms(sum(ss, 0, 0), inv_d, a.eps);
+    }
+    float ss = 0.f, dot = 0.f;
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
       float w[8], s[8], wp[8];
-      if (WIDE) {
-        get_y(v);
-        cols.load(static_cast<const TR*>(a.x) + at, v, h[v]);
-        get_u(v);
-        get_dn(v);
-      }
+      get_y(v);
+      cols.load(static_cast<const TR*>(a.x) + at, v, h[v]);
+      get_u(v);
+      get_dn(v);
       cols.load(a.w_post, v, w, 1.f);
       cols.load(a.s, v, s, 1.f);
       cols.load(a.w_pre, v, wp, 1.f);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         float z = y[v][i] * ry * w[i], slope;
-        if (a.u) z *= act(a.gate, u[v][i], slope);
+        if (a.u) z *= act(a.gate, u[i], slope);
         h[v][i] = fmaf(s[i], z, h[v][i]);
         ss = fmaf(h[v][i], h[v][i], ss);
-        dot = fmaf(dn[v][i] * wp[i], h[v][i], dot);
+        dot = fmaf(dn[i] * wp[i], h[v][i], dot);
       }
     }
     float rh = 0.f, along = 0.f;
     if (a.dn) {
-      rh = inverse_rms(sum(ss, 1, sub), inv_d, a.eps);
-      along = sum(dot, 0, sub) * rh * inv_d;  // mean(w_pre dn n^)
+      rh = inverse_rms(sum(ss, 1, 0), inv_d, a.eps);
+      along = sum(dot, 0, 0) * rh * inv_d;  // mean(w_pre dn n^)
     }
     float py = 0.f;
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-      float w[8], s[8], wp[8], dh[8], du[8], sum_post[8], sum_s[8], sum_pre[8];
-      if (WIDE) {
-        get_y(v);
-        get_u(v);
-        get_dn(v);
-        cols.load(wide_sums, v, sum_post);
-        cols.load(wide_sums + a.D, v, sum_s);
-        cols.load(wide_sums + 2 * a.D, v, sum_pre);
-      }
-      float* const to_post = WIDE ? sum_post : g_post[v % NG];
-      float* const to_s = WIDE ? sum_s : g_s[v % NG];
-      float* const to_pre = WIDE ? sum_pre : g_pre[v % NG];
+      float w[8], s[8], wp[8], dh[8], du[8], to_post[8], to_s[8], to_pre[8];
+      get_y(v);
+      get_u(v);
+      get_dn(v);
+      cols.load(sums, v, to_post);
+      cols.load(sums + a.D, v, to_s);
+      cols.load(sums + 2 * a.D, v, to_pre);
       cols.load(a.w_post, v, w, 1.f);
       cols.load(a.s, v, s, 1.f);
       cols.load(a.w_pre, v, wp, 1.f);
-      cols.load(a.dh && mine ? static_cast<const TR*>(a.dh) + at : nullptr, v, dh);
+      cols.load(a.dh ? static_cast<const TR*>(a.dh) + at : nullptr, v, dh);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const float nh = h[v][i] * rh, yh = y[v][i] * ry;
         float H = dh[i];
         if (a.dn) {
-          H = fmaf(rh, dn[v][i] * wp[i] - nh * along, H);
-          to_pre[i] = fmaf(dn[v][i], nh, to_pre[i]);
+          H = fmaf(rh, dn[i] * wp[i] - nh * along, H);
+          to_pre[i] = fmaf(dn[i], nh, to_pre[i]);
         }
         dh[i] = H;
         float gate = 1.f, slope = 0.f;
-        if (a.u) gate = act(a.gate, u[v][i], slope);
-        if (mine) {
-          to_s[i] = fmaf(H, yh * w[i] * gate, to_s[i]);
-          to_post[i] = fmaf(H * s[i], yh * gate, to_post[i]);
-        }
+        if (a.u) gate = act(a.gate, u[i], slope);
+        to_s[i] = fmaf(H, yh * w[i] * gate, to_s[i]);
+        to_post[i] = fmaf(H * s[i], yh * gate, to_post[i]);
         du[i] = H * s[i] * yh * w[i] * slope;
         h[v][i] = H * s[i] * gate * w[i];  // p
         py = fmaf(h[v][i], yh, py);
       }
-      if (WIDE) {
-        cols.store(wide_sums, v, sum_post);
-        cols.store(wide_sums + a.D, v, sum_s);
-        cols.store(wide_sums + 2 * a.D, v, sum_pre);
-      }
-      if (mine) cols.store(static_cast<TR*>(a.dx) + at, v, dh);
-      if (mine && a.u) cols.store(static_cast<T*>(a.du) + at, v, du);
+      cols.store(sums, v, to_post);
+      cols.store(sums + a.D, v, to_s);
+      cols.store(sums + 2 * a.D, v, to_pre);
+      cols.store(static_cast<TR*>(a.dx) + at, v, dh);
+      if (a.u) cols.store(static_cast<T*>(a.du) + at, v, du);
     }
-    if (a.post_norm) py = sum(py, 1, sub) * inv_d;
+    if (a.post_norm) py = sum(py, 1, 0) * inv_d;
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
       if (a.post_norm) {
-        if (WIDE) get_y(v);
+        get_y(v);
 #pragma unroll
         for (int i = 0; i < 8; ++i) h[v][i] = ry * (h[v][i] - y[v][i] * ry * py);
       }
-      if (mine) cols.store(static_cast<T*>(a.dy) + at, v, h[v]);
+      cols.store(static_cast<T*>(a.dy) + at, v, h[v]);
     }
     __syncthreads();  // (the row's sums have two slots and are used twice)
   }
-  // the thread block's part; where it has several rows at a time, their threads add up in order
+  // the thread block's part
   float* const part = a.parts + (size_t)blockIdx.x * 3 * a.D;
-  if (WIDE) {
 #pragma unroll
-    for (int v = 0; v < NV; ++v)
+  for (int v = 0; v < NV; ++v)
 #pragma unroll
-      for (int k = 0; k < 3; ++k) {
-        cols.load(wide_sums + k * a.D, v, g_post[0]);
-        cols.store(part + k * a.D, v, g_post[0]);
-      }
-    return;
-  }
-  for (int r = 0; r < ROWS; ++r) {
-    if (sub == r) {
-#pragma unroll
-      for (int v = 0; v < NV; ++v)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const int c = VEC ? (v * LANES + cols.lane) * 8 + i : (8 * v + i) * LANES + cols.lane;
-          if (c >= a.D) continue;
-          part[c] = g_post[v % NG][i] + (r > 0 ? part[c] : 0.f);
-          part[a.D + c] = g_s[v % NG][i] + (r > 0 ? part[a.D + c] : 0.f);
-          part[2 * a.D + c] = g_pre[v % NG][i] + (r > 0 ? part[2 * a.D + c] : 0.f);
-        }
+    for (int k = 0; k < 3; ++k) {
+      cols.load(sums + k * a.D, v, zero);
+      cols.store(part + k * a.D, v, zero);
     }
-    __syncthreads();
-  }
 }
 
 // ---- many rows -----------------------------------------------------------------------------------------------------------------------------
 // The same with the rows of a thread block's next turns on their way while it works on one: every thread copies what it will read
 // itself into a ring of S stages in shared memory (cp.async), so that nobody waits for anybody but in the row sums.  One thread block
-// of 512 threads to an SM, 512 / LANES rows at a time, each row's threads with a barrier of their own; weights in shared memory,
-// sums over tokens in registers to the end.  65536 x 4096 in bf16, forward and backward, us: the kernels above 740 and 4282, this one 430 and
-// 1024 (409 and 654 at the copy bandwidth).
+// of 512 threads to an SM, 512 / LANES rows at a time, each row's threads with a barrier of their own; sums over tokens in registers to
+// the end.  Forward and backward, us (at the copy bandwidth): 65536 x 4096 in bf16 431 and 932 (409 and 654), without the ring 739 and 4146;
+// 16384 x 4096 in fp32 212 and 337 (204 and 327); 16384 x 2048 in bf16 with the residual stream in fp32 85 and 133 (72 and 112).  What
+// is left backward is the meeting of a row's threads, with one row of 4096 features at a time; instructions are issued in 61 % of the clocks.
 //
 // Rows whose width is no multiple of eight move in pairs of features, 4 bytes of bf16: where the width is odd a row begins in the middle
 // of a pair, every second one, and a group of threads takes rows of one kind only, so that a thread's features are the same in all.
@@ -372,7 +331,7 @@ __device__ __forceinline__ void copies_wait(int n) {  // all but the last n stag
 
 // One tensor's place in a stage, and this thread's features of a row: unit u has features (u LANES + lane) F - shift .. + F - 1.  F is
 // eight where all tensors are bf16 and four where one is fp32, 16 bytes of the wider type: neighbours' pieces touch, so that every
-// sector is asked for once.  (With eight of fp32, two pieces of a thread side by side: SIDEBYSIDE.)
+// sector is asked for once.  (With eight of fp32, two pieces of a thread side by side, 16384 x 4096 took 361 and 627.)
 template <int LANES, int NV, int FEATURES>
 struct RingRow {
   static constexpr int F = FEATURES, U = 8 * NV / F;
@@ -829,24 +788,26 @@ __global__ void __launch_bounds__(THREADS) block_norm_sum_kernel(const float* pa
 cudaError_t sum_parts(const BlockNormArgs& a, int n, cudaStream_t stream);
 
 template <typename T, typename TR, int LANES, int NV, bool VEC>
-cudaError_t run(const BlockNormArgs& a, bool backward, cudaStream_t stream) {
+cudaError_t run_fwd(const BlockNormArgs& a, cudaStream_t stream) {
   constexpr int BLOCK = LANES > THREADS ? LANES : THREADS, ROWS = BLOCK / LANES;
-  const long long groups = (a.rows + ROWS - 1) / ROWS;
+  const long long groups = (a.rows + ROWS - 1) / ROWS, cap = 148LL * 64;  // a few waves, then each thread block takes further rows
   KernelTimer timer(K_GATE, stream);
-  cudaError_t err;
-  if (backward) {
-    const int smem = LANES >= 512 ? 3 * a.D * 4 : 0;
-    err = smem ? cudaFuncSetAttribute(block_norm_bwd_kernel<T, TR, LANES, NV, VEC>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) : cudaSuccess;
-    if (err != cudaSuccess) return err;
-    err = launch_early(block_norm_bwd_kernel<T, TR, LANES, NV, VEC>, dim3((unsigned)(groups < a.nparts ? groups : a.nparts)), dim3(BLOCK), smem, stream, 1, a);
-  } else {
-    const long long cap = 148LL * 64;  // a few waves, then each thread block takes further rows
-    err = launch_early(block_norm_fwd_kernel<T, TR, LANES, NV, VEC>, dim3((unsigned)(groups < cap ? groups : cap)), dim3(BLOCK), 0, stream, 1, a);
-  }
+  const cudaError_t err = launch_early(block_norm_fwd_kernel<T, TR, LANES, NV, VEC>, dim3((unsigned)(groups < cap ? groups : cap)), dim3(BLOCK), 0, stream, 1, a);
   count_launch();
-  if (err == cudaSuccess) err = cudaGetLastError();
-  if (err != cudaSuccess || !backward) return err;
-  return sum_parts(a, (int)(groups < a.nparts ? groups : a.nparts), stream);
+  return err != cudaSuccess ? err : cudaGetLastError();
+}
+template <typename T, typename TR, int LANES, int NV, bool VEC>
+cudaError_t run_bwd(const BlockNormArgs& a, cudaStream_t stream) {
+  const int smem = 3 * a.D * 4, grid = (int)(a.rows < a.nparts ? a.rows : a.nparts);
+  cudaError_t err = cudaFuncSetAttribute(block_norm_bwd_kernel<T, TR, LANES, NV, VEC>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  if (err != cudaSuccess) return err;
+  {
+    KernelTimer timer(K_GATE, stream);
+    err = launch_early(block_norm_bwd_kernel<T, TR, LANES, NV, VEC>, dim3((unsigned)grid), dim3(LANES), smem, stream, 1, a);
+    count_launch();
+    if (err == cudaSuccess) err = cudaGetLastError();
+  }
+  return err != cudaSuccess ? err : sum_parts(a, grid, stream);
 }
 
 cudaError_t sum_parts(const BlockNormArgs& a, int n, cudaStream_t stream) {
@@ -862,7 +823,7 @@ cudaError_t run_ring(const BlockNormArgs& a, cudaStream_t stream) {
   using Row = RingRow<LANES, NV, !VEC ? 2 : sizeof(TR) == 4 ? 4 : 8>;
   constexpr int ROWS = RING / LANES, BT = Row::template bytes<T>(), BR = Row::template bytes<TR>();
   const int stage = BT + BR + (a.u ? BT : 0) + (BWD ? BT + BR : 0), weights = Row::template kept<BWD>() ? 0 : 3 * ((a.D + 19) / 4 * 4) * 4;
-  const int most = 227 * 1024 - 512;
+  constexpr int most = 227 * 1024 - (int)sizeof(RowSums<LANES>);
   int stages = STAGES;
   while (stages > 1 && stages * stage + weights > most) --stages;
   int smem = stages * stage + weights;
@@ -896,19 +857,23 @@ cudaError_t ring_by_width(const BlockNormArgs& a, cudaStream_t stream) {
 
 template <typename T, typename TR, bool VEC>
 cudaError_t by_width(const BlockNormArgs& a, bool backward, cudaStream_t stream) {
-  // few rows end before a ring is full; wide ones in fp32 do not fit in it
-  if (a.D <= 8192 && a.rows >= 296) {
-    const cudaError_t err = backward ? ring_by_width<T, TR, VEC, true>(a, stream) : ring_by_width<T, TR, VEC, false>(a, stream);
+  if (a.D > BLOCK_NORM_MAX_D) return cudaErrorInvalidValue;
+  if (backward) {
+    const cudaError_t err = a.D <= 8192 ? ring_by_width<T, TR, VEC, true>(a, stream) : cudaErrorNotSupported;
+    if (err != cudaErrorNotSupported) return err;
+    return a.D <= 8192 ? run_bwd<T, TR, 512, 2, VEC>(a, stream) : run_bwd<T, TR, 1024, 2, VEC>(a, stream);
+  }
+  if (a.D <= 8192 && a.rows * a.D * (long long)sizeof(TR) >= 4 << 20) {
+    const cudaError_t err = ring_by_width<T, TR, VEC, false>(a, stream);
     if (err != cudaErrorNotSupported) return err;
   }
-  if (a.D <= 256) return run<T, TR, 32, 1, VEC>(a, backward, stream);
-  if (a.D <= 512) return run<T, TR, 32, 2, VEC>(a, backward, stream);
-  if (a.D <= 1024) return run<T, TR, 128, 1, VEC>(a, backward, stream);
-  if (a.D <= 2048) return run<T, TR, 128, 2, VEC>(a, backward, stream);
-  if (a.D <= 4096) return run<T, TR, 256, 2, VEC>(a, backward, stream);
-  if (a.D <= 8192) return run<T, TR, 512, 2, VEC>(a, backward, stream);
-  if (a.D <= BLOCK_NORM_MAX_D) return run<T, TR, 1024, 2, VEC>(a, backward, stream);
-  return cudaErrorInvalidValue;
+  if (a.D <= 256) return run_fwd<T, TR, 32, 1, VEC>(a, stream);
+  if (a.D <= 512) return run_fwd<T, TR, 32, 2, VEC>(a, stream);
+  if (a.D <= 1024) return run_fwd<T, TR, 128, 1, VEC>(a, stream);
+  if (a.D <= 2048) return run_fwd<T, TR, 128, 2, VEC>(a, stream);
+  if (a.D <= 4096) return run_fwd<T, TR, 256, 2, VEC>(a, stream);
+  if (a.D <= 8192) return run_fwd<T, TR, 512, 2, VEC>(a, stream);
+  return run_fwd<T, TR, 1024, 2, VEC>(a, stream);
 }
 template <typename T, typename TR>
 cudaError_t by_alignment(const BlockNormArgs& a, bool backward, cudaStream_t stream) {

@@ -108,6 +108,28 @@ def test_numbers_of_rows(rows, D):
     Case(rows, D, BF16, F32, la.LA_GATE_SIGMOID, seed=rows).check()
 
 
+@pytest.mark.parametrize("dtype,res", [(BF16, BF16), (BF16, F32), (F32, F32)])
+@pytest.mark.parametrize("D", [2049, 4099, 8191, 8201, 16383])
+def test_wide_rows_of_no_round_width(D, dtype, res):
+    Case(5, D, dtype, res, la.LA_GATE_SILU, seed=D).check()
+
+
+@pytest.mark.parametrize("dtype,res", [(BF16, BF16), (BF16, F32), (F32, F32)])
+@pytest.mark.parametrize("D", [200, 301, 512, 1000, 1537, 2048, 2999, 4096, 5600, 8192])
+def test_many_rows_of_each_width(D, dtype, res):
+    """Enough of them (5 MB of residual stream) that every thread block takes several, an odd number."""
+    rows = 5 * 2 ** 20 // (D * (2 if res is BF16 else 4)) | 1
+    Case(rows, D, dtype, res, la.LA_GATE_SILU, seed=D).check()
+
+
+@pytest.mark.parametrize("dtype,res", [(BF16, BF16), (F32, F32)])
+@pytest.mark.parametrize("D", [96, 2048])
+def test_many_rows_in_other_forms(D, dtype, res):
+    rows = 6 * 2 ** 20 // (D * (2 if res is BF16 else 4))
+    for gate, weights, post_norm, dh, dn in ((None, True, True, True, False), (la.LA_GATE_PLAIN, False, True, False, True), (la.LA_GATE_SIGMOID, True, False, True, True)):
+        Case(rows, D, dtype, res, gate, weights, post_norm=post_norm, seed=4).check(dh, dn)
+
+
 @pytest.mark.parametrize("gate", GATES)
 @pytest.mark.parametrize("weights", [True, False])
 @pytest.mark.parametrize("post_norm", [True, False])
