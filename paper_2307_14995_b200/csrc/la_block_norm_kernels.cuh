@@ -12,7 +12,7 @@
 //
 // Forward, the ring takes rows from 4 MB of residual stream on, us without / with it (bf16, gate): 4096 features 148 rows 4.5 / 5.3, 296
 // 5.7 / 5.4, 2400 30.5 / 22.6; 1024 features 296 rows 3.0 / 4.7, 2400 8.8 / 9.2, 4800 16.1 / 14.3.  Backward always, where it fits into
-// shared memory (up to 8192 features; fp32 with a gate up to 5600): 4096 features one row 16 / 10, 296 rows 39 / 15, 4800 rows 343 / 83.
+// shared memory (up to 8192 features; fp32 with a gate up to 5590): 4096 features one row 16 / 10, 296 rows 39 / 15, 4800 rows 343 / 83.
 #pragma once
 #include "la_block_norm.cuh"
 

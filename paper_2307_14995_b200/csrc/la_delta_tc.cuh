@@ -735,7 +735,9 @@ x_prepare_kernel(const __grid_constant__ XMaps maps, const __grid_constant__ Del
 // per thread block, the state in registers in fp32; the state that enters each chunk (REV: the gradient of the one that leaves it) goes
 // to the workspace as an image.  A step is one product, a conversion and two barriers; the images of M come three steps ahead.
 // Both terms of the state are columns of one B operand, [hi | lo], so that hi of M meets both in one pass: with NE = 32 an
-// instruction takes as long as its A operand comes from shared memory (4 KB, 32 clocks), whatever its columns.
+// instruction takes as long as its A operand comes from shared memory, whatever its columns.  Of a step's 2540 clocks the products take
+// 1600: M passes through shared memory twice, 64 KB in and 64 KB out to the tensor cores; half the columns for M's lo terms, state images
+// stored from registers instead of by a bulk copy or one warp alone looking for the products' end change nothing.  2048 chunks in 32 heads: 122 us.
 // D = 64: both terms of M are rows of one A operand; the rows of lo pass through shared memory to the threads of those of hi.
 constexpr int XC_STAGES = 3;
 enum { XC_LOAD0 = 0, XC_MMA = XC_STAGES, XC_DRAIN, XC_BARS };
@@ -882,7 +884,8 @@ x_chain_kernel(const __grid_constant__ XChainArgs a) {
 // ---- output ----------------------------------------------------------------------------------------------------------------------------
 // O = scale diag(e^G) Q S + X (V - diag(e^G) K S): 64 value columns of a chunk per thread block, two thread blocks to an SM.  Both terms of
 // the state, and then of the bracket, are one B operand of 128 columns [hi | lo]; the halves of the results are added up on the way
-// out of tensor memory.
+// out of tensor memory.  Bound by its three dependent groups of products; the loads of the thread block 296 places on come to L2 meanwhile.
+// 2048 chunks: 103 us, 0.5 GB (43 % of HBM's rate).
 enum { XO_LOAD = 0, XO_X, XO_MMA, XO_DRAIN, XO_BARS };
 template <int D>
 struct alignas(1024) XOutSmem {
@@ -1045,6 +1048,7 @@ x_output_kernel(const __grid_constant__ XMaps maps, const __grid_constant__ Delt
 // ---- adjoint ---------------------------------------------------------------------------------------------------------------------------
 // Z = X^T dO, and B = scale Q^T diag(e^G) dO - K^T diag(e^G) Z for the chain in reverse: 64 value columns of a chunk per thread block.
 // D = 64: [Q | K] are the rows of one A operand and [dO' | Z'] the columns of one B operand, of whose product two quarters are wanted.
+// 2048 chunks: 130 us, 0.5 GB; fetching ahead to L2, as the kernels around it do, made this one slower (and the prepare kernel).
 enum { XA_LOAD = 0, XA_QK, XA_MMA, XA_DRAIN, XA_BARS };
 template <int D>
 struct alignas(1024) XAdjSmem {
@@ -1169,7 +1173,8 @@ x_adjoint_kernel(const __grid_constant__ XMaps maps, const __grid_constant__ Del
 }
 
 // ---- values ----------------------------------------------------------------------------------------------------------------------------
-// Y = That (V - diag(e^G) K S) (even thread blocks) and dR = Z + U diag(beta e^(G_end - G)) K E' (odd ones), as images; dR is dV.
+// Y = That (V - diag(e^G) K S) (even thread blocks) and dR = Z + U diag(beta e^(G_end - G)) K E' (odd ones), as images; dR is dV.  Side
+// by side, the two read the same K and U.  Two dependent products behind loads of 160 KB: 2048 chunks 205 us, 1 GB (45 % of HBM's rate).
 enum { XV_LOAD = 0, XV_U, XV_MMA, XV_DRAIN, XV_BARS };
 template <int D>
 struct alignas(1024) XValSmem {
@@ -1299,7 +1304,8 @@ x_values_kernel(const __grid_constant__ XMaps maps, const __grid_constant__ Delt
 // 224 KB of operands come first, E' takes the place of S, q and k that of E', F and -H those of Y and dR, so that there is one thread
 // block to an SM.  The order is what keeps its threads within 128 registers: with the scores first F and -H (64 registers) waited for
 // the rest to be made, and what was spilled for them went to L2, since there is no L1 beside 227 KB of shared memory (480 us for 2048
-// chunks).
+// chunks; 308 now).  The tensor cores work for a quarter of it; the rest are the scores' exponentials and sums between the products, with
+// no second thread block to fill them.
 enum { XG_LOAD = 0, XG_E, XG_QK, XG_MMA, XG_DRAIN, XG_BARS };
 template <int D>
 struct alignas(1024) XGradSmem {
@@ -1735,7 +1741,8 @@ cudaError_t x_launch(K kern, int kind, dim3 grid, int threads, cudaStream_t stre
   return err != cudaSuccess ? err : cudaGetLastError();
 }
 
-// Thread blocks with 32 value columns each as long as they all run at once (one to an SM), else with 64.
+// Thread blocks with 32 value columns each as long as they all run at once (one to an SM), else with 64: 32 heads of 128 features, 64
+// chunks each, 125 us with 32 columns and 173 with 64.
 template <int D, bool REV>
 cudaError_t x_chain(const DeltaArgs& d, cudaStream_t stream) {
   using Rec = XRec<D>;

@@ -196,6 +196,37 @@ def test_same_bits_from_graphs_and_streams():
     assert all(torch.equal(a, b) for a, b in zip(grads, c.grads))
 
 
+def test_offsets_past_32_bits():
+    past_32_bits()
+    torch.cuda.empty_cache()
+
+
+def past_32_bits():
+    """More than 2^31 values to a tensor: the last rows have what they have alone."""
+    D, last = 4096, 6
+    rows = 2 ** 31 // D + 7
+    c = Case(last, D, BF16, BF16, la.LA_GATE_SILU)
+    shape = la.make_block_norm_shape(rows, D, BF16, BF16, **c.more)
+
+    def whole(x):
+        big = torch.zeros(rows, D, dtype=BF16, device=DEV)
+        big[-last:] = x.to(DEV)
+        return big
+
+    x, y, u, dh, dn = (whole(t) for t in (c.x, c.y, c.u, c.dh, c.dn))
+    w = [t.to(DEV) for t in c.w]
+    h, n, dx, dy, du = (torch.empty_like(x) for _ in range(5))
+    dw = [torch.empty(D, device=DEV) for _ in range(3)]
+    la.la_block_norm_fwd(shape, x, y, u, *w, h, n)
+    la.la_block_norm_bwd(shape, x, y, u, *w, dh, dn, dx, dy, du, *dw, la.alloc_block_norm_workspace(shape, DEV))
+    ref = orc.block_norm_fwd(c.x, c.y, c.u, *c.w, **c.more) + orc.block_norm_bwd(c.x, c.y, c.u, *c.w, c.dh, c.dn, **c.more)
+    terms = (None, None) + c.terms(True, True, ref[2])
+    for name, got, want, more in zip(("h", "n", "dx", "dy", "du"), (h, n, dx, dy, du), ref, terms):
+        near(got[-last:], want, name, more)
+    for name, got, want in zip(("dw_post", "ds", "dw_pre"), dw, ref[5:]):  # (the rows before are zeros)
+        near(got, want, name, np.sqrt(last))
+
+
 def test_gradient_against_differences():
     """Central differences of the forward pass along a random direction: the rest of third order is 1e-6 of the loss's scale at this
     step, the forward pass's roundings (1e-6 of a value, random signs) are divided by it."""

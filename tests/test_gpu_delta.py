@@ -336,6 +336,40 @@ def test_layer_between_two_norms(dtype):
     near(n2.view(B, N, D), second[1].reshape(B, N, D), 1e-5, "n2")
 
 
+@pytest.mark.parametrize("path", [la.LA_PATH_AUTO, la.LA_PATH_SIMT])
+def test_offsets_past_32_bits(path):
+    past_32_bits(path)
+    torch.cuda.empty_cache()
+
+
+def past_32_bits(path):
+    """More than 2^31 values and 2^32 bytes to a tensor, ten times that to a workspace.  The last head's last tokens stand alone behind a token that
+    forgets everything, so that they have a reference of their own."""
+    H, N, d, last = 64, 262800 + 200, 128, 200
+    gen = torch.Generator(DEV)
+    gen.manual_seed(8)
+    q, k = (torch.nn.functional.normalize(torch.randn(1, 1, N, d, generator=gen, device=DEV), dim=-1).to(BF16) for _ in range(2))
+    v, do = (torch.empty(1, H, N, d, dtype=BF16, device=DEV).normal_(generator=gen) for _ in range(2))
+    g, beta = (torch.rand(1, H, N, generator=gen, device=DEV) for _ in range(2))
+    g *= -0.1
+    g[:, :, N - last] = -np.inf
+    shape = la.make_delta_shape(1, H, N, d, d, BF16, BF16, Hk=1, scale=0.25, path=path)
+    o, dv = torch.empty_like(v), torch.empty_like(v)
+    dq, dk, dg, dbeta = torch.empty_like(q), torch.empty_like(k), torch.empty_like(g), torch.empty_like(g)
+    ws_f = la.alloc_delta_workspace(la.LA_OP_FWD, shape, DEV)
+    la.la_delta_fwd(shape, q, k, v, g, beta, o, workspace=ws_f)
+    ws_b = torch.empty(la.delta_workspace_bytes(la.LA_OP_BWD, shape) - ws_f.numel(), dtype=torch.uint8, device=DEV)
+    la.la_delta_bwd(shape, q, k, v, g, beta, do, dq, dk, dv, dg, dbeta, workspace=ws_b, fwd_workspace=ws_f)
+    torch.cuda.synchronize()
+    la.device_status()
+    tail = lambda x: x[:, -1:, N - last:].cpu()
+    data = [tail(x) for x in (q, k, v, g, beta, do)]
+    data[3][:, :, 0] = 0.0  # (on a state of zeros it makes no difference)
+    ref = reference(data)
+    for name, got in (("o", o), ("dv", dv), ("dg", dg), ("dbeta", dbeta)):
+        near(tail(got), ref[name], tol(path, BF16), name)
+
+
 @pytest.mark.parametrize("dtype,path", KINDS)
 def test_streams_and_graphs(dtype, path):
     """The same bits on a stream of the caller's and from a captured graph that is replayed on new inputs, two graphs on one workspace
