@@ -406,6 +406,34 @@ def test_streams_and_graphs(dtype, path):
 
 
 @pytest.mark.parametrize("dtype,path", KINDS)
+def test_two_calls_at_once(dtype, path):
+    """On two streams, each with its workspaces and beside an ordinary attention call on a third: the bits that each has alone."""
+    calls = [Call(draw(2, 8, 4, 900, 128, 60 + i, dtype), path=path) for i in range(2)]
+    wants = []
+    for call in calls:
+        call.fwd()
+        call.bwd()
+        call.done()
+        wants.append({n: x.clone() for n, x in call.results().items()})
+    q, k, v = (torch.randn(2, 8, 900, 128, device=DEV).to(BF16) for _ in range(3))
+    lam = np.full(8, 0.97, np.float32)
+    o = la.fwd(q, k, v, lam)
+    o = (o[0] if isinstance(o, tuple) else o).clone()
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for call, stream in zip(calls, streams):
+            call.fwd(stream=stream)
+            call.bwd(stream=stream)
+        with torch.cuda.stream(streams[2]):
+            again = la.fwd(q, k, v, lam)
+    for call, want in zip(calls, wants):
+        call.done()
+        assert all(torch.equal(want[n], x) for n, x in call.results().items())
+    assert torch.equal(again[0] if isinstance(again, tuple) else again, o)
+
+
+@pytest.mark.parametrize("dtype,path", KINDS)
 def test_a_bad_row_stays_where_it_belongs(dtype, path):
     """NaN and infinity in one sequence's and one head's tokens reach no other, and tokens before them stay as they are."""
     data = list(draw(2, 4, 2, 300, 128, 51, dtype))
