@@ -303,16 +303,21 @@ __global__ void __launch_bounds__(LANES) block_norm_bwd_kernel(const BlockNormAr
 // 16384 x 4096 in fp32 212 and 337 (204 and 327); 16384 x 2048 in bf16 with the residual stream in fp32 85 and 133 (72 and 112).  What
 // is left backward is the meeting of a row's threads, with one row of 4096 features at a time; instructions are issued in 61 % of the clocks.
 //
-// Rows whose width is no multiple of eight move in pairs of features, 4 bytes of bf16: where the width is odd a row begins in the middle
-// of a pair, every second one, and a group of threads takes rows of one kind only, so that a thread's features are the same in all.
+// Rows whose width is no multiple of eight begin anywhere in 16 bytes.  They move from the 16-byte boundary before them, and what a unit
+// has of the rows beside is left out; all rows of a thread block begin at the same place (the grid is a multiple of eight, and a block
+// takes rows that are a grid apart), so that a thread's features are the same in all.  us, and with pairs of features (4 bytes of bf16) that
+// need an even beginning alone: 16384 x 1003 in fp32 70 and 117 (91 and 159), in bf16 62 and 112 (73 and 123); 16384 x 5001 in bf16 339 and 809 (490
+// and 1367).  A row's first and last units, whose values go one by one, are what aligned rows do not have (16384 x 1000: 34 and 63).
 constexpr int RING = 512;
 template <int BYTES>
 __device__ __forceinline__ void copy(uint32_t to, const void* from) {
   if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
   else asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(to), "l"(from) : "memory");
 }
-__device__ __forceinline__ void copy4(uint32_t to, const void* from, int bytes) {  // the rest of the four are zeros
-  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to), "l"(from), "r"(bytes) : "memory");
+template <int BYTES>
+__device__ __forceinline__ void copy_part(uint32_t to, const void* from, int bytes) {  // the rest are zeros
+  if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(bytes) : "memory");
+  else asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(to), "l"(from), "r"(bytes) : "memory");
 }
 template <int N>
 __device__ __forceinline__ void copies_wait() {
@@ -331,67 +336,53 @@ __device__ __forceinline__ void copies_wait(int n) {  // all but the last n stag
 
 // One tensor's place in a stage, and this thread's features of a row: unit u has features (u LANES + lane) F - shift .. + F - 1.  F is
 // eight where all tensors are bf16 and four where one is fp32, 16 bytes of the wider type: neighbours' pieces touch, so that every
-// sector is asked for once.  (With eight of fp32, two pieces of a thread side by side, 16384 x 4096 took 361 and 627.)
-template <int LANES, int NV, int FEATURES>
+// sector is asked for once.  Four too for gradients of unaligned rows in bf16, whose ends are shorter then (with eight 117 and 900 for the 112
+// and 809 above; forward, 16384 x 2999, eight take 175 and four 194).  (With eight of fp32, two pieces of a thread side by side, 16384 x 4096 took 361 and 627.)
+template <int LANES, int NV, int FEATURES, bool ALIGNED>
 struct RingRow {
   static constexpr int F = FEATURES, U = 8 * NV / F;
-  static constexpr bool VEC = F > 2;
   template <bool BWD>
   static constexpr bool kept() { return NV == 1 && (!BWD || F == 8); }  // the weights' place
   int lane, D, shift;
   long long total;  // features of the tensor
   __device__ __forceinline__ int feature(int u) const { return (u * LANES + lane) * F - shift; }
+  __device__ __forceinline__ bool whole(int f) const { return ALIGNED ? f < D : f >= 0 && f + F <= D; }
   template <typename T>
   static constexpr int bytes() { return RING * 8 * NV * (int)sizeof(T); }
-  // stage memory: unit u of thread t in pieces of 16, 8 or 4 bytes at piece (k U + u) RING + t, k the piece of the unit
+  // stage memory: unit u of thread t at piece u RING + t
   template <typename T>
   __device__ __forceinline__ void fetch(uint32_t to, const T* base, long long row) const {
-    constexpr int PIECE = F == 4 ? 4 * (int)sizeof(T) : VEC ? 16 : 4, K = F * (int)sizeof(T) / PIECE, PER = F / K;  // pieces of a unit, features of a piece
-    const T* const at = base + row * D;
+    constexpr int PIECE = F * (int)sizeof(T);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int f = feature(u);
-#pragma unroll
-      for (int k = 0; k < K; ++k) {
-        const uint32_t dst = to + (uint32_t)((k * U + u) * RING + threadIdx.x) * PIECE;
-        const int g = f + k * PER;
-        if (VEC) {
-          if (g < D) copy<PIECE>(dst, at + g);
-        } else if (sizeof(T) == 4) {
-          if (g >= 0 && g < D) copy4(dst, at + g, 4);
-        } else if (g + 1 >= 0 && g < D) {
-          copy4(dst, at + g, row * D + g + 2 <= total ? 4 : 2);
-        }
+      const uint32_t dst = to + (uint32_t)(u * RING + threadIdx.x) * PIECE;
+      const T* const at = base + row * D + f;
+      if (f < D) {
+        const long long left = total - (row * D + f);  // (only the tensor's last piece is cut short)
+        if (ALIGNED || left >= F) copy<PIECE>(dst, at);
+        else copy_part<PIECE>(dst, at, (int)left * (int)sizeof(T));
       }
     }
   }
   template <typename T>
   __device__ __forceinline__ void get(const unsigned char* from, int u, float (&x)[F]) const {
-    constexpr int PIECE = F == 4 ? 4 * (int)sizeof(T) : VEC ? 16 : 4, K = F * (int)sizeof(T) / PIECE;
+    const unsigned char* const src = from + (u * RING + threadIdx.x) * F * (int)sizeof(T);
+    if constexpr (sizeof(T) == 4) {
+      const float4 v = *reinterpret_cast<const float4*>(src);
+      x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w;
+    } else {
+      uint32_t w[F / 2];
+      if constexpr (F == 4) *reinterpret_cast<uint2*>(w) = *reinterpret_cast<const uint2*>(src);
+      else *reinterpret_cast<uint4*>(w) = *reinterpret_cast<const uint4*>(src);
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-      const unsigned char* const src = from + ((k * U + u) * RING + threadIdx.x) * PIECE;
-      if constexpr (F == 4 && sizeof(T) == 2) {
-        const uint2 v = *reinterpret_cast<const uint2*>(src);
-        x[0] = __uint_as_float(v.x << 16), x[1] = __uint_as_float(v.x & 0xffff0000u);
-        x[2] = __uint_as_float(v.y << 16), x[3] = __uint_as_float(v.y & 0xffff0000u);
-      } else if constexpr (VEC && sizeof(T) == 2) {
-        const uint4 v = *reinterpret_cast<const uint4*>(src);
-        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+      for (int i = 0; i < F / 2; ++i) x[2 * i] = __uint_as_float(w[i] << 16), x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    }
+    if (!ALIGNED) {
+      const int f = feature(u);
+      if (!whole(f)) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) x[2 * i] = __uint_as_float(w[i] << 16), x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-      } else if constexpr (VEC) {
-        const float4 v = *reinterpret_cast<const float4*>(src);
-        x[4 * k] = v.x; x[4 * k + 1] = v.y; x[4 * k + 2] = v.z; x[4 * k + 3] = v.w;
-      } else if constexpr (sizeof(T) == 2) {
-        const uint32_t w = *reinterpret_cast<const uint32_t*>(src);
-        const int f = feature(u);
-        x[0] = f >= 0 && f < D ? __uint_as_float(w << 16) : 0.f;
-        x[1] = f + 1 < D ? __uint_as_float(w & 0xffff0000u) : 0.f;
-      } else {
-        const float w = *reinterpret_cast<const float*>(src);
-        const int f = feature(u) + k;
-        x[k] = f >= 0 && f < D ? w : 0.f;
+        for (int i = 0; i < F; ++i) x[i] = f + i >= 0 && f + i < D ? x[i] : 0.f;
       }
     }
   }
@@ -399,33 +390,26 @@ struct RingRow {
   __device__ __forceinline__ void put(T* base, long long row, int u, const float (&x)[F]) const {
     T* const at = base + row * D;
     const int f = feature(u);
-    if constexpr (F == 4) {
-      if (f < D) Vec4<T>::store(at + f, x);
-    } else if constexpr (VEC) {
-      if (f < D) store8(at + f, x);
-    } else if (f >= 0 && f + 1 < D) {  // (the pair begins at an even element of the tensor)
-      if constexpr (sizeof(T) == 2) *reinterpret_cast<__nv_bfloat162*>(at + f) = __floats2bfloat162_rn(x[0], x[1]);
-      else *reinterpret_cast<float2*>(at + f) = make_float2(x[0], x[1]);
-    } else {
-      if (f >= 0 && f < D) at[f] = from_f32<T>(x[0]);
-      if (f + 1 < D) at[f + 1] = from_f32<T>(x[1]);
+    if (whole(f)) {
+      if constexpr (F == 4) Vec4<T>::store(at + f, x);
+      else store8(at + f, x);
+    } else if (!ALIGNED) {
+#pragma unroll
+      for (int i = 0; i < F; ++i)
+        if (f + i >= 0 && f + i < D) at[f + i] = from_f32<T>(x[i]);
     }
   }
-  // [D] in shared memory, with a margin; units of eight: the first four of every eight features, then the others, so that neighbours read without
-  // conflicts (weight_at: where feature f is)
-  static __device__ __forceinline__ int weight_at(int f, int D) { return F == 8 ? (f & 4 ? D / 2 : 0) + (f >> 3) * 4 + (f & 3) : f; }
+  // Weights in shared memory begin where the units do, `length` of them; units of eight: the first four of every eight, then the
+  // others, so that neighbours read without conflicts (weight_at: where position p is).
+  static __host__ __device__ __forceinline__ int length(int D) { return (D + (ALIGNED ? 7 : 14)) / 8 * 8; }
+  static __device__ __forceinline__ int weight_at(int p, int D) { return F == 8 ? (p & 4 ? length(D) / 2 : 0) + (p >> 3) * 4 + (p & 3) : p; }
   __device__ __forceinline__ void weights(const float* w, int u, float (&x)[F]) const {
-    const int f = feature(u);
-    if constexpr (F == 4) {
-      const float4 a = *reinterpret_cast<const float4*>(w + (f < D ? f : 0));
-      x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
-    } else if constexpr (VEC) {
-      const int at = f < D ? f / 2 : 0;
-      const float4 a = *reinterpret_cast<const float4*>(w + at), b = *reinterpret_cast<const float4*>(w + D / 2 + at);
-      x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
-    } else {
-      x[0] = w[f >= 0 && f < D ? f : 0];
-      x[1] = w[f + 1 < D ? f + 1 : 0];
+    const int p = feature(u) < D ? (u * LANES + lane) * F : 0;
+    const float4 a = *reinterpret_cast<const float4*>(w + (F == 8 ? p / 2 : p));
+    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
+    if constexpr (F == 8) {
+      const float4 b = *reinterpret_cast<const float4*>(w + length(D) / 2 + p / 2);
+      x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
     }
   }
 };
@@ -525,7 +509,7 @@ __device__ __forceinline__ void gate_values(int kind, float (&g)[F], float (&slo
 
 template <typename T, typename TR, int LANES, int NV, bool VEC, bool BWD>
 __global__ void __launch_bounds__(RING, 1) block_norm_ring_kernel(const BlockNormArgs a, const int S) {
-  using Row = RingRow<LANES, NV, !VEC ? 2 : sizeof(TR) == 4 ? 4 : 8>;
+  using Row = RingRow<LANES, NV, sizeof(TR) == 4 || (BWD && !VEC) ? 4 : 8, VEC>;  // (see RingRow)
   constexpr int F = Row::F, U = Row::U, ROWS = RING / LANES;
   constexpr int BT = Row::template bytes<T>(), BR = Row::template bytes<TR>();
   extern __shared__ __align__(16) unsigned char ring[];
@@ -536,13 +520,13 @@ __global__ void __launch_bounds__(RING, 1) block_norm_ring_kernel(const BlockNor
   const int stage_bytes = BT + BR + (a.u ? BT : 0) + (BWD ? BT + BR : 0);
   const int at_x = BT, at_u = BT + BR, at_dn = at_u + (a.u ? BT : 0), at_dh = at_dn + BT;
   float* const w_post = reinterpret_cast<float*>(ring + S * stage_bytes);
-  const int wd = (a.D + 19) / 4 * 4;
+  const int wd = Row::length(a.D);
   float *const w_s = w_post + wd, *const w_pre = w_s + wd;
   for (int i = threadIdx.x; i < S * stage_bytes / 16; i += RING) reinterpret_cast<uint4*>(ring)[i] = make_uint4(0u, 0u, 0u, 0u);  // units past the end stay zeros
   __syncthreads();
   const int sub = threadIdx.x / LANES;
-  const long long first = (long long)blockIdx.x * ROWS + sub, step = (long long)gridDim.x * ROWS;
-  const Row my{(int)threadIdx.x % LANES, a.D, VEC ? 0 : (int)((first * a.D) & 1), a.rows * a.D};
+  const long long first = VEC ? (long long)blockIdx.x * ROWS + sub : (long long)gridDim.x * sub + blockIdx.x, step = (long long)gridDim.x * ROWS;
+  const Row my{(int)threadIdx.x % LANES, a.D, VEC ? 0 : (int)(blockIdx.x * (unsigned)a.D % F), a.rows * a.D};
   const float inv_d = 1.f / (float)a.D;
   const uint32_t ring_at = static_cast<uint32_t>(__cvta_generic_to_shared(ring));
   auto fetch = [&](long long row, int s) {
@@ -578,11 +562,12 @@ __global__ void __launch_bounds__(RING, 1) block_norm_ring_kernel(const BlockNor
         k_pre[u][i] = in && a.w_pre ? a.w_pre[f] : 1.f;
       }
   } else {
-    for (int i = threadIdx.x; i < a.D; i += RING) {
-      const int at = Row::weight_at(i, a.D);
-      w_post[at] = a.w_post ? a.w_post[i] : 1.f;
-      w_s[at] = a.s ? a.s[i] : 1.f;
-      w_pre[at] = a.w_pre ? a.w_pre[i] : 1.f;
+    for (int p = threadIdx.x; p < wd; p += RING) {
+      const int at = Row::weight_at(p, a.D), i = p - my.shift;
+      const bool in = i >= 0 && i < a.D;
+      w_post[at] = in && a.w_post ? a.w_post[i] : 1.f;
+      w_s[at] = in && a.s ? a.s[i] : 1.f;
+      w_pre[at] = in && a.w_pre ? a.w_pre[i] : 1.f;
     }
     __syncthreads();
   }
@@ -820,9 +805,9 @@ cudaError_t sum_parts(const BlockNormArgs& a, int n, cudaStream_t stream) {
 
 template <typename T, typename TR, int LANES, int NV, bool VEC, bool BWD>
 cudaError_t run_ring(const BlockNormArgs& a, cudaStream_t stream) {
-  using Row = RingRow<LANES, NV, !VEC ? 2 : sizeof(TR) == 4 ? 4 : 8>;
+  using Row = RingRow<LANES, NV, sizeof(TR) == 4 || (BWD && !VEC) ? 4 : 8, VEC>;
   constexpr int ROWS = RING / LANES, BT = Row::template bytes<T>(), BR = Row::template bytes<TR>();
-  const int stage = BT + BR + (a.u ? BT : 0) + (BWD ? BT + BR : 0), weights = Row::template kept<BWD>() ? 0 : 3 * ((a.D + 19) / 4 * 4) * 4;
+  const int stage = BT + BR + (a.u ? BT : 0) + (BWD ? BT + BR : 0), weights = Row::template kept<BWD>() ? 0 : 3 * Row::length(a.D) * 4;
   constexpr int most = 227 * 1024 - (int)sizeof(RowSums<LANES>);
   int stages = STAGES;
   while (stages > 1 && stages * stage + weights > most) --stages;
@@ -833,7 +818,8 @@ cudaError_t run_ring(const BlockNormArgs& a, cudaStream_t stream) {
   cudaError_t err = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (err != cudaSuccess) return err;
   long long grid = (a.rows + ROWS - 1) / ROWS;
-  grid = grid < 148 ? (grid + 1) / 2 * 2 : 148;  // even: see RingRow::shift
+  if (!VEC) grid = grid < 144 ? (grid + 7) / 8 * 8 : 144;  // a multiple of eight: see above
+  else if (grid > 148) grid = 148;
   if (BWD && grid > a.nparts) return cudaErrorInvalidValue;
   {
     KernelTimer timer(K_GATE, stream);
@@ -847,11 +833,13 @@ cudaError_t run_ring(const BlockNormArgs& a, cudaStream_t stream) {
 // Backward eight features to a thread as far as 512 threads go: with sixteen its sums over tokens leave too few registers.
 template <typename T, typename TR, bool VEC, bool BWD>
 cudaError_t ring_by_width(const BlockNormArgs& a, cudaStream_t stream) {
-  if (a.D <= 256) return run_ring<T, TR, 32, 1, VEC, BWD>(a, stream);
-  if (a.D <= 512) return run_ring<T, TR, BWD ? 64 : 32, BWD ? 1 : 2, VEC, BWD>(a, stream);
-  if (a.D <= 1024) return run_ring<T, TR, 128, 1, VEC, BWD>(a, stream);
-  if (a.D <= 2048) return run_ring<T, TR, BWD ? 256 : 128, BWD ? 1 : 2, VEC, BWD>(a, stream);
-  if (a.D <= 4096) return run_ring<T, TR, BWD ? 512 : 256, BWD ? 1 : 2, VEC, BWD>(a, stream);
+  const int d = a.D + (VEC ? 0 : 7);  // that many may have to fit
+  if (d <= 256) return run_ring<T, TR, 32, 1, VEC, BWD>(a, stream);
+  if (d <= 512) return run_ring<T, TR, BWD ? 64 : 32, BWD ? 1 : 2, VEC, BWD>(a, stream);
+  if (d <= 1024) return run_ring<T, TR, 128, 1, VEC, BWD>(a, stream);
+  if (d <= 2048) return run_ring<T, TR, BWD ? 256 : 128, BWD ? 1 : 2, VEC, BWD>(a, stream);
+  if (d <= 4096) return run_ring<T, TR, BWD ? 512 : 256, BWD ? 1 : 2, VEC, BWD>(a, stream);
+  if (d > 8192) return cudaErrorNotSupported;
   return run_ring<T, TR, 512, 2, VEC, BWD>(a, stream);
 }
 

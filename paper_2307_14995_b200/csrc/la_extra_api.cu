@@ -74,10 +74,11 @@ la_status check_norm(const la_block_norm_shape* s) {
   if (s->dtype == LA_F32 && s->res_dtype != LA_F32) return LA_ERR_UNSUPPORTED;
   return LA_OK;
 }
-// Thread blocks of the backward pass, each of which leaves a part of the sums over tokens: as many as run at once, an even number.
+// Thread blocks of the backward pass, each of which leaves a part of the sums over tokens: as many as run at once; of few, a multiple of eight.
 int norm_parts(const la_block_norm_shape* s) {
   const long long most = s->D > 4096 && s->D <= 8192 ? 148 * 2 : 148;
-  return (int)(s->rows < most ? (s->rows + 1) / 2 * 2 : most);
+  const long long rows = (s->rows + 7) / 8 * 8;
+  return (int)(rows < most ? rows : most);
 }
 BlockNormArgs norm_args(const la_block_norm_shape* s, const void* x, const void* y, const void* u, const float* w_post, const float* sc,
                         const float* w_pre) {
