@@ -11,7 +11,9 @@
 // atomics, the same bits every time.
 //
 // Forward, the ring takes rows from 4 MB of residual stream on, us without / with it (bf16, gate): 4096 features 148 rows 4.5 / 5.3, 296
-// 5.7 / 5.4, 2400 30.5 / 22.6; 1024 features 296 rows 3.0 / 4.7, 2400 8.8 / 9.2, 4800 16.1 / 14.3.  Backward always, where it fits into
+// 5.7 / 5.4, 2400 30.5 / 22.6; 1024 features 296 rows 3.0 / 4.7, 2400 8.8 / 9.2, 4800 16.1 / 14.3.  Rows that are not aligned it takes in any
+// number, since the other form loads them value by value: 1003 features one row 4.6 / 4.9, 296 4.9 / 5.8, 301 features 3001 rows 12.3 / 8.7, 5001
+// features one row 7.9 / 6.1, 296 15.8 / 12.3.  Backward always, where it fits into
 // shared memory (up to 8192 features; fp32 with a gate up to 5590): 4096 features one row 16 / 10, 296 rows 39 / 15, 4800 rows 343 / 83.
 #pragma once
 #include "la_block_norm.cuh"
@@ -851,15 +853,17 @@ cudaError_t by_width(const BlockNormArgs& a, bool backward, cudaStream_t stream)
     if (err != cudaErrorNotSupported) return err;
     return a.D <= 8192 ? run_bwd<T, TR, 512, 2, VEC>(a, stream) : run_bwd<T, TR, 1024, 2, VEC>(a, stream);
   }
-  if (a.D <= 8192 && a.rows * a.D * (long long)sizeof(TR) >= 4 << 20) {
+  if (a.D <= 8192 && (!VEC || a.rows * a.D * (long long)sizeof(TR) >= 4 << 20)) {
     const cudaError_t err = ring_by_width<T, TR, VEC, false>(a, stream);
     if (err != cudaErrorNotSupported) return err;
   }
-  if (a.D <= 256) return run_fwd<T, TR, 32, 1, VEC>(a, stream);
-  if (a.D <= 512) return run_fwd<T, TR, 32, 2, VEC>(a, stream);
-  if (a.D <= 1024) return run_fwd<T, TR, 128, 1, VEC>(a, stream);
-  if (a.D <= 2048) return run_fwd<T, TR, 128, 2, VEC>(a, stream);
-  if (a.D <= 4096) return run_fwd<T, TR, 256, 2, VEC>(a, stream);
+  if constexpr (VEC) {
+    if (a.D <= 256) return run_fwd<T, TR, 32, 1, VEC>(a, stream);
+    if (a.D <= 512) return run_fwd<T, TR, 32, 2, VEC>(a, stream);
+    if (a.D <= 1024) return run_fwd<T, TR, 128, 1, VEC>(a, stream);
+    if (a.D <= 2048) return run_fwd<T, TR, 128, 2, VEC>(a, stream);
+    if (a.D <= 4096) return run_fwd<T, TR, 256, 2, VEC>(a, stream);
+  }
   if (a.D <= 8192) return run_fwd<T, TR, 512, 2, VEC>(a, stream);
   return run_fwd<T, TR, 1024, 2, VEC>(a, stream);
 }
