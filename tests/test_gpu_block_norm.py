@@ -265,3 +265,44 @@ def test_wrong_tensors_are_refused():
     with pytest.raises(TypeError):
         la.la_block_norm_fwd(la.make_shape(1, 2, 64, 64, 64, BF16, F32), x, y, u, *w, h, n)
     assert la.launch_count() == launched
+
+
+@pytest.mark.parametrize("dtype,res", [(BF16, BF16), (BF16, F32), (F32, F32)])
+@pytest.mark.parametrize("D", [8190, 8201, 12288])
+def test_wide_rows_in_turn(D, dtype, res):
+    """More rows than thread blocks (9472) where the ring does not go, so that one takes several: the bits of calls in which each has one
+    row, with one sum to a row (no post norm, or h alone) and with two."""
+    rows, part = 2 * 9472 + 5, 9472
+    gen = torch.Generator(DEV)
+    gen.manual_seed(D)
+    new = lambda dt: torch.empty(rows, D, dtype=dt, device=DEV).normal_(generator=gen)
+    x, y, w = new(res), new(dtype), [0.5 + torch.rand(D, generator=gen, device=DEV) for _ in range(3)]
+    y *= torch.rand(rows, 1, generator=gen, device=DEV).to(dtype)  # (rows of different sizes)
+    for post_norm, want_h, want_n in ((False, True, True), (False, False, True), (True, True, False), (True, True, True)):
+        def run(a, b):
+            shape = la.make_block_norm_shape(b - a, D, dtype, res, eps=1e-6, post_norm=post_norm)
+            h = torch.empty(b - a, D, dtype=res, device=DEV) if want_h else None
+            n = torch.empty(b - a, D, dtype=dtype, device=DEV) if want_n else None
+            la.la_block_norm_fwd(shape, x[a:b], y[a:b], None, *w, h, n)
+            return h, n
+
+        whole = run(0, rows)
+        for a in range(0, rows, part):
+            b = min(rows, a + part)
+            for got, want in zip(whole, run(a, b)):
+                assert got is None or torch.equal(got[a:b], want), (post_norm, want_h, want_n)
+        del whole
+
+
+@pytest.mark.parametrize("post_norm", [True, False])
+@pytest.mark.parametrize("D,dtype,res,rows", [
+    (8190, BF16, BF16, 901), (8190, BF16, F32, 601), (8190, F32, F32, 601), (8201, BF16, BF16, 301), (8201, F32, F32, 449), (12288, BF16, F32, 301),
+    (16384, BF16, BF16, 301), (16384, F32, F32, 301), (5700, F32, F32, 601), (6144, F32, F32, 901), (8192, F32, F32, 601)])
+def test_gradients_of_wide_rows_in_turn(D, dtype, res, rows, post_norm):
+    """Gradients where the ring does not go, with several rows to a thread block: 148 of more than 8192 features, else 296."""
+    Case(rows, D, dtype, res, la.LA_GATE_SILU, post_norm=post_norm, seed=D).check()
+
+
+@pytest.mark.parametrize("dh,dn", [(True, False), (False, True)])
+def test_either_gradient_of_wide_rows_in_turn(dh, dn):
+    Case(301, 8201, BF16, BF16, la.LA_GATE_SIGMOID, seed=5).check(dh, dn)
