@@ -477,32 +477,53 @@ __device__ __forceinline__ float pair_sum(uint64_t v) {
   return a + b;
 }
 
-// 1 / (1 + exp(-u)) of two values, exp and the reciprocal good to an ulp or two (relative 2^-22); where exp is infinite it is 0.
+// 1 / (1 + exp(-u)) of two values.  The exponential and the reciprocal are good to an ulp or two (5.4e-7 of the result with the roundings
+// around them), but the exponent -u log2(e) is a rounded product, whose error is multiplied by |u|: |u| 7.3e-8 of a small result more, 2^-20
+// at u = -20, 2^-18 at u = -80.  Where u is bf16, given to 2^-9 of itself, that stays.  EXACT, where u is fp32: the exponent is t + r, the product
+// rounded down and the rest, r = (what the product lost) - u (log2(e)'s own rest), and 2^(t + r) = 2^t + 2^t r ln 2 (|r| < 2^-15).  Beyond |u| = 104
+// the result is 0 or 1, and r stays finite; the product is rounded down so that r >= 0 where 2^t is infinite and the sum stays so.
+// 65536 x 4096 in bf16, forward and backward: 1461 us, EXACT 1511.
+template <bool EXACT>
 __device__ __forceinline__ uint64_t sigmoid2(uint64_t u) {
+  constexpr float LOG2E = 1.44269502f, REST = 1.92596299e-8f, LN2 = 0.693147181f;
   float a, b;
-  f2_unpack(f2_mul(u, f2_pack(-1.44269504f, -1.44269504f)), a, b);
+  uint64_t t, r = 0;
+  if (EXACT) {
+    f2_unpack(u, a, b);
+    asm("min.NaN.xorsign.abs.f32 %0, %0, %1;" : "+f"(a) : "f"(104.f));  // the sign of u
+    asm("min.NaN.xorsign.abs.f32 %0, %0, %1;" : "+f"(b) : "f"(104.f));
+    u = f2_pack(a, b);
+    t = f2_mul_down(u, f2_pack(-LOG2E, -LOG2E));
+    const uint64_t lost = f2_fma(u, f2_pack(LOG2E, LOG2E), t);                                   // (its negative)
+    r = f2_fma(u, f2_pack(-REST * LN2, -REST * LN2), f2_mul(lost, f2_pack(-LN2, -LN2)));  // times ln 2
+  } else {
+    t = f2_mul(u, f2_pack(-LOG2E, -LOG2E));
+  }
+  f2_unpack(t, a, b);
   asm("ex2.approx.f32 %0, %0;" : "+f"(a));
   asm("ex2.approx.f32 %0, %0;" : "+f"(b));
-  f2_unpack(f2_add(f2_pack(a, b), f2_pack(1.f, 1.f)), a, b);
+  uint64_t e = f2_pack(a, b);
+  if (EXACT) e = f2_fma(e, r, e);
+  f2_unpack(f2_add(e, f2_pack(1.f, 1.f)), a, b);
   asm("rcp.approx.f32 %0, %0;" : "+f"(a));
   asm("rcp.approx.f32 %0, %0;" : "+f"(b));
   return f2_pack(a, b);
 }
 // g becomes act(g), slope act'(g); one branch for all of a unit's features
-template <bool SLOPE, int F>
+template <bool SLOPE, bool EXACT, int F>
 __device__ __forceinline__ void gate_values(int kind, float (&g)[F], float (&slope)[F]) {
   const uint64_t one = f2_pack(1.f, 1.f), minus = f2_pack(-1.f, -1.f);
   if (kind == GATE_SILU) {
 #pragma unroll
     for (int i = 0; i < F; i += 2) {
-      const uint64_t s = sigmoid2(pair(g, i)), v = f2_mul(pair(g, i), s);
+      const uint64_t s = sigmoid2<EXACT>(pair(g, i)), v = f2_mul(pair(g, i), s);
       unpair(v, g, i);
       if (SLOPE) unpair(f2_fma(v, f2_fma(s, minus, one), s), slope, i);
     }
   } else if (kind == GATE_SIGMOID) {
 #pragma unroll
     for (int i = 0; i < F; i += 2) {
-      const uint64_t s = sigmoid2(pair(g, i));
+      const uint64_t s = sigmoid2<EXACT>(pair(g, i));
       unpair(s, g, i);
       if (SLOPE) unpair(f2_mul(s, f2_fma(s, minus, one)), slope, i);
     }
@@ -590,7 +611,7 @@ __global__ void __launch_bounds__(RING, 1) block_norm_ring_kernel(const BlockNor
   auto get_gate = [&](const unsigned char* in, int u) {
     if (a.u) {
       my.template get<T>(in + at_u, u, g[u]);
-      gate_values<BWD>(a.gate, g[u], slope[u]);
+      gate_values<BWD, sizeof(T) == 4>(a.gate, g[u], slope[u]);
     } else {
 #pragma unroll
       for (int i = 0; i < F; ++i) g[u][i] = 1.f, slope[u][i] = 0.f;

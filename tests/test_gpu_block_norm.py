@@ -306,3 +306,42 @@ def test_gradients_of_wide_rows_in_turn(D, dtype, res, rows, post_norm):
 @pytest.mark.parametrize("dh,dn", [(True, False), (False, True)])
 def test_either_gradient_of_wide_rows_in_turn(dh, dn):
     Case(301, 8201, BF16, BF16, la.LA_GATE_SIGMOID, seed=5).check(dh, dn)
+
+
+@pytest.mark.parametrize("gate", [la.LA_GATE_SIGMOID, la.LA_GATE_SILU])
+@pytest.mark.parametrize("D,rows,dtype", [(1024, 9, F32), (1024, 1200, F32), (1003, 9, F32), (8200, 3, F32), (1024, 9, BF16), (1024, 1200, BF16), (8200, 3, BF16)])
+def test_gates_relative_to_their_own_size(D, rows, dtype, gate):
+    """The gate and its derivative alone (x = 0, y = 1, no norm), in the direct forms and the ring's.  The exponential is good to 2^-22, the
+    reciprocal to 2^-23, three roundings to 2^-24 each: 5.4e-7 of a sigmoid, however small; two factors round once more.  The derivatives
+    are sums of two terms where u is small: where they are not (|u| >= 3, negative), those of a sigmoid have two such errors, and those
+    of SiLU, s + u s (1 - s), 2.9 + 1 of them over 1.9.  Below exp(-87) values are subnormal.  With u in bf16 the ring's exponent is a
+    product rounded once, 2^-24 of it, of a constant that is off by 1.34e-8 of itself: |u| 7.3e-8 more, twice that for the derivatives,
+    and those are rounded to bf16."""
+    c = Case(rows, D, dtype, F32, gate, weights=False, post_norm=False)
+    c.x[:], c.y[:], c.dh[:] = 0.0, 1.0, 1.0
+    c.u[:] = torch.linspace(-120.0, 120.0, rows * D).view(rows, D)[:, torch.randperm(D, generator=torch.Generator().manual_seed(2))]
+    c.u[0, :4] = torch.tensor([-np.inf, np.inf, -2.0 ** 127, 2.0 ** 127])
+    u = c.u.double().numpy()
+    bf16 = dtype is BF16
+    more = np.minimum(np.abs(u), 130) * (7.3e-8 if bf16 else 0.0)
+    with np.errstate(over="ignore", invalid="ignore"):
+        want, slope = (f(u) for f in orc.ACT[gate])
+    odd = np.zeros_like(u, dtype=bool)
+    odd[0, :4] = True
+    h = torch.empty(rows, D, device=DEV)
+    la.la_block_norm_fwd(c.shape, *c.inputs(), h, None)
+    got = h.double().cpu().numpy()
+    off = np.abs(got[~odd] - want[~odd]) - ((6.5e-7 + more) * np.abs(want))[~odd] - 2.0 ** -126 * np.maximum(1, np.abs(u[~odd]))
+    assert off.max() <= 0
+    if gate == la.LA_GATE_SIGMOID:
+        assert np.array_equal(got[odd], [0, 1, 0, 1])
+    else:
+        assert np.isnan(got[0, 0]) and got[0, 1] == np.inf and got[0, 2] == 0 and got[0, 3] == 2.0 ** 127
+    c.u[0, :4] = -50.0
+    u[0, :4], more[0, :4] = -50.0, 50 * 7.3e-8 if bf16 else 0.0
+    slope = orc.ACT[gate][1](np.clip(u, -700, 700))
+    du = c.bwd(dn=False)[2].double().cpu().numpy()
+    some = u <= -3
+    off = np.abs(du - slope)[some] - ((2e-6 + 2 * more + (2.0 ** -8 if bf16 else 0.0)) * np.abs(slope))[some] - 2.0 ** -126 * np.maximum(1, np.abs(u[some]))
+    assert off.max() <= 0
+    c.done()
