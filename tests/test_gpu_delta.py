@@ -471,3 +471,93 @@ def test_wrong_tensors_are_refused():
         la.la_delta_bwd(call.shape, *call.inputs, call.do, call.dq, call.dk, call.dv, call.dg, call.dbeta, workspace=call.ws_b,
                         fwd_workspace=call.ws_f[:-256])
     assert la.launch_count() == launched
+
+
+@pytest.mark.parametrize("d,B,H,Hk", [(64, 5, 16, 16), (64, 5, 16, 4), (128, 2, 20, 20), (128, 4, 12, 6)])
+@pytest.mark.parametrize("layout", [HEADS, TOKENS])
+def test_more_heads_than_run_at_once(d, B, H, Hk, layout):
+    """From 75 heads of 64 features and 38 of 128 on, a thread block of the chain has 64 columns of a state: every output, states in and out."""
+    data = draw(B, H, Hk, 300, d, H, rates=np.logspace(-3, 0.5, H).tolist())
+    kv_in, grad = states(B, H, d, 6)
+    call = Call(data, layout=layout, kv_in=kv_in, grad_kv_out=grad)
+    call.fwd()
+    call.bwd()
+    call.done()
+    check(call, reference(data, kv_in=kv_in, grad_kv_out=grad), tol(la.LA_PATH_AUTO, BF16))
+
+
+@pytest.mark.parametrize("dtype,path", KINDS)
+@pytest.mark.parametrize("H,Hk", [(4, 2), (6, 2), (8, 1)])
+def test_shared_heads_of_64_features(H, Hk, dtype, path):
+    data = draw(2, H, Hk, 200, 64, H, dtype)
+    kv_in, grad = states(2, H, 64, 7)
+    call = Call(data, layout=TOKENS, path=path, kv_in=kv_in, grad_kv_out=grad)
+    call.fwd()
+    call.bwd()
+    call.done()
+    check(call, reference(data, kv_in=kv_in, grad_kv_out=grad), tol(path, dtype))
+
+
+@pytest.mark.parametrize("dtype,path", KINDS)
+def test_packed_sequences_gradients_of_gates(dtype, path):
+    """dg of packed sequences: every one as on its own, and nothing at all where everything is forgotten."""
+    lengths = [40, 130, 64, 1, 200]
+    data = list(draw(1, 4, 2, sum(lengths), 128, 62, dtype))
+    first = np.cumsum([0] + lengths)
+    data[3][:, :, first[:-1]] = -np.inf
+    call = Call(data, path=path)
+    call.fwd()
+    call.bwd()
+    call.done()
+    assert not call.dg[:, :, first[:-1]].any()
+    for a, b in zip(first[:-1], first[1:]):
+        if b - a > 1:
+            near(call.dg[:, :, a:b], reference([x[:, :, a:b].contiguous() for x in data])["dg"], tol(path, dtype), "dg")
+
+
+@pytest.mark.parametrize("dtype,path", KINDS)
+@pytest.mark.parametrize("d", [64, 128])
+def test_precision_that_is_stated(d, dtype, path):
+    """The relative 2-norm of the error of fp32 results.  Tensor cores: operands formed on chip are off by 2.7e-6 on the root of the mean
+    square, of which a result passes six forward and twelve backward, 6.6e-6 and 9.4e-6 with random signs, and half as much again for the
+    products of lo terms that are left out.  CUDA cores: a product's sum of 128 terms rounds 128 times, each by 2^-24 / 3^1/2 of a partial sum
+    at most, whose size grows as the root of its terms: 2^-24 (128 / 6)^1/2 = 2.8e-7; six of them 6.7e-7, twelve 9.5e-7."""
+    data = draw(2, 4, 2, 515, d, 14, dtype, rates=[1e-3, 0.03, 0.3, 2.0])
+    kv_in, grad = states(2, 4, d, 8)
+    call = Call(data, kv_in=kv_in, grad_kv_out=grad, path=path)
+    call.fwd()
+    call.bwd()
+    call.done()
+    ref = reference(data, kv_in=kv_in, grad_kv_out=grad)
+    tensor = dtype is BF16 and path == la.LA_PATH_AUTO
+    for name, got in call.results().items():
+        error = np.linalg.norm(got.double().cpu().numpy() - ref[name]) / np.linalg.norm(ref[name])
+        forward = name in ("o", "kv_out")
+        print(name, error)
+        assert error <= ((1e-5 if forward else 1.4e-5) if tensor else (7e-7 if forward else 1e-6)), (name, error)
+
+
+@pytest.mark.parametrize("dtype,path", KINDS)
+@pytest.mark.parametrize("d", [64, 128])
+def test_gradient_along_itself_against_differences(d, dtype, path):
+    """As above, but along the gradient, where the loss changes by as much as it can.  The fp64 oracle's own central differences at these
+    steps are off by 7e-4 of the derivative at most (third order; dg), and the forward pass's error, 1e-5 of the outputs' size, divided by
+    twice the step is 2e-4 of it: 2e-3 leaves twice that."""
+    B, H, N = 1, 2, 150
+    data = draw(B, H, H, N, d, 21, dtype, rates=[0.01, 0.2])
+    kv_in, _ = states(B, H, d, 4)
+    base = Call(data, kv_in=kv_in, path=path)
+    base.fwd()
+    base.bwd()
+    base.done()
+    for i, grad, step in ((3, "dg", 2.0 ** -7), (4, "dbeta", 0.25), (None, "grad_kv_in", 0.25)):
+        along = base.results()[grad].double().cpu()
+        way, loss = along / along.norm(), []
+        for sign in (1, -1):
+            moved = [(x.double() + sign * step * way).float() if j == i else x for j, x in enumerate(data)]
+            call = Call(moved, kv_in=kv_in if i else (kv_in.double() + sign * step * way).float(), path=path)
+            call.fwd()
+            call.done()
+            loss.append((call.o.double() * call.do.double()).sum().item())
+        want = along.norm().item()
+        assert abs((loss[0] - loss[1]) / (2 * step) - want) <= 2e-3 * want, grad
