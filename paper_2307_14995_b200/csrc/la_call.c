@@ -98,6 +98,12 @@ static int slot(char kind, PyObject* a, uint64_t* out) {
   return !(*out == (uint64_t)-1 && PyErr_Occurred());
 }
 
+// The product of a shape's sizes; -1 where it is more than 63 bits, which the function called refuses by the shape.
+static long long product(long long a, long long b) {
+  long long x;
+  return a < 0 || b < 0 || __builtin_mul_overflow(a, b, &x) ? -1 : x;
+}
+
 // The type (0: bf16, 1: fp32; anything else: any) and the number of elements (-1: any) that a letter stands for.
 static void expected(char kind, const void* shape, int is_norm, int* dtype, long long* count) {
   *dtype = -1;
@@ -106,14 +112,14 @@ static void expected(char kind, const void* shape, int is_norm, int* dtype, long
   if (is_norm) {
     const NormShape* const s = (const NormShape*)shape;
     *dtype = kind == 'X' ? s->res_dtype : kind == 'Y' ? s->dtype : 1;
-    *count = kind == 'F' ? s->D : s->rows * s->D;
+    *count = kind == 'F' ? s->D : product(s->rows, s->D);
     return;
   }
   const DeltaShape* const s = (const DeltaShape*)shape;
-  const long long rows = (long long)s->B * s->N;
+  const long long rows = product(s->B, s->N);
   *dtype = kind == 'Q' || kind == 'V' ? s->in_dtype : kind == 'P' || kind == 'O' ? s->out_dtype : 1;
-  *count = kind == 'Q' || kind == 'P' ? rows * s->Hk * s->d : kind == 'V' || kind == 'O' ? rows * s->H * s->e
-         : kind == 'G' ? rows * s->H : (long long)s->B * s->H * s->d * s->e;
+  *count = kind == 'Q' || kind == 'P' ? product(product(rows, s->Hk), s->d) : kind == 'V' || kind == 'O' ? product(product(rows, s->H), s->e)
+         : kind == 'G' ? product(rows, s->H) : product(product(product(s->B, s->H), s->d), s->e);
 }
 
 static int as_long(PyObject* x, long long* out) {  // takes the reference

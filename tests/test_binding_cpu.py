@@ -157,3 +157,36 @@ def test_the_extension_module_is_this_interpreters():
     from paper_2307_14995_b200 import _la_call
     suffix = importlib.machinery.EXTENSION_SUFFIXES[0]  # the one with the interpreter's tag
     assert suffix != ".so" and _la_call.__file__.endswith("_la_call" + suffix)
+
+
+class OnDevice:
+    """What the binding asks of a tensor."""
+
+    def __init__(self, dtype, numel):
+        self.dtype, self.count = dtype, numel
+
+    def numel(self):
+        return self.count
+
+    def get_device(self):
+        return 0
+
+    def is_contiguous(self):
+        return True
+
+    def data_ptr(self):
+        return 256
+
+
+@pytest.mark.parametrize("numel", [0, 4])
+def test_sizes_beyond_63_bits_are_refused_by_the_shape(monkeypatch, numel):
+    """However many elements the tensors have, and whatever the product of the sizes is modulo 2^64."""
+    monkeypatch.setattr(la, "_current_device", lambda: 0)
+    monkeypatch.setattr(la, "_stream", lambda s: 0)
+    bf, f = OnDevice(torch.bfloat16, numel), OnDevice(torch.float32, numel)
+    norm = la.make_block_norm_shape(1 << 60, 16, torch.bfloat16, torch.bfloat16)
+    with pytest.raises(la.LaError):
+        la.la_block_norm_fwd(norm, bf, bf, h=bf)
+    delta = la.make_delta_shape(1 << 16, 1 << 16, 1 << 30, 128, 128, torch.bfloat16, torch.bfloat16)
+    with pytest.raises(la.LaError):
+        la.la_delta_steps(delta, bf, bf, bf, OnDevice(torch.float32, 1 << 62), OnDevice(torch.float32, 1 << 62), OnDevice(torch.float32, 1 << 46), bf)
