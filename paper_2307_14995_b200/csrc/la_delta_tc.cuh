@@ -1475,11 +1475,7 @@ x_gradient_kernel(const __grid_constant__ XMaps maps, const __grid_constant__ De
       for (int o = 16; o > 0; o >>= 1) whole += __shfl_xor_sync(0xffffffffu, whole, o);
       X_WAIT(sm.bars[XG_MMA], mma, 104);
       mma ^= 1;
-      if (tid == 0) {
-        uint64_t* const bar = expect(sm, XG_QK, 2 * TOK);
-        for (int x = 0; x < PANELS; ++x) tma_load_4d(sm.a + x * 16384, &maps.q, bar, x * 64, c * 128, hk, b);
-        for (int x = 0; x < PANELS; ++x) tma_load_4d(sm.a + TOK + x * 16384, &maps.k, bar, x * 64, c * 128, hk, b);
-      }
+      if (tid == 0) load_qk(expect(sm, XG_QK, 2 * TOK));
       X_WAIT(sm.bars[XG_QK], second, 105);
       float dot_a = 0.f, dot_b = 0.f;
       if (feat)
