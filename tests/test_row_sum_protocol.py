@@ -18,31 +18,23 @@ def body(start, end):
     return text[at:text.index(end, at)]
 
 
-def turns():
-    """Whether a call of RowSum turns its slot over."""
-    text = body("struct RowSum {", "};")
-    return "int& slot" in text and re.search(r"slot \^= 1;\s*return x;", text) is not None
-
-
 def slots_named(kernel, end):
     """The slots that the calls of a direct kernel name, in the order of its source."""
-    return re.findall(r"\bsum\(\w+, (\w+), \w+\)", body("void __launch_bounds__(LANES%s) %s(" % (" > THREADS ? LANES : THREADS" if "fwd" in kernel else "", kernel), end))
+    return re.findall(r"\bsum\(\w+, (\d), \w+\)", body("void __launch_bounds__(LANES%s) %s(" % (" > THREADS ? LANES : THREADS" if "fwd" in kernel else "", kernel), end))
 
 
-def overlaps(rows, meet_after_row):
-    """rows: for every row the slots that its sums name ("slot": the one that turns over).  Slots written while they may be read."""
-    own, at, found = 0, 0, []  # at: meetings so far
-    read = {}                   # slot -> the last interval between meetings in which it was read
-    for row in rows:
-        for name in row:
-            slot = own if name == "slot" else int(name)
-            if read.get(slot) == at:
-                found.append(slot)
+def overlaps(ops):
+    """ops: the sums' slots in order, "meet" for a barrier besides theirs.  Slots written while they may be read."""
+    at, found = 0, []  # at: meetings so far
+    read = {}          # slot -> the last interval between meetings in which it was read
+    for op in ops:
+        if op == "meet":
             at += 1
-            read[slot] = at
-            if turns():
-                own ^= 1
-        at += meet_after_row
+            continue
+        if read.get(op) == at:
+            found.append(op)
+        at += 1
+        read[op] = at
     return found
 
 
@@ -55,7 +47,10 @@ BACKWARD = ("block_norm_bwd_kernel", "struct RingRow")
 @pytest.mark.parametrize("want_n", [True, False])
 def test_forward(rows, post_norm, want_n):
     of_y, of_h = slots_named(*FORWARD)
-    assert overlaps([[of_y] * post_norm + [of_h] * want_n] * rows, 0) == []
+    text = body("block_norm_fwd_kernel(", FORWARD[1])
+    meets = "alternate = a.post_norm && a.n;" in text and re.search(r"if \(!alternate\) __syncthreads\(\);\s*if \(!a\.n\) continue;", text) is not None
+    between = ["meet"] if meets and not (post_norm and want_n) else []
+    assert overlaps(([of_y] * post_norm + between + [of_h] * want_n) * rows) == []
 
 
 @pytest.mark.parametrize("rows", [1, 2, 3, 10])
@@ -63,10 +58,10 @@ def test_forward(rows, post_norm, want_n):
 @pytest.mark.parametrize("dn", [True, False])
 def test_backward(rows, post_norm, dn):
     of_y, of_h, of_dot, of_p = slots_named(*BACKWARD)
-    meets = "__syncthreads" in body("void __launch_bounds__(LANES) block_norm_bwd_kernel(", "struct RingRow")
-    assert overlaps([[of_y] * post_norm + [of_h, of_dot] * dn + [of_p] * post_norm] * rows, meets) == []
+    meets = re.search(r"__syncthreads\(\);\s*\}\s*float\* const part", body("block_norm_bwd_kernel(", BACKWARD[1])) is not None
+    assert overlaps(([of_y] * post_norm + [of_h, of_dot] * dn + [of_p] * post_norm + ["meet"] * meets) * rows) == []
 
 
 def test_a_slot_of_its_own_for_every_sum_would_be_met():
     """The model finds the fault: slots by what is summed up, where a row has one sum only."""
-    assert overlaps([["0", "1"]] * 5, 0) == [] and overlaps([["1"]] * 5, 0) != []
+    assert overlaps(["0", "1"] * 5) == [] and overlaps(["1"] * 5) != []
