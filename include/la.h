@@ -304,7 +304,8 @@ la_status la_decode_steps(const la_shape* shape, const void* q, const void* k, c
  *   states       [B,H,d,e] fp32, as those of la_fwd; kv_in / kv_out / grad_kv_out / grad_kv_in may be NULL.
  * d == e in {64, 128}; 1 <= Hk <= H, H a multiple of Hk; B * H <= 65535; types as in la_shape.  Accumulation and states are fp32.  bf16
  * inputs run on the tensor cores (path AUTO or TENSOR), where operands formed on chip are carried as two bf16 terms (results
- * in fp32 are then off by 4e-6 to 7e-6 in the relative 2-norm); fp32 inputs, and path SIMT, on the CUDA cores (3e-7).
+ * in fp32 are then off by up to 8e-6 of a head's 2-norm, dg of a head that hardly forgets by up to 1.4e-5); fp32 inputs, and path SIMT, on
+ * the CUDA cores (5e-7 and 1e-6).
  * A NaN or infinity of a token reaches all tokens of its chunk (128 tokens; CUDA cores 64) and those after it, in the heads that read it.
  * Sequences one after the other in one row of tokens, each from a zero state: g = -inf at the first token of each.
  *
@@ -350,8 +351,9 @@ la_status la_delta_steps(const la_delta_shape* shape, const void* q, const void*
  *   la_block_norm_bwd    gradients of <h, dh> + <n, dn>, everything made again from x, y and u; dh or dn may be NULL (zero), not both;
  *                        dw_post, ds, dw_pre [D] fp32 may be NULL; du is required with u.  workspace:
  *                        la_block_norm_workspace_bytes(shape), 256-byte aligned.
- * dtype BF16 with res_dtype BF16 or F32, or both F32; 1 <= D <= 16384 (a multiple of 8 moves 16 bytes at a time), rows >= 1.  Sums
- * are fp32 and run in a fixed order.
+ * dtype BF16 with res_dtype BF16 or F32, or both F32; 1 <= D <= 16384, rows >= 1.  Sums are fp32 and run in a fixed
+ * order, which depends on the shape alone; one kernel takes few rows forward and another many, so that a row's last bits may depend on how
+ * many there are.  Sigmoids of fp32 gates are good to 5.4e-7 of their own size; those of bf16 gates to |u| 7.3e-8 more.
  */
 #define LA_GATE_PLAIN 0
 #define LA_GATE_SIGMOID 1

@@ -14,7 +14,7 @@
 // 5.7 / 5.4, 2400 30.5 / 22.6; 1024 features 296 rows 3.0 / 4.7, 2400 8.8 / 9.2, 4800 16.1 / 14.3.  Rows that are not aligned it takes in any
 // number, since the other form loads them value by value: 1003 features one row 4.6 / 4.9, 296 4.9 / 5.8, 301 features 3001 rows 12.3 / 8.7, 5001
 // features one row 7.9 / 6.1, 296 15.8 / 12.3.  Backward always, where it fits into
-// shared memory (up to 8192 features; fp32 with a gate up to 5590): 4096 features one row 16 / 10, 296 rows 39 / 15, 4800 rows 343 / 83.
+// shared memory (up to 8192 features; fp32 with a gate up to 5608, 5601 where that is no multiple of eight): 4096 features one row 16 / 10, 296 rows 39 / 15, 4800 rows 343 / 83.
 #pragma once
 #include "la_block_norm.cuh"
 
@@ -185,7 +185,7 @@ __global__ void __launch_bounds__(LANES > THREADS ? LANES : THREADS) block_norm_
 }
 
 // For rows that the ring does not take.  A row's values and the sums over tokens do not fit in the registers together: the sums are in
-// shared memory [3][D], and what a row has is read again (from L2) where it is used.  4096 x 16384 in bf16: 824 us, all in registers 1775.
+// shared memory [3][D], and what a row has is read again (from L2) where it is used.  4096 x 16384 in bf16: 860 us, all in registers 1775.
 template <typename T, typename TR, int LANES, int NV, bool VEC>
 __global__ void __launch_bounds__(LANES) block_norm_bwd_kernel(const BlockNormArgs a) {
   extern __shared__ float sums[];
@@ -305,15 +305,15 @@ __global__ void __launch_bounds__(LANES) block_norm_bwd_kernel(const BlockNormAr
 // The same with the rows of a thread block's next turns on their way while it works on one: every thread copies what it will read
 // itself into a ring of S stages in shared memory (cp.async), so that nobody waits for anybody but in the row sums.  One thread block
 // of 512 threads to an SM, 512 / LANES rows at a time, each row's threads with a barrier of their own; sums over tokens in registers to
-// the end.  Forward and backward, us (at the copy bandwidth): 65536 x 4096 in bf16 431 and 932 (409 and 654), without the ring 739 and 4146;
-// 16384 x 4096 in fp32 212 and 337 (204 and 327); 16384 x 2048 in bf16 with the residual stream in fp32 85 and 133 (72 and 112).  What
+// the end.  Forward and backward, us (at the copy bandwidth): 65536 x 4096 in bf16 447 and 914 (409 and 654), without the ring 739 and 4146;
+// 16384 x 4096 in fp32 209 and 338 (204 and 327); 16384 x 2048 in bf16 with the residual stream in fp32 86 and 134 (72 and 112).  What
 // is left backward is the meeting of a row's threads, with one row of 4096 features at a time; instructions are issued in 61 % of the clocks.
 //
 // Rows whose width is no multiple of eight begin anywhere in 16 bytes.  They move from the 16-byte boundary before them, and what a unit
 // has of the rows beside is left out; all rows of a thread block begin at the same place (the grid is a multiple of eight, and a block
 // takes rows that are a grid apart), so that a thread's features are the same in all.  us, and with pairs of features (4 bytes of bf16) that
-// need an even beginning alone: 16384 x 1003 in fp32 70 and 117 (91 and 159), in bf16 62 and 112 (73 and 123); 16384 x 5001 in bf16 339 and 809 (490
-// and 1367).  A row's first and last units, whose values go one by one, are what aligned rows do not have (16384 x 1000: 34 and 63).
+// need an even beginning alone: 16384 x 1003 in fp32 71 and 118 (91 and 159), in bf16 63 and 113 (73 and 123); 16384 x 5001 in bf16 344 and 818 (490
+// and 1367).  A row's first and last units, whose values go one by one, are what aligned rows do not have (16384 x 1000 in bf16: 44 and 79).
 constexpr int RING = 512;
 template <int BYTES>
 __device__ __forceinline__ void copy(uint32_t to, const void* from) {
