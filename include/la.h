@@ -304,8 +304,8 @@ la_status la_decode_steps(const la_shape* shape, const void* q, const void* k, c
  *   states       [B,H,d,e] fp32, as those of la_fwd; kv_in / kv_out / grad_kv_out / grad_kv_in may be NULL.
  * d == e in {64, 128}; 1 <= Hk <= H, H a multiple of Hk; B * H <= 65535; types as in la_shape.  Accumulation and states are fp32.  bf16
  * inputs run on the tensor cores (path AUTO or TENSOR), where operands formed on chip are carried as two bf16 terms (results
- * in fp32 are then off by up to 8e-6 of a head's 2-norm, dg of a head that hardly forgets by up to 1.4e-5); fp32 inputs, and path SIMT, on
- * the CUDA cores (5e-7 and 1e-6).
+ * in fp32 are then off by up to 8e-6 of a head's 2-norm; dg, a sum of products of a state with its gradient, by that of the products: where they
+ * nearly cancel by more of itself, 4e-5 seen); fp32 inputs, and path SIMT, on the CUDA cores (5e-7, dg 3e-6).
  * A NaN or infinity of a token reaches all tokens of its chunk (128 tokens; CUDA cores 64) and those after it, in the heads that read it.
  * Sequences one after the other in one row of tokens, each from a zero state: g = -inf at the first token of each.
  *

@@ -18,7 +18,7 @@
 //
 // As in the walk, operands formed on chip from fp32 values are two bf16 terms hi + lo, off by 2^-16 of a value at most and by 2.7e-6 of
 // it on the root of the mean square: in a result that passes six of them 6e-6 (measured, relative 2-norm: outputs, states and gradients up
-// to 8e-6 in a head, dg of a head that hardly forgets up to 1.4e-5).  Products of two such operands leave
+// to 8e-6 in a head, dg up to 4e-5 where the products of state and gradient that it sums up nearly cancel).  Products of two such operands leave
 // out lo x lo, except where it comes with the columns of an operand [hi | lo].  Sums are fp32, in an order that depends on the shape
 // alone: the products of lo terms first, so that fewer additions meet a large sum, whose rounding is towards zero.
 //
